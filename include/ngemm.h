@@ -374,6 +374,101 @@ ngemm_status ngemm_run_batched_u8s8s32(ngemm_ctx *ctx, int count, const ngemm_pr
                                        void *workspace_dev, size_t workspace_bytes,
                                        void *hip_stream);
 
+/*
+ * ---- Attention on an 8-bit key-value cache in pages ----
+ *
+ * What a transformer block needs between the products above: the rows of K and V that its projections give are
+ * quantised into a cache as they are written, and queries attend to them there, or to rows that are not in a cache.
+ *
+ * Element types of rows (queries, keys, values, outputs).  A token's row of one head is head_dim consecutive
+ * elements; tokens and heads lie token_stride and head_stride elements apart, in any order.
+ */
+typedef enum {
+    NGEMM_F32 = 0,               /* kv_write and kv_read only */
+    NGEMM_F16 = 1,
+    NGEMM_BF16 = 2
+} ngemm_type;
+
+typedef struct ngemm_kv_cache ngemm_kv_cache; /* opaque host descriptor of a caller-owned device buffer */
+
+/*
+ * A cache of num_pages pages of page_tokens tokens (a multiple of 16) of kv_heads heads of head_dim elements (a multiple
+ * of 16 up to 256), in one device buffer of ngemm_kv_cache_bytes bytes (0 for sizes that are not allowed):
+ *     [num_pages][kv_heads][page_tokens / 16] blocks of 32 head_dim + 128 bytes, each
+ *         K codes  int8    [16 tokens][head_dim]
+ *         V codes  int8    [head_dim][16 tokens]      (the attention's second product runs along the tokens)
+ *         K scales float   [16 tokens]
+ *         V scales float   [16 tokens]
+ * A row is code * scale: per token and head scale = amax / 127 (one division) and code = rint(127 x / amax), ties to
+ * even, amax = max |x| over the row.  A row of zeros has scale 0; a row that holds an infinity or a NaN has scale
+ * NaN and codes 0, so that it is NaN throughout when it is read.
+ *
+ * ngemm_kv_cache_create describes a buffer (16-byte aligned; its content is left alone: a buffer's pages are written
+ * before they are read); the descriptor is a host object owned by the caller until ngemm_kv_cache_free.
+ */
+size_t ngemm_kv_cache_bytes(int64_t num_pages, int64_t page_tokens, int64_t kv_heads, int64_t head_dim);
+ngemm_status ngemm_kv_cache_create(ngemm_ctx *ctx, int64_t num_pages, int64_t page_tokens, int64_t kv_heads, int64_t head_dim,
+                                   void *cache_dev, size_t cache_bytes, ngemm_kv_cache **out);
+ngemm_status ngemm_kv_cache_free(ngemm_kv_cache *cache);
+
+/*
+ * Quantise `tokens` rows of K and V per head into the cache (write), or read them back (read; each element is
+ * code * scale as a float, then rounded to the type).  The rows are packed: sequence b has the rows offsets[b] .. offsets[b + 1] - 1
+ * (offsets_dev: int32 [batch + 1], not falling, from 0 to tokens), which stand at the positions starts[b], starts[b] + 1, ...
+ * of the sequence (starts_dev: int32 [batch], or NULL for 0).  Position t of sequence b lies in page
+ * pages[b * pages_stride + t / page_tokens] (pages_dev: int32, pages_stride entries per sequence), at t % page_tokens.
+ * Two tokens of a write must not fall on the same place.  Device data is not validated on the host; a position that is
+ * negative, past pages_stride pages or in a page that is not one of the cache's is not written, and reads as 0.
+ * Rows of the usual strides and 16-byte alignment move in 16-byte pieces, others element by element.
+ */
+ngemm_status ngemm_kv_write(ngemm_ctx *ctx, const ngemm_kv_cache *cache, ngemm_type type, int64_t batch, int64_t tokens,
+                            const void *K_dev, int64_t k_token_stride, int64_t k_head_stride,
+                            const void *V_dev, int64_t v_token_stride, int64_t v_head_stride,
+                            const int32_t *offsets_dev, const int32_t *starts_dev,
+                            const int32_t *pages_dev, int64_t pages_stride, void *hip_stream);
+ngemm_status ngemm_kv_read(ngemm_ctx *ctx, const ngemm_kv_cache *cache, ngemm_type type, int64_t batch, int64_t tokens,
+                           void *K_dev, int64_t k_token_stride, int64_t k_head_stride,
+                           void *V_dev, int64_t v_token_stride, int64_t v_head_stride,
+                           const int32_t *offsets_dev, const int32_t *starts_dev,
+                           const int32_t *pages_dev, int64_t pages_stride, void *hip_stream);
+
+/*
+ * One new token per sequence attends to the cache (f16 or bf16):
+ *     O[b][h] = sum_t p_t V_t / sum_t p_t,  p_t = exp(scale <Q[b][h], K_t> - max),  t < lengths[b],
+ * with the K and V of head h / (q_heads / kv_heads) (q_heads a multiple of the cache's kv_heads).  lengths_dev: int32
+ * [batch], the tokens of each sequence in the cache, the new one included; at most max_length of them are read.  A
+ * sequence without tokens gives 0; tokens in a page that is not one of the cache's are left out.  Softmax
+ * statistics and sums are float; the weights p_t times V's scales enter the second product as f16, relative
+ * to the largest.  Scores are products of the 8-bit codes and the query as f16 (bf16 queries relative to a power of
+ * two per head).  Long sequences are split over workgroups; the parts meet in the workspace and are joined in their order, so that
+ * equal calls give equal bits.  The workspace has to be 16-byte aligned and must not be in use by a call on another stream.
+ */
+size_t ngemm_attention_decode_workspace_bytes(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t max_length);
+ngemm_status ngemm_attention_decode(ngemm_ctx *ctx, const ngemm_kv_cache *cache, ngemm_type type, int64_t batch, int64_t q_heads,
+                                    const void *Q_dev, int64_t q_token_stride, int64_t q_head_stride,
+                                    const int32_t *lengths_dev, int64_t max_length,
+                                    const int32_t *pages_dev, int64_t pages_stride, float scale,
+                                    void *O_dev, int64_t o_token_stride, int64_t o_head_stride,
+                                    void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * Whole prompts attend to themselves, or to a longer context that ends with them (f16 or bf16).  Packed sequences: b has
+ * the query rows q_offsets[b] .. q_offsets[b + 1] - 1 and the K and V rows k_offsets[b] .. k_offsets[b + 1] - 1 (int32
+ * [batch + 1] on the device; k_offsets_dev NULL: the same as the queries').  With n queries and m keys, query i sees the
+ * keys j <= i + m - n when `causal` is not 0, all of them when it is 0; a query that sees none gives 0, and what the K and V rows that
+ * it does not see hold is without effect, infinities and NaN included.  q_heads a multiple of kv_heads, head_dim a multiple of 16 up to 256.
+ * Softmax statistics and sums are float; the weights enter the second product in the rows' type.
+ */
+size_t ngemm_attention_prompt_workspace_bytes(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
+                                              int64_t q_tokens, int64_t k_tokens);
+ngemm_status ngemm_attention_prompt(ngemm_ctx *ctx, ngemm_type type, int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
+                                    int64_t q_tokens, const void *Q_dev, int64_t q_token_stride, int64_t q_head_stride,
+                                    int64_t k_tokens, const void *K_dev, int64_t k_token_stride, int64_t k_head_stride,
+                                    const void *V_dev, int64_t v_token_stride, int64_t v_head_stride,
+                                    const int32_t *q_offsets_dev, const int32_t *k_offsets_dev, int causal, float scale,
+                                    void *O_dev, int64_t o_token_stride, int64_t o_head_stride,
+                                    void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
 #ifdef __cplusplus
 }
 #endif

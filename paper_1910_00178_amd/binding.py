@@ -31,12 +31,18 @@ NGEMM_KERNEL_TILE_256 = 3
 NGEMM_KERNEL_SPLIT_K = 4
 NGEMM_KERNEL_TILE_192 = 5
 
+NGEMM_F32 = 0
+NGEMM_F16 = 1
+NGEMM_BF16 = 2
+
 EXPORTS = (
     "ngemm_status_string", "ngemm_create", "ngemm_destroy", "ngemm_set_kernel", "ngemm_tune_u8s8s32", "ngemm_tuned_kernel", "ngemm_set_max_workgroups",
     "ngemm_packed_b_bytes", "ngemm_pack_b", "ngemm_pack_b_u8", "ngemm_packed_b_free", "ngemm_packed_b_shape",
     "ngemm_workspace_bytes", "ngemm_run_u8s8s32", "ngemm_run_u8s8s32_static", "ngemm_run_s8s8s32", "ngemm_run_u8u8s32", "ngemm_packed_b_bytes_s16", "ngemm_pack_b_s16", "ngemm_run_s16s16s32", "ngemm_run_u8s8u8_requant",
     "ngemm_run_u8s8u8_requant_channel", "ngemm_unpacked_workspace_bytes", "ngemm_run_u8s8s32_unpacked",
     "ngemm_batched_workspace_bytes", "ngemm_run_batched_u8s8s32",
+    "ngemm_kv_cache_bytes", "ngemm_kv_cache_create", "ngemm_kv_cache_free", "ngemm_kv_write", "ngemm_kv_read",
+    "ngemm_attention_decode_workspace_bytes", "ngemm_attention_decode", "ngemm_attention_prompt_workspace_bytes", "ngemm_attention_prompt",
 )
 
 
@@ -102,6 +108,22 @@ _lib.ngemm_run_u8s8s32_unpacked.restype = _int
 _lib.ngemm_batched_workspace_bytes.restype = _sz
 _lib.ngemm_batched_workspace_bytes.argtypes = [_int, ctypes.POINTER(ngemm_problem)]
 _lib.ngemm_run_batched_u8s8s32.argtypes = [_p, _int, ctypes.POINTER(ngemm_problem), _p, _sz, _p]
+_lib.ngemm_kv_cache_bytes.restype = _sz
+_lib.ngemm_kv_cache_bytes.argtypes = [_i64, _i64, _i64, _i64]
+_lib.ngemm_kv_cache_create.argtypes = [_p, _i64, _i64, _i64, _i64, _p, _sz, ctypes.POINTER(_p)]
+_lib.ngemm_kv_cache_free.argtypes = [_p]
+_lib.ngemm_kv_write.argtypes = [_p, _p, _int, _i64, _i64, _p, _i64, _i64, _p, _i64, _i64, _p, _p, _p, _i64, _p]
+_lib.ngemm_kv_read.argtypes = list(_lib.ngemm_kv_write.argtypes)
+_lib.ngemm_attention_decode_workspace_bytes.restype = _sz
+_lib.ngemm_attention_decode_workspace_bytes.argtypes = [_i64, _i64, _i64, _i64, _i64]
+_lib.ngemm_attention_decode.argtypes = [_p, _p, _int, _i64, _i64, _p, _i64, _i64, _p, _i64, _p, _i64, _f32, _p, _i64, _i64, _p, _sz, _p]
+_lib.ngemm_attention_prompt_workspace_bytes.restype = _sz
+_lib.ngemm_attention_prompt_workspace_bytes.argtypes = [_i64, _i64, _i64, _i64, _i64, _i64]
+_lib.ngemm_attention_prompt.argtypes = [_p, _int, _i64, _i64, _i64, _i64, _i64, _p, _i64, _i64, _i64, _p, _i64, _i64, _p, _i64, _i64, _p, _p, _int,
+                                        _f32, _p, _i64, _i64, _p, _sz, _p]
+for _name in ("ngemm_kv_cache_create", "ngemm_kv_cache_free", "ngemm_kv_write", "ngemm_kv_read", "ngemm_attention_decode",
+              "ngemm_attention_prompt"):
+    getattr(_lib, _name).restype = _int
 for _name in ("ngemm_create", "ngemm_destroy", "ngemm_set_kernel", "ngemm_set_max_workgroups", "ngemm_pack_b", "ngemm_packed_b_free",
               "ngemm_packed_b_shape", "ngemm_run_u8s8s32", "ngemm_run_u8s8u8_requant",
               "ngemm_run_batched_u8s8s32"):
@@ -330,6 +352,62 @@ def ngemm_run_batched_u8s8s32(ctx, problems, workspace_dev=None, workspace_bytes
     _check(_lib.ngemm_run_batched_u8s8s32(ctx, len(problems), problems, _dev(workspace_dev),
                                           int(workspace_bytes), _stream(hip_stream)),
            "ngemm_run_batched_u8s8s32")
+
+
+def ngemm_kv_cache_bytes(num_pages, page_tokens, kv_heads, head_dim):
+    return int(_lib.ngemm_kv_cache_bytes(int(num_pages), int(page_tokens), int(kv_heads), int(head_dim)))
+
+
+def ngemm_kv_cache_create(ctx, num_pages, page_tokens, kv_heads, head_dim, cache_dev, cache_bytes):
+    h = _p()
+    _check(_lib.ngemm_kv_cache_create(ctx, int(num_pages), int(page_tokens), int(kv_heads), int(head_dim), _dev(cache_dev),
+                                      int(cache_bytes), ctypes.byref(h)), "ngemm_kv_cache_create")
+    return h
+
+
+def ngemm_kv_cache_free(cache):
+    _check(_lib.ngemm_kv_cache_free(cache), "ngemm_kv_cache_free")
+
+
+def ngemm_kv_write(ctx, cache, type, batch, tokens, K_dev, k_token_stride, k_head_stride, V_dev, v_token_stride, v_head_stride,
+                   offsets_dev, starts_dev, pages_dev, pages_stride, hip_stream=None):
+    _check(_lib.ngemm_kv_write(ctx, cache, int(type), int(batch), int(tokens), _dev(K_dev), int(k_token_stride), int(k_head_stride),
+                               _dev(V_dev), int(v_token_stride), int(v_head_stride), _dev(offsets_dev), _dev(starts_dev),
+                               _dev(pages_dev), int(pages_stride), _stream(hip_stream)), "ngemm_kv_write")
+
+
+def ngemm_kv_read(ctx, cache, type, batch, tokens, K_dev, k_token_stride, k_head_stride, V_dev, v_token_stride, v_head_stride,
+                  offsets_dev, starts_dev, pages_dev, pages_stride, hip_stream=None):
+    _check(_lib.ngemm_kv_read(ctx, cache, int(type), int(batch), int(tokens), _dev(K_dev), int(k_token_stride), int(k_head_stride),
+                              _dev(V_dev), int(v_token_stride), int(v_head_stride), _dev(offsets_dev), _dev(starts_dev),
+                              _dev(pages_dev), int(pages_stride), _stream(hip_stream)), "ngemm_kv_read")
+
+
+def ngemm_attention_decode_workspace_bytes(batch, q_heads, kv_heads, head_dim, max_length):
+    return int(_lib.ngemm_attention_decode_workspace_bytes(int(batch), int(q_heads), int(kv_heads), int(head_dim), int(max_length)))
+
+
+def ngemm_attention_decode(ctx, cache, type, batch, q_heads, Q_dev, q_token_stride, q_head_stride, lengths_dev, max_length, pages_dev,
+                           pages_stride, scale, O_dev, o_token_stride, o_head_stride, workspace_dev=None, workspace_bytes=0, hip_stream=None):
+    _check(_lib.ngemm_attention_decode(ctx, cache, int(type), int(batch), int(q_heads), _dev(Q_dev), int(q_token_stride), int(q_head_stride),
+                                       _dev(lengths_dev), int(max_length), _dev(pages_dev), int(pages_stride), float(scale),
+                                       _dev(O_dev), int(o_token_stride), int(o_head_stride), _dev(workspace_dev), int(workspace_bytes),
+                                       _stream(hip_stream)), "ngemm_attention_decode")
+
+
+def ngemm_attention_prompt_workspace_bytes(batch, q_heads, kv_heads, head_dim, q_tokens, k_tokens):
+    return int(_lib.ngemm_attention_prompt_workspace_bytes(int(batch), int(q_heads), int(kv_heads), int(head_dim), int(q_tokens), int(k_tokens)))
+
+
+def ngemm_attention_prompt(ctx, type, batch, q_heads, kv_heads, head_dim, q_tokens, Q_dev, q_token_stride, q_head_stride, k_tokens,
+                           K_dev, k_token_stride, k_head_stride, V_dev, v_token_stride, v_head_stride, q_offsets_dev, k_offsets_dev,
+                           causal, scale, O_dev, o_token_stride, o_head_stride, workspace_dev=None, workspace_bytes=0, hip_stream=None):
+    _check(_lib.ngemm_attention_prompt(ctx, int(type), int(batch), int(q_heads), int(kv_heads), int(head_dim), int(q_tokens), _dev(Q_dev),
+                                       int(q_token_stride), int(q_head_stride), int(k_tokens), _dev(K_dev), int(k_token_stride),
+                                       int(k_head_stride), _dev(V_dev), int(v_token_stride), int(v_head_stride), _dev(q_offsets_dev),
+                                       _dev(k_offsets_dev), int(bool(causal)), float(scale), _dev(O_dev), int(o_token_stride),
+                                       int(o_head_stride), _dev(workspace_dev), int(workspace_bytes), _stream(hip_stream)),
+           "ngemm_attention_prompt")
 
 
 # The calls above that a program makes per product, weight or batch: natively where all arguments are of the usual types,

@@ -3,10 +3,12 @@ import os
 import subprocess
 import sys
 import sysconfig
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SRC = os.path.join(HERE, "csrc", "ngemm.hip")
+SOURCES = [os.path.join(HERE, "csrc", name) for name in ("ngemm.hip", "attention.hip")]
 LIB = os.path.join(HERE, "libngemm.so")
 CALLS_SRC = os.path.join(HERE, "csrc", "calls.c")
 CALLS = os.path.join(HERE, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
@@ -15,12 +17,12 @@ HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
     "-O3", "--offload-arch=gfx950",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
-    "-ffp-contract=off", "-fPIC", "-shared", "-std=c++17",
+    "-ffp-contract=off", "-fPIC", "-std=c++17",
     "-I" + os.path.join(ROOT, "include"),
     "-Wall", "-Wextra", "-Wno-pass-failed",
-    "-Wl,--no-undefined",        # a kernel the host pass failed to emit must fail the build, not the first load
 ]
-
+LINK = ["-shared", "--offload-arch=gfx950",
+        "-Wl,--no-undefined"]    # a kernel the host pass failed to emit must fail the build, not the first load
 
 CC = os.environ.get("CC", "gcc")
 CALLS_FLAGS = ["-O2", "-std=gnu11", "-fPIC", "-shared", "-Wall", "-Wextra", "-Wno-cast-function-type", "-Wno-missing-field-initializers",
@@ -28,7 +30,7 @@ CALLS_FLAGS = ["-O2", "-std=gnu11", "-fPIC", "-shared", "-Wall", "-Wextra", "-Wn
 
 
 def _compile(cmd, src, lib, verbose):
-    cmd = [*cmd, "-o", lib, src]
+    cmd = [*cmd, "-o", lib, *([src] if isinstance(src, str) else src)]
     if verbose:
         print(" ".join(cmd), flush=True)
     res = subprocess.run(cmd, stdout=subprocess.PIPE, stderr=subprocess.STDOUT, text=True)
@@ -43,7 +45,10 @@ def _compile(cmd, src, lib, verbose):
 def build_library(verbose=False):
     """The HIP library, and the binding's native calls beside it."""
     _compile([CC, *CALLS_FLAGS], CALLS_SRC, CALLS, verbose)
-    return _compile([HIPCC, *FLAGS], SRC, LIB, verbose)
+    with tempfile.TemporaryDirectory() as at, ThreadPoolExecutor(len(SOURCES)) as pool:
+        objects = [os.path.join(at, os.path.basename(src) + ".o") for src in SOURCES]
+        list(pool.map(lambda src, obj: _compile([HIPCC, *FLAGS, "-c"], src, obj, verbose), SOURCES, objects))
+        return _compile([HIPCC, *LINK], objects, LIB, verbose)
 
 
 if __name__ == "__main__":

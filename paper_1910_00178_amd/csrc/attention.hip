@@ -1,0 +1,222 @@
+// Host side of the key-value cache and the attention calls of include/ngemm.h: argument validation and launches.
+#include "ngemm.h"
+#include "ngemm_host.h"
+#include "attention.h"
+
+#include <cmath>
+#include <new>
+
+using namespace ngemm;
+
+struct ngemm_kv_cache {
+    uint32_t magic;
+    int device;
+    int64_t num_pages, page_tokens, kv_heads, head_dim;
+    uint8_t *data;           // device, caller-owned
+};
+
+namespace {
+
+constexpr uint32_t kCacheMagic = 0x4e474b56u;   // "NGKV"
+constexpr int64_t kMaxCount = 0x7fffffff - 4096;
+constexpr int64_t kMaxStride = 1ll << 40;       // elements; products with a row's number stay within 64 bits
+
+bool cache_ok(const ngemm_kv_cache *c) { return c && c->magic == kCacheMagic; }
+
+bool head_dim_ok(int64_t d) { return d >= 16 && d <= 256 && d % 16 == 0; }
+
+int64_t elem_bytes(int type) { return type == NGEMM_F32 ? 4 : 2; }
+
+// Rows that a call reads may overlap (a stride of 0 gives every token or head the same row).
+ngemm_status check_rows(const Rows &r, int type, int64_t tokens, int64_t heads, int64_t head_dim, bool written)
+{
+    if (tokens == 0) return NGEMM_OK;
+    if (!r.data || ((uintptr_t)r.data & (elem_bytes(type) - 1)) != 0) return NGEMM_ERR_INVALID_ARG;
+    const int64_t t = r.token_stride, h = r.head_stride;
+    if (t < 0 || h < 0 || t > kMaxStride || h > kMaxStride) return NGEMM_ERR_BAD_SHAPE;
+    if (written) {                                       // no two elements at one place: heads inside tokens or tokens inside heads
+        const bool heads_inside = (heads == 1 || h >= head_dim) && (tokens == 1 || t >= (heads - 1) * h + head_dim);
+        const bool tokens_inside = (tokens == 1 || t >= head_dim) && (heads == 1 || h >= (tokens - 1) * t + head_dim);
+        if (!heads_inside && !tokens_inside) return NGEMM_ERR_BAD_SHAPE;
+    }
+    return NGEMM_OK;
+}
+
+CacheView view_of(const ngemm_kv_cache *c, const int32_t *pages, int64_t pages_stride)
+{
+    return CacheView{c->data, pages, pages_stride, (int32_t)c->num_pages, (int32_t)c->kv_heads, (int32_t)c->head_dim,
+                     (int32_t)(c->page_tokens / kBlockTokens)};
+}
+
+ngemm_status launched() { return hipGetLastError() == hipSuccess ? NGEMM_OK : NGEMM_ERR_DEVICE; }
+
+ngemm_status move_rows(bool write, ngemm_ctx *ctx, const ngemm_kv_cache *cache, int type, int64_t batch, int64_t tokens, Rows k, Rows v,
+                       const int32_t *offsets, const int32_t *starts, const int32_t *pages, int64_t pages_stride, void *stream)
+{
+    if (!ctx_ok(ctx) || !cache_ok(cache) || cache->device != ctx->device) return NGEMM_ERR_INVALID_ARG;
+    if (type != NGEMM_F32 && type != NGEMM_F16 && type != NGEMM_BF16) return NGEMM_ERR_INVALID_ARG;
+    if (batch < 0 || tokens < 0 || batch > kMaxCount || tokens > kMaxCount || pages_stride < 0 || pages_stride > kMaxCount) return NGEMM_ERR_BAD_SHAPE;
+    if (tokens == 0) return NGEMM_OK;
+    if (batch == 0) return NGEMM_ERR_BAD_SHAPE;
+    if (!offsets || !pages) return NGEMM_ERR_INVALID_ARG;
+    for (const Rows &r : {k, v})
+        if (const ngemm_status s = check_rows(r, type, tokens, cache->kv_heads, cache->head_dim, !write); s != NGEMM_OK) return s;
+    const int64_t groups = (tokens * cache->kv_heads + 3) / 4;
+    if (groups > kMaxCount) return NGEMM_ERR_BAD_SHAPE;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return NGEMM_ERR_DEVICE;
+    const MoveArgs a{view_of(cache, pages, pages_stride), k, v, offsets, starts, (int32_t)batch, (int32_t)tokens};
+    const dim3 grid((unsigned)groups), block(256);
+    hipStream_t st = (hipStream_t)stream;
+    if (write) {
+        if (type == NGEMM_F32) hipLaunchKernelGGL(kv_write_kernel<F32>, grid, block, 0, st, a);
+        else if (type == NGEMM_F16) hipLaunchKernelGGL(kv_write_kernel<F16>, grid, block, 0, st, a);
+        else hipLaunchKernelGGL(kv_write_kernel<BF16>, grid, block, 0, st, a);
+    } else {
+        if (type == NGEMM_F32) hipLaunchKernelGGL(kv_read_kernel<F32>, grid, block, 0, st, a);
+        else if (type == NGEMM_F16) hipLaunchKernelGGL(kv_read_kernel<F16>, grid, block, 0, st, a);
+        else hipLaunchKernelGGL(kv_read_kernel<BF16>, grid, block, 0, st, a);
+    }
+    return launched();
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t ngemm_kv_cache_bytes(int64_t num_pages, int64_t page_tokens, int64_t kv_heads, int64_t head_dim)
+{
+    if (num_pages < 1 || num_pages > kMaxCount || page_tokens < kBlockTokens || page_tokens > (1 << 24) || page_tokens % kBlockTokens ||
+        kv_heads < 1 || kv_heads > 65536 || !head_dim_ok(head_dim))
+        return 0;
+    const __int128 bytes = (__int128)num_pages * kv_heads * page_tokens * (2 * head_dim + 8);
+    return bytes < ((__int128)1 << 62) ? (size_t)bytes : 0;
+}
+
+ngemm_status ngemm_kv_cache_create(ngemm_ctx *ctx, int64_t num_pages, int64_t page_tokens, int64_t kv_heads, int64_t head_dim,
+                                   void *cache_dev, size_t cache_bytes, ngemm_kv_cache **out)
+{
+    if (!out) return NGEMM_ERR_INVALID_ARG;
+    *out = nullptr;
+    if (!ctx_ok(ctx)) return NGEMM_ERR_INVALID_ARG;
+    const size_t need = ngemm_kv_cache_bytes(num_pages, page_tokens, kv_heads, head_dim);
+    if (need == 0) return NGEMM_ERR_BAD_SHAPE;
+    if (!cache_dev || ((uintptr_t)cache_dev & 15u) != 0) return NGEMM_ERR_INVALID_ARG;
+    if (cache_bytes < need) return NGEMM_ERR_BUFFER_TOO_SMALL;
+    ngemm_kv_cache *c = new (std::nothrow) ngemm_kv_cache{kCacheMagic, ctx->device, num_pages, page_tokens, kv_heads, head_dim, (uint8_t *)cache_dev};
+    if (!c) return NGEMM_ERR_DEVICE;
+    *out = c;
+    return NGEMM_OK;
+}
+
+ngemm_status ngemm_kv_cache_free(ngemm_kv_cache *cache)
+{
+    if (!cache) return NGEMM_OK;
+    if (!cache_ok(cache)) return NGEMM_ERR_INVALID_ARG;
+    cache->magic = 0;
+    delete cache;
+    return NGEMM_OK;
+}
+
+ngemm_status ngemm_kv_write(ngemm_ctx *ctx, const ngemm_kv_cache *cache, ngemm_type type, int64_t batch, int64_t tokens,
+                            const void *K_dev, int64_t k_token_stride, int64_t k_head_stride,
+                            const void *V_dev, int64_t v_token_stride, int64_t v_head_stride,
+                            const int32_t *offsets_dev, const int32_t *starts_dev,
+                            const int32_t *pages_dev, int64_t pages_stride, void *hip_stream)
+{
+    return move_rows(true, ctx, cache, type, batch, tokens, Rows{const_cast<void *>(K_dev), k_token_stride, k_head_stride},
+                     Rows{const_cast<void *>(V_dev), v_token_stride, v_head_stride}, offsets_dev, starts_dev, pages_dev, pages_stride, hip_stream);
+}
+
+ngemm_status ngemm_kv_read(ngemm_ctx *ctx, const ngemm_kv_cache *cache, ngemm_type type, int64_t batch, int64_t tokens,
+                           void *K_dev, int64_t k_token_stride, int64_t k_head_stride,
+                           void *V_dev, int64_t v_token_stride, int64_t v_head_stride,
+                           const int32_t *offsets_dev, const int32_t *starts_dev,
+                           const int32_t *pages_dev, int64_t pages_stride, void *hip_stream)
+{
+    return move_rows(false, ctx, cache, type, batch, tokens, Rows{K_dev, k_token_stride, k_head_stride},
+                     Rows{V_dev, v_token_stride, v_head_stride}, offsets_dev, starts_dev, pages_dev, pages_stride, hip_stream);
+}
+
+size_t ngemm_attention_decode_workspace_bytes(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t max_length)
+{
+    (void)batch; (void)q_heads; (void)kv_heads; (void)head_dim; (void)max_length;
+    return 0;
+}
+
+ngemm_status ngemm_attention_decode(ngemm_ctx *ctx, const ngemm_kv_cache *cache, ngemm_type type, int64_t batch, int64_t q_heads,
+                                    const void *Q_dev, int64_t q_token_stride, int64_t q_head_stride,
+                                    const int32_t *lengths_dev, int64_t max_length,
+                                    const int32_t *pages_dev, int64_t pages_stride, float scale,
+                                    void *O_dev, int64_t o_token_stride, int64_t o_head_stride,
+                                    void *workspace_dev, size_t workspace_bytes, void *hip_stream)
+{
+    if (!ctx_ok(ctx) || !cache_ok(cache) || cache->device != ctx->device) return NGEMM_ERR_INVALID_ARG;
+    if ((type != NGEMM_F16 && type != NGEMM_BF16) || !std::isfinite(scale)) return NGEMM_ERR_INVALID_ARG;
+    if (batch < 0 || batch > kMaxCount || q_heads < 1 || q_heads > 65536 || q_heads % cache->kv_heads || max_length < 0 || max_length > kMaxCount ||
+        pages_stride < 0 || pages_stride > kMaxCount || batch * q_heads > kMaxCount)
+        return NGEMM_ERR_BAD_SHAPE;
+    if (batch == 0) return NGEMM_OK;
+    if (!lengths_dev || (!pages_dev && max_length > 0)) return NGEMM_ERR_INVALID_ARG;
+    const Rows q{const_cast<void *>(Q_dev), q_token_stride, q_head_stride}, o{O_dev, o_token_stride, o_head_stride};
+    if (const ngemm_status s = check_rows(q, type, batch, q_heads, cache->head_dim, false); s != NGEMM_OK) return s;
+    if (const ngemm_status s = check_rows(o, type, batch, q_heads, cache->head_dim, true); s != NGEMM_OK) return s;
+    const size_t need = ngemm_attention_decode_workspace_bytes(batch, q_heads, cache->kv_heads, cache->head_dim, max_length);
+    if (need > 0 && !workspace_dev) return NGEMM_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return NGEMM_ERR_BUFFER_TOO_SMALL;
+    if (need > 0 && ((uintptr_t)workspace_dev & 15u) != 0) return NGEMM_ERR_INVALID_ARG;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return NGEMM_ERR_DEVICE;
+    const DecodeArgs a{view_of(cache, pages_dev, pages_stride), q, o, lengths_dev, (int32_t)batch, (int32_t)q_heads, (int32_t)max_length, scale};
+    const dim3 grid((unsigned)(batch * q_heads)), block(64);
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (type == NGEMM_F16) hipLaunchKernelGGL(attention_decode_kernel<F16>, grid, block, 0, st, a);
+    else hipLaunchKernelGGL(attention_decode_kernel<BF16>, grid, block, 0, st, a);
+    return launched();
+}
+
+size_t ngemm_attention_prompt_workspace_bytes(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
+                                              int64_t q_tokens, int64_t k_tokens)
+{
+    (void)batch; (void)q_heads; (void)kv_heads; (void)head_dim; (void)q_tokens; (void)k_tokens;
+    return 0;
+}
+
+ngemm_status ngemm_attention_prompt(ngemm_ctx *ctx, ngemm_type type, int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
+                                    int64_t q_tokens, const void *Q_dev, int64_t q_token_stride, int64_t q_head_stride,
+                                    int64_t k_tokens, const void *K_dev, int64_t k_token_stride, int64_t k_head_stride,
+                                    const void *V_dev, int64_t v_token_stride, int64_t v_head_stride,
+                                    const int32_t *q_offsets_dev, const int32_t *k_offsets_dev, int causal, float scale,
+                                    void *O_dev, int64_t o_token_stride, int64_t o_head_stride,
+                                    void *workspace_dev, size_t workspace_bytes, void *hip_stream)
+{
+    if (!ctx_ok(ctx)) return NGEMM_ERR_INVALID_ARG;
+    if ((type != NGEMM_F16 && type != NGEMM_BF16) || !std::isfinite(scale)) return NGEMM_ERR_INVALID_ARG;
+    if (batch < 0 || batch > kMaxCount || q_heads < 1 || q_heads > 65536 || kv_heads < 1 || q_heads % kv_heads || !head_dim_ok(head_dim) || q_tokens < 0 ||
+        k_tokens < 0 || q_tokens > kMaxCount || k_tokens > kMaxCount || q_tokens * q_heads > kMaxCount)
+        return NGEMM_ERR_BAD_SHAPE;
+    if (q_tokens == 0) return NGEMM_OK;
+    if (batch == 0 || (!k_offsets_dev && k_tokens != q_tokens)) return NGEMM_ERR_BAD_SHAPE;
+    if (!q_offsets_dev) return NGEMM_ERR_INVALID_ARG;
+    const Rows q{const_cast<void *>(Q_dev), q_token_stride, q_head_stride}, k{const_cast<void *>(K_dev), k_token_stride, k_head_stride},
+        v{const_cast<void *>(V_dev), v_token_stride, v_head_stride}, o{O_dev, o_token_stride, o_head_stride};
+    if (const ngemm_status s = check_rows(q, type, q_tokens, q_heads, head_dim, false); s != NGEMM_OK) return s;
+    if (const ngemm_status s = check_rows(k, type, k_tokens, kv_heads, head_dim, false); s != NGEMM_OK) return s;
+    if (const ngemm_status s = check_rows(v, type, k_tokens, kv_heads, head_dim, false); s != NGEMM_OK) return s;
+    if (const ngemm_status s = check_rows(o, type, q_tokens, q_heads, head_dim, true); s != NGEMM_OK) return s;
+    const size_t need = ngemm_attention_prompt_workspace_bytes(batch, q_heads, kv_heads, head_dim, q_tokens, k_tokens);
+    if (need > 0 && !workspace_dev) return NGEMM_ERR_INVALID_ARG;
+    if (workspace_bytes < need) return NGEMM_ERR_BUFFER_TOO_SMALL;
+    if (need > 0 && ((uintptr_t)workspace_dev & 15u) != 0) return NGEMM_ERR_INVALID_ARG;
+    DeviceGuard g(ctx->device);
+    if (!g.ok) return NGEMM_ERR_DEVICE;
+    const PromptArgs a{q, k, v, o, q_offsets_dev, k_offsets_dev ? k_offsets_dev : q_offsets_dev, (int32_t)batch, (int32_t)q_heads, (int32_t)kv_heads,
+                       (int32_t)head_dim, (int32_t)q_tokens, (int32_t)k_tokens, causal != 0, scale};
+    const dim3 grid((unsigned)(q_tokens * q_heads)), block(64);
+    hipStream_t st = (hipStream_t)hip_stream;
+    if (type == NGEMM_F16) hipLaunchKernelGGL(attention_prompt_kernel<F16>, grid, block, 0, st, a);
+    else hipLaunchKernelGGL(attention_prompt_kernel<BF16>, grid, block, 0, st, a);
+    return launched();
+}
+
+}  // extern "C"

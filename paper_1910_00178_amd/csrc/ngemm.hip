@@ -2,6 +2,7 @@
 // selection and launches.  Every step of the path runs in the kernels of
 // ngemm_kernels.h; there is no CPU fallback.
 #include "ngemm.h"
+#include "ngemm_host.h"
 #include "ngemm_kernels.h"
 #include "ngemm_mid.h"
 
@@ -24,23 +25,6 @@ constexpr int64_t kStaticMaxM = 65536;
 constexpr size_t kStaticScratchBytes = (size_t)kStaticMaxM * 4;
 static __device__ __align__(256) unsigned char scratch[kStaticScratchBytes];
 
-struct ngemm_ctx {
-    uint32_t magic;
-    int device;
-    int num_cus;
-    int num_xcd;             // XCDs (L2 domains) of the device; workgroup ids go round them in turn
-    int force_kernel;
-    int max_workgroups;      // 0 = one per compute unit
-    void *static_scratch;    // device address of this device's copy of `scratch`
-    // kernels found fastest by ngemm_tune_u8s8s32, by shape; consulted before the shape heuristic
-    struct Tuned {
-        int64_t M, N, K;
-        int kernel;          // the fastest of NGEMM_KERNEL_*
-        bool wavek;          // what only the automatic choice launches (gemm_wavek_kernel, gemm_mid_kernel) was faster still
-    };
-    std::vector<Tuned> tuned;
-};
-
 struct ngemm_packed_b {
     uint32_t magic;
     int device;
@@ -53,7 +37,6 @@ struct ngemm_packed_b {
 
 namespace {
 
-constexpr uint32_t kCtxMagic = 0x4e47454du;   // "NGEM"
 constexpr uint32_t kPackMagic = 0x4e47504bu;  // "NGPK"
 constexpr int64_t kMaxDim = 0x7fffffff - 4096;
 constexpr int kSkinnyMaxM = 32;
@@ -77,25 +60,6 @@ inline bool wavek_offsets_fit(int64_t lda_bytes, int64_t kbytes, int64_t Kp, int
     return lda_bytes < most / 64 && 64 * lda_bytes + kbytes < most && Kp < most / 128 && ldb < most / 128 && 128 * ldb + kbytes < most;
 }
 
-struct DeviceGuard {
-    int prev = -1;
-    bool ok = false;
-    explicit DeviceGuard(int dev)
-    {
-        if (hipGetDevice(&prev) != hipSuccess) return;
-        ok = (prev == dev) || (hipSetDevice(dev) == hipSuccess);
-        if (prev == dev) prev = -1;
-        // the launches below are checked with hipGetLastError(): drop an error that other code on
-        // this thread left behind, so that it is not reported as one of ours
-        (void)hipGetLastError();
-    }
-    ~DeviceGuard()
-    {
-        if (prev >= 0) (void)hipSetDevice(prev);
-    }
-};
-
-bool ctx_ok(const ngemm_ctx *c) { return c && c->magic == kCtxMagic; }
 bool pack_ok(const ngemm_packed_b *b) { return b && b->magic == kPackMagic; }
 
 template <int BM, int BN, int WGM, int WGN, int BK>
