@@ -1,7 +1,8 @@
 // Host side of the key-value cache and the attention calls of include/ngemm.h: argument validation and launches.
 #include "ngemm.h"
 #include "ngemm_host.h"
-#include "attention.h"
+#include "attention_decode.h"
+#include "attention_prompt.h"
 
 #include <cmath>
 #include <new>
@@ -80,7 +81,62 @@ ngemm_status move_rows(bool write, ngemm_ctx *ctx, const ngemm_kv_cache *cache, 
     return launched();
 }
 
+// ---- prompts ----
+
+// f(PromptCfg<...>{}) for the smallest DP that holds head_dim.
+template <class F>
+void with_prompt_form(int64_t head_dim, F &&f)
+{
+    if (head_dim <= 64) f(PromptCfg<64, 4, 64, 2>{});
+    else if (head_dim <= 96) f(PromptCfg<96, 4, 64, 2>{});
+    else if (head_dim <= 128) f(PromptCfg<128, 4, 64, 2>{});
+    else if (head_dim <= 192) f(PromptCfg<192, 4, 64, 1>{});
+    else f(PromptCfg<256, 4, 32, 1>{});
+}
+
+template <class E, class C, bool VEC>
+hipError_t allow_prompt_lds()
+{
+    return hipFuncSetAttribute((const void *)attention_prompt_kernel<E, C, VEC>, hipFuncAttributeMaxDynamicSharedMemorySize, C::kLds);
+}
+
+template <class C>
+bool allow_prompt_form()
+{
+    return allow_prompt_lds<F16, C, true>() == hipSuccess && allow_prompt_lds<F16, C, false>() == hipSuccess &&
+           allow_prompt_lds<BF16, C, true>() == hipSuccess && allow_prompt_lds<BF16, C, false>() == hipSuccess;
+}
+
+// 16-byte pieces: bases and strides of 16-byte multiples, and a tile's offsets within 31 bits.
+bool rows_in_pieces(const Rows &r)
+{
+    return ((uintptr_t)r.data & 15u) == 0 && r.token_stride % 8 == 0 && r.head_stride % 8 == 0 && r.token_stride < (1 << 23);
+}
+
+template <class E, class C>
+void launch_prompt_form(PromptArgs a, bool vec, hipStream_t st)
+{
+    a.slots = (int32_t)((int64_t)a.q_tokens * (a.q_heads / a.kv_heads) / C::BM) + a.batch;
+    const dim3 grid((unsigned)(a.slots * a.kv_heads)), block(C::NW * 64);
+    if (vec) hipLaunchKernelGGL((attention_prompt_kernel<E, C, true>), grid, block, C::kLds, st, a);
+    else hipLaunchKernelGGL((attention_prompt_kernel<E, C, false>), grid, block, C::kLds, st, a);
+}
+
+template <class E>
+void launch_prompt(const PromptArgs &a, bool vec, hipStream_t st)
+{
+    with_prompt_form(a.head_dim, [&](auto form) { launch_prompt_form<E, decltype(form)>(a, vec, st); });
+}
+
 }  // namespace
+
+bool ngemm::attention_setup()
+{
+    bool ok = true;
+    for (int64_t d : {64, 96, 128, 192, 256})
+        with_prompt_form(d, [&](auto form) { ok = ok && allow_prompt_form<decltype(form)>(); });
+    return ok;
+}
 
 extern "C" {
 
@@ -193,7 +249,7 @@ ngemm_status ngemm_attention_prompt(ngemm_ctx *ctx, ngemm_type type, int64_t bat
     if (!ctx_ok(ctx)) return NGEMM_ERR_INVALID_ARG;
     if ((type != NGEMM_F16 && type != NGEMM_BF16) || !std::isfinite(scale)) return NGEMM_ERR_INVALID_ARG;
     if (batch < 0 || batch > kMaxCount || q_heads < 1 || q_heads > 65536 || kv_heads < 1 || q_heads % kv_heads || !head_dim_ok(head_dim) || q_tokens < 0 ||
-        k_tokens < 0 || q_tokens > kMaxCount || k_tokens > kMaxCount || q_tokens * q_heads > kMaxCount)
+        k_tokens < 0 || q_tokens > kMaxCount || k_tokens > kMaxCount || (q_tokens + 128 * batch) * q_heads > kMaxCount)
         return NGEMM_ERR_BAD_SHAPE;
     if (q_tokens == 0) return NGEMM_OK;
     if (batch == 0 || (!k_offsets_dev && k_tokens != q_tokens)) return NGEMM_ERR_BAD_SHAPE;
@@ -210,12 +266,14 @@ ngemm_status ngemm_attention_prompt(ngemm_ctx *ctx, ngemm_type type, int64_t bat
     if (need > 0 && ((uintptr_t)workspace_dev & 15u) != 0) return NGEMM_ERR_INVALID_ARG;
     DeviceGuard g(ctx->device);
     if (!g.ok) return NGEMM_ERR_DEVICE;
+    // the kernel's scale is not negative (the sign goes to Q), and not 0 (hidden scores are minus infinity)
+    const float scale2 = std::fmax(std::fabs(scale) * 1.44269504f, 1.17549435e-38f);
     const PromptArgs a{q, k, v, o, q_offsets_dev, k_offsets_dev ? k_offsets_dev : q_offsets_dev, (int32_t)batch, (int32_t)q_heads, (int32_t)kv_heads,
-                       (int32_t)head_dim, (int32_t)q_tokens, (int32_t)k_tokens, causal != 0, scale};
-    const dim3 grid((unsigned)(q_tokens * q_heads)), block(64);
+                       (int32_t)head_dim, (int32_t)q_tokens, (int32_t)k_tokens, causal != 0, scale2, std::signbit(scale) ? 0x80008000u : 0u, 0};
+    const bool vec = rows_in_pieces(q) && rows_in_pieces(k) && rows_in_pieces(v) && rows_in_pieces(o);
     hipStream_t st = (hipStream_t)hip_stream;
-    if (type == NGEMM_F16) hipLaunchKernelGGL(attention_prompt_kernel<F16>, grid, block, 0, st, a);
-    else hipLaunchKernelGGL(attention_prompt_kernel<BF16>, grid, block, 0, st, a);
+    if (type == NGEMM_F16) launch_prompt<F16>(a, vec, st);
+    else launch_prompt<BF16>(a, vec, st);
     return launched();
 }
 

@@ -1,0 +1,323 @@
+// Attention over packed rows, whole prompts and prompts behind a context.
+#pragma once
+#include "kv_cache.h"
+
+namespace ngemm {
+
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef _Float16 h8 __attribute__((ext_vector_type(8)));
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+typedef short s4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) void *lds_ptr;
+typedef __attribute__((address_space(3))) s4 *lds_s4;
+
+__device__ __forceinline__ f16v mfma32(F16, u4 a, u4 b, f16v c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f16v mfma32(BF16, u4 a, u4 b, f16v c)
+{
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
+}
+
+// Two floats rounded to nearest even, packed.
+template <class E>
+__device__ __forceinline__ uint32_t pack2(float lo, float hi)
+{
+    typedef typename E::T T2 __attribute__((ext_vector_type(2)));
+    typedef float V2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((V2){lo, hi}, T2));
+}
+
+// What lane l and lane l ^ 32 hold, both in both lanes.
+__device__ __forceinline__ float max_of_halves(float x)
+{
+    const u2 s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1]));
+}
+__device__ __forceinline__ float sum_of_halves(float x)
+{
+    const u2 s = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(s[0]) + __uint_as_float(s[1]);
+}
+
+struct PromptArgs {
+    Rows q, k, v, o;
+    const int32_t *q_offsets, *k_offsets;
+    int32_t batch, q_heads, kv_heads, head_dim, q_tokens, k_tokens, causal;
+    float scale;             // of the scores, times log2 e; not negative (Q's sign is turned instead)
+    uint32_t q_xor;
+    int32_t slots;           // tiles of query rows that the grid has room for
+};
+
+// DP: head_dim rounded up; NW wavefronts of 32 rows; BN keys per tile.
+template <int DP_, int NW_, int BN_, int PER_CU_>
+struct PromptCfg {
+    static constexpr int DP = DP_, NW = NW_, BN = BN_, PER_CU = PER_CU_;
+    static constexpr int BM = 32 * NW, CH = DP / 8;              // CH: 16-byte chunks of a row
+    static constexpr int kTile = BN * DP * 2, kStage = 2 * kTile, kLds = 2 * kStage;
+    static constexpr int LOADS = kTile / 1024 / NW;              // 1 KiB copies of K (and of V) per wavefront
+    static_assert(kTile % (1024 * NW) == 0, "whole copies");
+    // Where chunk c of key j lies: so that 16 consecutive keys' equal chunks of K, and the 64 bytes of four consecutive keys of V,
+    // fall on different banks (64 banks of 4 bytes).
+    static __device__ __forceinline__ int k_swizzle(int j)
+    {
+        return CH % 16 == 0 ? j & 15 : CH % 8 == 0 ? (j >> 1) & 7 : (j >> 2) & 3;
+    }
+    static __device__ __forceinline__ int v_swizzle(int j)
+    {
+        return CH % 16 == 0 ? (j & 3) << 2 : CH % 8 == 0 ? (j & 2) << 1 : 0;
+    }
+};
+
+// Each half of a dword without its sign, as two 16-bit numbers: at least `least` where it is an infinity or a NaN.
+__device__ __forceinline__ uint32_t max_u16(uint32_t a, uint32_t b)
+{
+    typedef uint16_t V2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(V2, a), __builtin_bit_cast(V2, b)));
+}
+template <class E> constexpr uint32_t kInfinity = 0x7f80;
+template <> constexpr uint32_t kInfinity<F16> = 0x7c00;
+
+// Copies memory -> LDS, 16 bytes a lane; what lies past the buffer's end becomes 0.  (No templates: the host pass, which cannot know the
+// copies' width, drops a template's instance with such a call in it.)
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *from, int bytes)
+{
+    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(from), (short)0, bytes, 0x00020000);
+}
+__device__ __forceinline__ void copy_to_lds(__amdgpu_buffer_rsrc_t from, uint8_t *to, uint32_t offset)
+{
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_ptr)to, 16, offset, 0, 0, 0);
+}
+
+// Rows of a workgroup: the queries of a sequence times the q_heads / kv_heads heads that share a K/V head, heads fastest.  S^T = K Q^T
+// and O^T = V^T P^T on 32 x 32 x 16 matrix instructions: a lane holds scores of one row (lane % 32), so the softmax needs one exchange of
+// lane halves per tile, and P^T's operand is what the lane holds, rounded, with the keys in the order in which the transposing LDS
+// reads deliver V.
+template <class E, class C, bool VEC>
+__global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_prompt_kernel(const PromptArgs a)
+{
+    extern __shared__ __align__(1024) uint8_t lds[];
+    constexpr int DP = C::DP, NW = C::NW, BN = C::BN, BM = C::BM, CH = C::CH;
+    typedef typename E::T T;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int half = lane >> 5, col = lane & 31;
+    const int head = blockIdx.x % a.kv_heads, slot = a.slots - 1 - blockIdx.x / a.kv_heads;
+    const int group = a.q_heads / a.kv_heads, D = a.head_dim;
+
+    // Sequence b has the slots floor(rows before it / BM) + b .. : as many as its rows need or one more.
+    int lo = 0, hi = a.batch;
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) / 2;
+        if (a.q_offsets[mid] * group / BM + mid <= slot) lo = mid; else hi = mid;
+    }
+    const int b = lo;
+    const int q_first = min(max(a.q_offsets[b], 0), a.q_tokens), queries = min(max(a.q_offsets[b + 1], q_first), a.q_tokens) - q_first;
+    const int row0 = (slot - (a.q_offsets[b] * group / BM + b)) * BM, rows = queries * group;
+    if (row0 < 0 || row0 >= rows) return;
+    const int k_first = min(max(a.k_offsets[b], 0), a.k_tokens), keys = min(max(a.k_offsets[b + 1], k_first), a.k_tokens) - k_first;
+
+    // the last key that a row sees
+    auto last_seen = [&](int row) { return a.causal ? min(row / group + keys - queries, keys - 1) : keys - 1; };
+    const int row = row0 + 32 * wave + col;
+    const bool row_there = row < rows;
+    const int query = min(row, rows - 1) / group, qhead = head * group + min(row, rows - 1) % group;
+    const int seen = last_seen(min(row, rows - 1));
+    const int wave_first = min(row0 + 32 * wave, rows - 1), wave_last = min(row0 + 32 * wave + 31, rows - 1);
+    const int seen_by_all = last_seen(wave_first), seen_by_any = last_seen(wave_last);
+    const int group_seen_by_all = last_seen(row0), group_seen_by_any = last_seen(min(row0 + BM, rows) - 1);
+    const int tiles = (group_seen_by_any + BN) / BN;             // group_seen_by_any >= -1 or no tile
+
+    const T *kbase = (const T *)a.k.data + k_first * a.k.token_stride + head * a.k.head_stride;
+    const T *vbase = (const T *)a.v.data + k_first * a.v.token_stride + head * a.v.head_stride;
+
+    // ---- copies of a tile into LDS ----
+    uint32_t kv_off[2][C::LOADS];
+    if constexpr (VEC) {
+#pragma unroll
+        for (int i = 0; i < C::LOADS; ++i) {
+            const int s = (i * NW + wave) * 64 + lane, j = s / CH, p = s % CH;
+            const int kc = p ^ C::k_swizzle(j), vc = p ^ C::v_swizzle(j);
+            kv_off[0][i] = kc * 8 < D ? (uint32_t)(j * a.k.token_stride * 2 + kc * 16) : 0x80000000u;
+            kv_off[1][i] = vc * 8 < D ? (uint32_t)(j * a.v.token_stride * 2 + vc * 16) : 0x80000000u;
+        }
+    }
+    auto load_tile = [&](int tile, int stage) {
+        const int left = min(keys - tile * BN, BN);              // rows past it, and elements past head_dim, become 0
+#pragma unroll
+        for (int which = 0; which < 2; ++which) {
+            const T *from = which ? vbase + (int64_t)tile * BN * a.v.token_stride : kbase + (int64_t)tile * BN * a.k.token_stride;
+            const int64_t stride = which ? a.v.token_stride : a.k.token_stride;
+            uint8_t *to = lds + stage * C::kStage + which * C::kTile;
+            if constexpr (VEC) {
+                const __amdgpu_buffer_rsrc_t rsrc = buffer_of(from, (int)((left - 1) * stride * 2 + D * 2));
+#pragma unroll
+                for (int i = 0; i < C::LOADS; ++i) copy_to_lds(rsrc, to + (i * NW + wave) * 1024, kv_off[which][i]);
+            } else {
+                for (int i = 0; i < C::LOADS; ++i) {
+                    const int s = (i * NW + wave) * 64 + lane, j = s / CH;
+                    const int c = (s % CH) ^ (which ? C::v_swizzle(j) : C::k_swizzle(j));
+                    T x[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = j < left && c * 8 < D ? from[j * stride + c * 8 + e] : (T)0.0f;
+                    __builtin_memcpy(to + s * 16, x, 16);
+                }
+            }
+        }
+    };
+    if (tiles > 0) load_tile(0, 0);
+
+    // ---- Q^T's operand: 8 elements of the lane's row per step ----
+    u4 q[DP / 16];
+    {
+        const T *from = (const T *)a.q.data + (q_first + query) * a.q.token_stride + qhead * a.q.head_stride;
+#pragma unroll
+        for (int s = 0; s < DP / 16; ++s) {
+            const int d = 16 * s + 8 * half;
+            const T *at = from + (d < D ? d : 0);
+            if constexpr (VEC) {
+                q[s] = *(const u4 *)at;
+            } else {
+                T x[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[e] = at[e];
+                __builtin_memcpy(&q[s], x, 16);
+            }
+            q[s] = d < D ? q[s] ^ a.q_xor : (u4)(0u);
+        }
+    }
+
+    // ---- LDS addresses of the operands, which the two stages turn by a bit ----
+    int k_at[DP / 16], v_at[DP / 32][2];
+#pragma unroll
+    for (int s = 0; s < DP / 16; ++s) k_at[s] = col * DP * 2 + ((2 * s + half) ^ C::k_swizzle(col)) * 16;
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int i = lane & 15, j = 8 * h + 4 * half + (i >> 2), c = 4 * t + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
+            v_at[t][h] = C::kTile + j * DP * 2 + (c ^ C::v_swizzle(j)) * 16 + (i & 1) * 8;
+        }
+
+    f16v o[DP / 32];
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t) o[t] = (f16v)(0.0f);
+    // m: what the weights are relative to, in units of the scores; no less than a number whose product with the scale is finite
+    float m = -3.0e38f / fmaxf(a.scale, 1.0f), l = 0.0f;
+
+    for (int tile = 0; tile < tiles; ++tile) {
+        const int stage = tile & 1;
+        __builtin_amdgcn_s_waitcnt(0);
+        __syncthreads();
+        if (tile + 1 < tiles) load_tile(tile + 1, stage ^ 1);
+        const uint8_t *at = lds + stage * C::kStage;
+        const bool masked = tile * BN + BN - 1 > group_seen_by_all;          // for some row of the workgroup
+        bool odd = false;
+        if (masked) {                            // a value that some row does not see must not reach it through 0 * infinity
+            uint32_t most = 0;
+            for (int i = 0; i < C::LOADS; ++i) {
+                const u4 x = *(const u4 *)(at + C::kTile + ((i * NW + wave) * 64 + lane) * 16) & 0x7fff7fffu;
+                most = max_u16(most, max_u16(max_u16(x[0], x[1]), max_u16(x[2], x[3])));
+            }
+            odd = __syncthreads_or((most & 0xffff) >= kInfinity<E> || (most >> 16) >= kInfinity<E>);
+        }
+        if (tile * BN > seen_by_any) continue;
+        f16v s[BN / 32];
+#pragma unroll
+        for (int t = 0; t < BN / 32; ++t) {
+            s[t] = (f16v)(0.0f);
+#pragma unroll
+            for (int u = 0; u < DP / 16; ++u)
+                s[t] = mfma32(E{}, *(const u4 *)(at + k_at[u] + t * 32 * DP * 2), q[u], s[t]);
+        }
+        if (tile * BN + BN - 1 > seen_by_all) {
+#pragma unroll
+            for (int t = 0; t < BN / 32; ++t)
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (tile * BN + 32 * t + 8 * (i / 4) + 4 * half + i % 4 > seen) s[t][i] = -__builtin_inff();
+        }
+        float most = m;
+#pragma unroll
+        for (int t = 0; t < BN / 32; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) most = fmaxf(most, s[t][i]);
+        most = max_of_halves(most);
+        if (__any(most > m)) {
+            const float fall = __builtin_amdgcn_exp2f((m - most) * a.scale);
+            l *= fall;
+#pragma unroll
+            for (int t = 0; t < DP / 32; ++t) o[t] *= fall;
+            m = most;
+        }
+        const float ms = m * a.scale;
+        u4 p[BN / 16];
+#pragma unroll
+        for (int t = 0; t < BN / 32; ++t)
+#pragma unroll
+            for (int i = 0; i < 16; i += 2) {
+                const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], a.scale, -ms));
+                const float y = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i + 1], a.scale, -ms));
+                l += x + y;
+                p[2 * t + i / 8][(i % 8) / 2] = pack2<E>(x, y);
+            }
+#pragma unroll
+        for (int u = 0; u < BN / 16; ++u)
+#pragma unroll
+            for (int t = 0; t < DP / 32; ++t) {
+                const u2 v0 = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(at + v_at[t][0] + u * 16 * DP * 2)));
+                const u2 v1 = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(at + v_at[t][1] + u * 16 * DP * 2)));
+                u4 v = {v0[0], v0[1], v1[0], v1[1]};
+                if (odd) {                       // infinities and NaN apart, below
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) {
+                        if ((v[e] & 0x7fff) >= kInfinity<E>) v[e] &= 0xffff0000u;
+                        if ((v[e] >> 16 & 0x7fff) >= kInfinity<E>) v[e] &= 0xffffu;
+                    }
+                }
+                o[t] = mfma32(E{}, v, p[u], o[t]);
+            }
+        if (odd) {
+            for (int j = 0; j < BN; ++j) {
+                if (tile * BN + j > seen) break;
+#pragma unroll
+                for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        const int d = 32 * t + 8 * (i / 4) + 4 * half + i % 4;
+                        const uint16_t x = *(const uint16_t *)(at + C::kTile + j * DP * 2 + ((d / 8) ^ C::v_swizzle(j)) * 16 + d % 8 * 2);
+                        if ((x & 0x7fff) >= kInfinity<E>) o[t][i] += E::get(__builtin_bit_cast(T, x));
+                    }
+            }
+        }
+    }
+
+    // ---- O = O^T / l: 4 consecutive elements per lane and quarter, exchanged between lane halves to 8 ----
+    l = sum_of_halves(l);
+    const float by = seen < 0 ? 0.0f : 1.0f / l;
+    T *out = (T *)a.o.data + (q_first + query) * a.o.token_stride + qhead * a.o.head_stride;
+#pragma unroll
+    for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; i += 8) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = seen < 0 ? 0.0f : o[t][i + e] * by;
+            const u2 s0 = __builtin_amdgcn_permlane32_swap(pack2<E>(x[0], x[1]), pack2<E>(x[4], x[5]), false, false);
+            const u2 s1 = __builtin_amdgcn_permlane32_swap(pack2<E>(x[2], x[3]), pack2<E>(x[6], x[7]), false, false);
+            const u4 y = {s0[0], s1[0], s0[1], s1[1]};
+            const int d = 32 * t + 2 * i + 8 * half;
+            if (row_there && d < D) {
+                if constexpr (VEC) {
+                    *(u4 *)(out + d) = y;
+                } else {
+                    T e8[8];
+                    __builtin_memcpy(e8, &y, 16);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) out[d + e] = e8[e];
+                }
+            }
+        }
+}
+
+}  // namespace ngemm

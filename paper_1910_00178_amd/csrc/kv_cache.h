@@ -76,7 +76,7 @@ struct MoveArgs {
 
 // A wavefront per token and head: amax over the row by lane exchanges, then the codes.
 template <class E>
-__global__ void __launch_bounds__(256) kv_write_kernel(const MoveArgs a)
+__global__ __launch_bounds__(256) void kv_write_kernel(const MoveArgs a)
 {
     const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) / 64;
     const int lane = threadIdx.x & 63, D = a.cache.head_dim;
@@ -115,7 +115,7 @@ __global__ void __launch_bounds__(256) kv_write_kernel(const MoveArgs a)
 }
 
 template <class E>
-__global__ void __launch_bounds__(256) kv_read_kernel(const MoveArgs a)
+__global__ __launch_bounds__(256) void kv_read_kernel(const MoveArgs a)
 {
     const int64_t item = ((int64_t)blockIdx.x * 256 + threadIdx.x) / 64;
     const int lane = threadIdx.x & 63, D = a.cache.head_dim;
