@@ -4,6 +4,7 @@
 #include "attention_decode.h"
 #include "attention_prompt.h"
 
+#include <algorithm>
 #include <cmath>
 #include <new>
 
@@ -81,6 +82,48 @@ ngemm_status move_rows(bool write, ngemm_ctx *ctx, const ngemm_kv_cache *cache, 
     return launched();
 }
 
+// ---- one token per sequence ----
+
+// How a sequence is cut: chunks of whole rounds of a workgroup's tiles, so long that the grid has some workgroups per unit, and no longer than a
+// sequence of middling length leaves balanced.
+struct DecodeCut {
+    int64_t chunk, chunks;
+};
+DecodeCut decode_cut(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t max_length)
+{
+    constexpr int64_t round = 64 * kDecodeWaves;
+    const int64_t grid = batch * kv_heads * ((q_heads / kv_heads + 15) / 16);
+    int64_t chunk = (max_length * grid / 2048 + round - 1) / round * round;
+    chunk = std::min<int64_t>(std::max<int64_t>(chunk, round), 1024);
+    return DecodeCut{chunk, std::max<int64_t>(1, (max_length + chunk - 1) / chunk)};
+}
+
+template <class E, int NJ>
+void launch_decode_form(const DecodeArgs &a, unsigned grid, size_t lds, hipStream_t st)
+{
+    hipLaunchKernelGGL((attention_decode_kernel<E, NJ>), dim3(grid), dim3(kDecodeWaves * 64), lds, st, a);
+}
+
+template <class E>
+void launch_decode(const DecodeArgs &a, hipStream_t st)
+{
+    const int group = a.q_heads / a.cache.kv_heads, D = a.cache.head_dim;
+    const unsigned grid = (unsigned)((int64_t)a.batch * a.cache.kv_heads * ((group + 15) / 16) * a.chunks);
+    const size_t lds = (size_t)kDecodeWaves * (32 + std::min(group, 16) * D) * 4;
+    if (D <= 64) launch_decode_form<E, 1>(a, grid, lds, st);
+    else if (D <= 128) launch_decode_form<E, 2>(a, grid, lds, st);
+    else if (D <= 192) launch_decode_form<E, 3>(a, grid, lds, st);
+    else launch_decode_form<E, 4>(a, grid, lds, st);
+    if (a.chunks > 1) hipLaunchKernelGGL(attention_decode_join_kernel<E>, dim3((unsigned)(a.batch * a.q_heads)), dim3(256), 0, st, a);
+}
+
+template <class E, int NJ>
+bool allow_decode_lds()
+{
+    void (*const kernel)(DecodeArgs) = attention_decode_kernel<E, NJ>;
+    return hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kDecodeWaves * (32 + 16 * 64 * NJ) * 4) == hipSuccess;
+}
+
 // ---- prompts ----
 
 // f(PromptCfg<...>{}) for the smallest DP that holds head_dim.
@@ -132,7 +175,7 @@ void launch_prompt(const PromptArgs &a, bool vec, hipStream_t st)
 
 bool ngemm::attention_setup()
 {
-    bool ok = true;
+    bool ok = allow_decode_lds<F16, 3>() && allow_decode_lds<F16, 4>() && allow_decode_lds<BF16, 3>() && allow_decode_lds<BF16, 4>();
     for (int64_t d : {64, 96, 128, 192, 256})
         with_prompt_form(d, [&](auto form) { ok = ok && allow_prompt_form<decltype(form)>(); });
     return ok;
@@ -145,8 +188,8 @@ size_t ngemm_kv_cache_bytes(int64_t num_pages, int64_t page_tokens, int64_t kv_h
     if (num_pages < 1 || num_pages > kMaxCount || page_tokens < kBlockTokens || page_tokens > (1 << 24) || page_tokens % kBlockTokens ||
         kv_heads < 1 || kv_heads > 65536 || !head_dim_ok(head_dim))
         return 0;
-    const __int128 bytes = (__int128)num_pages * kv_heads * page_tokens * (2 * head_dim + 8);
-    return bytes < ((__int128)1 << 62) ? (size_t)bytes : 0;
+    const __int128 blocks = (__int128)num_pages * kv_heads * (page_tokens / kBlockTokens);       // numbered in 31 bits
+    return blocks <= kMaxCount ? (size_t)(blocks * (32 * head_dim + 8 * kBlockTokens)) : 0;
 }
 
 ngemm_status ngemm_kv_cache_create(ngemm_ctx *ctx, int64_t num_pages, int64_t page_tokens, int64_t kv_heads, int64_t head_dim,
@@ -196,8 +239,11 @@ ngemm_status ngemm_kv_read(ngemm_ctx *ctx, const ngemm_kv_cache *cache, ngemm_ty
 
 size_t ngemm_attention_decode_workspace_bytes(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t max_length)
 {
-    (void)batch; (void)q_heads; (void)kv_heads; (void)head_dim; (void)max_length;
-    return 0;
+    if (batch < 1 || q_heads < 1 || kv_heads < 1 || q_heads % kv_heads || !head_dim_ok(head_dim) || max_length < 0 || max_length > kMaxCount ||
+        batch > kMaxCount || q_heads > 65536 || batch * q_heads > kMaxCount)
+        return 0;
+    const DecodeCut cut = decode_cut(batch, q_heads, kv_heads, max_length);
+    return cut.chunks > 1 ? (size_t)(batch * q_heads * cut.chunks * (head_dim + 2) * 4) : 0;
 }
 
 ngemm_status ngemm_attention_decode(ngemm_ctx *ctx, const ngemm_kv_cache *cache, ngemm_type type, int64_t batch, int64_t q_heads,
@@ -223,11 +269,13 @@ ngemm_status ngemm_attention_decode(ngemm_ctx *ctx, const ngemm_kv_cache *cache,
     if (need > 0 && ((uintptr_t)workspace_dev & 15u) != 0) return NGEMM_ERR_INVALID_ARG;
     DeviceGuard g(ctx->device);
     if (!g.ok) return NGEMM_ERR_DEVICE;
-    const DecodeArgs a{view_of(cache, pages_dev, pages_stride), q, o, lengths_dev, (int32_t)batch, (int32_t)q_heads, (int32_t)max_length, scale};
-    const dim3 grid((unsigned)(batch * q_heads)), block(64);
+    const DecodeCut cut = decode_cut(batch, q_heads, cache->kv_heads, max_length);
+    if (batch * q_heads * cut.chunks > kMaxCount) return NGEMM_ERR_BAD_SHAPE;
+    const DecodeArgs a{view_of(cache, pages_dev, pages_stride), q, o, lengths_dev, (int32_t)batch, (int32_t)q_heads, (int32_t)max_length,
+                       (int32_t)cut.chunk, (int32_t)cut.chunks, scale * 1.44269504f, (float *)workspace_dev};
     hipStream_t st = (hipStream_t)hip_stream;
-    if (type == NGEMM_F16) hipLaunchKernelGGL(attention_decode_kernel<F16>, grid, block, 0, st, a);
-    else hipLaunchKernelGGL(attention_decode_kernel<BF16>, grid, block, 0, st, a);
+    if (type == NGEMM_F16) launch_decode<F16>(a, st);
+    else launch_decode<BF16>(a, st);
     return launched();
 }
 

@@ -1,6 +1,6 @@
 // Attention of one token per sequence over the 8-bit cache.
 #pragma once
-#include "kv_cache.h"
+#include "attention_common.h"
 
 namespace ngemm {
 
@@ -9,60 +9,277 @@ struct DecodeArgs {
     Rows q, o;
     const int32_t *lengths;
     int32_t batch, q_heads, max_length;
-    float scale;
+    int32_t chunk, chunks;   // tokens of a workgroup, workgroups along a sequence
+    float scale;             // of the scores, times log2 e
+    float *part;             // chunks > 1: [batch][q_heads][chunks][head_dim] sums, then [batch][q_heads][chunks][2] maxima and weights
 };
 
-// A wavefront per sequence and query head, 64 tokens at a time: lanes are tokens in the first product, elements of V in the second.
-template <class E>
-__global__ __launch_bounds__(64) void attention_decode_kernel(const DecodeArgs a)
+constexpr int kDecodeWaves = 4;
+
+// 16 codes as 16-bit floats, in order.  A code with its sign bit turned, as the low byte under 0x64, is the float 1024 + 128 + code.
+__device__ __forceinline__ void codes_to_f16(u4 x, u4 (&out)[2])
 {
-    __shared__ float q[256], p[64];
-    const int b = blockIdx.x / a.q_heads, h = blockIdx.x % a.q_heads, lane = threadIdx.x, D = a.cache.head_dim;
-    const int g = h / (a.q_heads / a.cache.kv_heads);
-    const typename E::T *qrow = (const typename E::T *)a.q.data + b * a.q.token_stride + h * a.q.head_stride;
-    for (int d = lane; d < D; d += 64) q[d] = E::get(qrow[d]) * a.scale;
-    __syncthreads();
-    const int length = min(a.lengths[b], a.max_length);
-    float m = -__builtin_inff(), l = 0.0f, o[4] = {};
-    for (int t0 = 0; t0 < length; t0 += 64) {
-        const int t = t0 + lane;
-        const uint8_t *block = t < length ? cache_block(a.cache, b, g, t / 16) : nullptr;
-        float s = -__builtin_inff(), vs = 0.0f;
-        if (block) {
-            const int8_t *k = (const int8_t *)block + (t & 15) * D;
-            float dot = 0.0f;
-            for (int d = 0; d < D; ++d) dot += q[d] * k[d];
-            const float *scales = (const float *)(block + 32 * D);
-            s = dot * scales[t & 15];
-            vs = scales[16 + (t & 15)];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t y = x[e] ^ 0x80808080u;
+        const h2 base = {(_Float16)-1152.0f, (_Float16)-1152.0f};
+        const h2 lo = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, y, 0x04010400u)) + base;
+        const h2 hi = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, y, 0x04030402u)) + base;
+        out[e / 2][2 * (e % 2)] = __builtin_bit_cast(uint32_t, lo);
+        out[e / 2][2 * (e % 2) + 1] = __builtin_bit_cast(uint32_t, hi);
+    }
+}
+
+// Lane 16 r + K's value in all lanes 16 r .. 16 r + 15.
+template <int K>
+__device__ __forceinline__ float of_row(float x)
+{
+    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x150 + K, 0xf, 0xf, true));
+}
+
+// Over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
+__device__ __forceinline__ float max_of_rows(float x)
+{
+    const u2 s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return max_of_halves(fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1])));
+}
+__device__ __forceinline__ float sum_of_rows(float x)
+{
+    const u2 s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return sum_of_halves(__uint_as_float(s[0]) + __uint_as_float(s[1]));
+}
+
+// f(IntC<0>) .. f(IntC<N - 1>)
+template <int I> struct DecodeIndex { static constexpr int value = I; };
+template <int N, int I = 0, class F>
+__device__ __forceinline__ void unrolled(F &&f)
+{
+    if constexpr (I < N) {
+        f(DecodeIndex<I>{});
+        unrolled<N, I + 1>(f);
+    }
+}
+
+// A wavefront takes tiles of 64 tokens = 4 blocks: S^T = K Q^T and O^T = V^T P^T on 16 x 16 x 32 matrix instructions, up to 16 heads that share
+// a K/V head.  Row r of the first product's tile t is token 4 t + r % 4 of block r / 4, so that lane 16 g + h holds head h's scores of
+// block g's tokens, which is what the second product wants of it: the 16 tokens of a row of V in a block are the lane's 16-byte load.
+// NJ: head_dim / 64, rounded up.
+template <class E, int NJ>
+__global__ __launch_bounds__(kDecodeWaves * 64, NJ == 1 ? 4 : NJ == 2 ? 3 : NJ == 3 ? 2 : 1) void attention_decode_kernel(const DecodeArgs a)
+{
+    extern __shared__ __align__(16) float shared[];
+    constexpr int NW = kDecodeWaves;
+    typedef typename E::T T;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int h = lane & 15, g = lane >> 4;
+    const int kv_heads = a.cache.kv_heads, D = a.cache.head_dim, group = a.q_heads / kv_heads, head_tiles = (group + 15) / 16;
+    int id = blockIdx.x;
+    const int head_tile = id % head_tiles;
+    id /= head_tiles;
+    const int head = id % kv_heads;
+    id /= kv_heads;
+    const int b = id % a.batch, chunk = id / a.batch;
+    const int heads = min(16, group - 16 * head_tile), q_head0 = head * group + 16 * head_tile;
+
+    const int first = chunk * a.chunk;
+    const int end = min(min(a.lengths[b], a.max_length), first + a.chunk);
+    if (first >= end && chunk > 0) return;               // (an empty sequence's first workgroup writes its zeros)
+
+    // the wavefront's blocks, 16 tiles ahead: lane l looks up block l % 4 of its tile l / 4
+    const int blocks_per_page = a.cache.page_blocks, block_bytes = a.cache.block_bytes();
+    auto look_up = [&](int tile) {
+        const int index = (first + 64 * (tile + NW * (lane >> 2))) / 16 + (lane & 3);
+        const int page = index / blocks_per_page;
+        int where = -1;
+        if (16 * index < end && page < a.cache.pages_stride) {
+            const int id = a.cache.pages[b * a.cache.pages_stride + page];
+            if (id >= 0 && id < a.cache.num_pages) where = (id * kv_heads + head) * blocks_per_page + (index - page * blocks_per_page);
         }
-        float most = s;
-        for (int x = 32; x; x /= 2) most = fmaxf(most, __shfl_xor(most, x));
-        const float now = fmaxf(m, most), ref = now == -__builtin_inff() ? 0.0f : now;
-        const float w = block ? expf(s - ref) : 0.0f, fall = expf(m - ref);
-        float sum = w;
-        for (int x = 32; x; x /= 2) sum += __shfl_xor(sum, x);
-        l = l * fall + sum;
-        m = now;
-        __syncthreads();
-        p[lane] = block ? w * vs : 0.0f;
-        __syncthreads();
-        for (int n = 0; n < 4; ++n) o[n] *= fall;
-        for (int u = 0; u < 64 && t0 + u < length; u += 16) {
-            const int8_t *v = (const int8_t *)cache_block(a.cache, b, g, (t0 + u) / 16);
-            if (!v) continue;
-            for (int n = 0; n < 4; ++n) {
-                const int d = lane + 64 * n;
-                if (d < D)
-                    for (int j = 0; j < 16; ++j) o[n] += p[u + j] * v[16 * D + 16 * d + j];
+        return where;
+    };
+
+    // Q as f16, relative to a power of two for a bf16 row: its 8 bits are exact there
+    u4 q[2 * NJ];
+    float scale = a.scale;
+    {
+        const int qh = q_head0 + min(h, heads - 1);
+        const T *row = (const T *)a.q.data + b * a.q.token_stride + qh * a.q.head_stride;
+        float x[2 * NJ][8], most = 0.0f;
+#pragma unroll
+        for (int s = 0; s < 2 * NJ; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int d = 64 * (s / 2) + 16 * g + 8 * (s % 2) + e;
+                x[s][e] = d < D && h < heads ? E::get(row[d < D ? d : 0]) : 0.0f;
+                most = fmaxf(most, fabsf(x[s][e]));
+            }
+        int turn = 0;
+        if constexpr (sizeof(T) == 2 && !__is_same(T, _Float16)) {
+            most = max_of_rows(most);
+            if (most > 0.0f && most < __builtin_inff()) turn = 15 - __builtin_amdgcn_frexp_expf(most);
+            scale = __builtin_amdgcn_ldexpf(scale, -turn);
+        }
+#pragma unroll
+        for (int s = 0; s < 2 * NJ; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; e += 2)
+                q[s][e / 2] = pack2<F16>(__builtin_amdgcn_ldexpf(x[s][e], turn), __builtin_amdgcn_ldexpf(x[s][e + 1], turn));
+    }
+
+    f4 o[4 * NJ];
+#pragma unroll
+    for (int t = 0; t < 4 * NJ; ++t) o[t] = (f4)(0.0f);
+    float m = -3.0e38f, l = 0.0f;                        // the row's reference and this lane's part of the sum of its weights
+    float unit = 0x1p-120f, per_unit = 0x1p120f;         // V's scales enter relative to a power of two, 2^6 at most
+
+    const int tiles = end > first ? (end - first + 63) / 64 : 0;
+    int places = tiles > wave ? look_up(wave) : -1;
+    for (int tile = wave, n = 0; tile < tiles; tile += NW, ++n) {
+        if (n == 16) {
+            places = look_up(tile);
+            n = 0;
+        }
+        // ---- loads ----
+        const int k_place = __shfl(places, 4 * n + (h >> 2)), v_place = __shfl(places, 4 * n + g);
+        const uint8_t *kb = a.cache.data + (int64_t)max(k_place, 0) * block_bytes + (h & 3) * D;
+        const uint8_t *vb = a.cache.data + (int64_t)max(v_place, 0) * block_bytes;
+        u4 k[4][NJ], v[4 * NJ];
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) k[t][j] = *(const u4 *)(kb + 4 * t * D + min(64 * j + 16 * g, D - 16));
+        float ks = *(const float *)(vb + 32 * D + 4 * h), vs = *(const float *)(vb + 32 * D + 64 + 4 * h);
+#pragma unroll
+        for (int t = 0; t < 4 * NJ; ++t)
+            if (16 * t < D) v[t] = *(const u4 *)(vb + 16 * D + (16 * t + h) * 16);
+
+        // ---- scores ----
+        const int there = v_place < 0 ? 0 : end - (first + 64 * tile + 16 * g);     // tokens of block g that count
+        if (h >= there) ks = vs = 0.0f;
+        f4 s[4];
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+            s[t] = (f4)(0.0f);
+#pragma unroll
+            for (int j = 0; j < NJ; ++j) {
+                u4 x[2];
+                codes_to_f16(k[t][j], x);
+                s[t] = mfma16(x[0], q[2 * j], s[t]);
+                s[t] = mfma16(x[1], q[2 * j + 1], s[t]);
             }
         }
+        unrolled<16>([&](auto i) {
+            constexpr int I = decltype(i)::value;
+            s[I / 4][I % 4] = s[I / 4][I % 4] * of_row<I>(ks) * scale;
+        });
+        if (!__all(there >= 16)) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                if (i >= there) s[i / 4][i % 4] = -__builtin_inff();
+        }
+        float most = fmaxf(fmaxf(s[0][0], s[0][1]), s[0][2]);
+#pragma unroll
+        for (int i = 3; i < 16; ++i) most = fmaxf(most, s[i / 4][i % 4]);
+        if (__any(most > m + 8.0f)) {                    // weights up to 2^8 fit
+            most = fmaxf(max_of_rows(most), m);
+            const float fall = __builtin_amdgcn_exp2f(m - most);
+            l *= fall;
+#pragma unroll
+            for (int t = 0; t < 4 * NJ; ++t) o[t] *= fall;
+            m = most;
+        }
+        if (__any(vs > 64.0f * unit)) {
+            float top = vs;
+            for (int x = 32; x; x /= 2) top = fmaxf(top, __shfl_xor(top, x));
+            const int e = __builtin_amdgcn_frexp_expf(top);
+            const float now = __builtin_amdgcn_ldexpf(1.0f, e), fall = unit * __builtin_amdgcn_ldexpf(1.0f, -e);
+#pragma unroll
+            for (int t = 0; t < 4 * NJ; ++t) o[t] *= fall;
+            unit = now;
+            per_unit = __builtin_amdgcn_ldexpf(1.0f, -e);
+        }
+        vs *= per_unit;
+        u4 p[2];
+        unrolled<8>([&](auto i) {
+            constexpr int I = 2 * decltype(i)::value;
+            const float x = __builtin_amdgcn_exp2f(s[I / 4][I % 4] - m), y = __builtin_amdgcn_exp2f(s[I / 4][I % 4 + 1] - m);
+            l += x + y;
+            p[I / 8][I % 8 / 2] = pack2<F16>(x * of_row<I>(vs), y * of_row<I + 1>(vs));
+        });
+        // ---- values ----
+#pragma unroll
+        for (int t = 0; t < 4 * NJ; ++t)
+            if (16 * t < D) {
+                u4 x[2];
+                codes_to_f16(v[t], x);
+                o[t] = mfma16(x[0], p[0], o[t]);
+                o[t] = mfma16(x[1], p[1], o[t]);
+            }
     }
-    typename E::T *out = (typename E::T *)a.o.data + b * a.o.token_stride + h * a.o.head_stride;
-    for (int n = 0; n < 4; ++n) {
-        const int d = lane + 64 * n;
-        if (d < D) out[d] = E::put(length > 0 && l != 0.0f ? o[n] / l : 0.0f);
+
+    // ---- the wavefronts' parts, joined in their order ----
+    float *ms = shared, *ls = shared + 16 * NW, *os = shared + 32 * NW;      // [wave][16], [wave][16], [wave][heads][D]
+    l = sum_of_rows(l);
+    if (g == 0) ms[16 * wave + h] = m;
+    __syncthreads();
+    float top = m;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) top = fmaxf(top, ms[16 * w + h]);
+    const float fall = __builtin_amdgcn_exp2f(m - top);
+    if (g == 0) ls[16 * wave + h] = l * fall;
+    if (h < heads) {
+        float *mine = os + (wave * heads + h) * D;
+#pragma unroll
+        for (int t = 0; t < 4 * NJ; ++t)
+            if (16 * t < D) *(f4 *)(mine + 16 * t + 4 * g) = o[t] * (fall * unit);
     }
+    __syncthreads();
+    for (int i = threadIdx.x; i < heads * D; i += NW * 64) {
+        const int hh = i / D, d = i - hh * D;
+        float sum = 0.0f, weight = 0.0f, ref = -3.0e38f;
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            sum += os[w * heads * D + i];
+            weight += ls[16 * w + hh];
+            ref = fmaxf(ref, ms[16 * w + hh]);
+        }
+        const int qh = q_head0 + hh;
+        if (a.chunks > 1) {
+            const int64_t at = ((int64_t)b * a.q_heads + qh) * a.chunks + chunk;
+            a.part[at * D + d] = sum;
+            if (d == 0) {
+                float *stats = a.part + (int64_t)a.batch * a.q_heads * a.chunks * D + 2 * at;
+                stats[0] = ref;
+                stats[1] = weight;
+            }
+        } else {
+            ((T *)a.o.data)[b * a.o.token_stride + qh * a.o.head_stride + d] = E::put(weight == 0.0f ? 0.0f : sum / weight);
+        }
+    }
+}
+
+// The chunks of a sequence and query head, joined in their order.  A workgroup per sequence and head.
+template <class E>
+__global__ __launch_bounds__(256) void attention_decode_join_kernel(const DecodeArgs a)
+{
+    __shared__ float sums[256 * 4];
+    typedef typename E::T T;
+    const int D = a.cache.head_dim, b = blockIdx.x / a.q_heads, qh = blockIdx.x % a.q_heads;
+    const int length = min(a.lengths[b], a.max_length), chunks = length > 0 ? (length + a.chunk - 1) / a.chunk : 1;
+    const int64_t at = (int64_t)blockIdx.x * a.chunks;
+    const float *part = a.part + at * D, *stats = a.part + (int64_t)a.batch * a.q_heads * a.chunks * D + 2 * at;
+    float top = -3.0e38f;
+    for (int c = 0; c < chunks; ++c) top = fmaxf(top, stats[2 * c]);
+    const int d = threadIdx.x;
+    if (d >= D) return;
+    float sum = 0.0f, weight = 0.0f;
+    for (int c = 0; c < chunks; ++c) {
+        const float fall = __builtin_amdgcn_exp2f(stats[2 * c] - top);
+        sum += part[c * D + d] * fall;
+        weight += stats[2 * c + 1] * fall;
+    }
+    (void)sums;
+    ((T *)a.o.data)[b * a.o.token_stride + qh * a.o.head_stride + d] = E::put(weight == 0.0f ? 0.0f : sum / weight);
 }
 
 }  // namespace ngemm
