@@ -52,6 +52,23 @@ CacheView view_of(const ngemm_kv_cache *c, const int32_t *pages, int64_t pages_s
 
 ngemm_status launched() { return hipGetLastError() == hipSuccess ? NGEMM_OK : NGEMM_ERR_DEVICE; }
 
+// Whether 16-byte pieces of rows lie at 16-byte multiples.
+bool in_pieces(const Rows &r, int type)
+{
+    const int64_t pieces = 16 / elem_bytes(type);
+    return ((uintptr_t)r.data & 15u) == 0 && r.token_stride % pieces == 0 && r.head_stride % pieces == 0;
+}
+
+template <class E>
+void launch_move(bool write, bool vec, unsigned groups, hipStream_t st, const MoveArgs &a)
+{
+    const dim3 grid(groups), block(256);
+    if (write && vec) hipLaunchKernelGGL((kv_write_kernel<E, true>), grid, block, 0, st, a);
+    else if (write) hipLaunchKernelGGL((kv_write_kernel<E, false>), grid, block, 0, st, a);
+    else if (vec) hipLaunchKernelGGL((kv_read_kernel<E, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((kv_read_kernel<E, false>), grid, block, 0, st, a);
+}
+
 ngemm_status move_rows(bool write, ngemm_ctx *ctx, const ngemm_kv_cache *cache, int type, int64_t batch, int64_t tokens, Rows k, Rows v,
                        const int32_t *offsets, const int32_t *starts, const int32_t *pages, int64_t pages_stride, void *stream)
 {
@@ -63,22 +80,16 @@ ngemm_status move_rows(bool write, ngemm_ctx *ctx, const ngemm_kv_cache *cache, 
     if (!offsets || !pages) return NGEMM_ERR_INVALID_ARG;
     for (const Rows &r : {k, v})
         if (const ngemm_status s = check_rows(r, type, tokens, cache->kv_heads, cache->head_dim, !write); s != NGEMM_OK) return s;
-    const int64_t groups = (tokens * cache->kv_heads + 3) / 4;
-    if (groups > kMaxCount) return NGEMM_ERR_BAD_SHAPE;
+    const int64_t groups = move_slots(tokens, batch) * cache->kv_heads;
+    if (groups > kMaxCount || move_slots(tokens, batch) * 16 > kMaxCount) return NGEMM_ERR_BAD_SHAPE;
     DeviceGuard g(ctx->device);
     if (!g.ok) return NGEMM_ERR_DEVICE;
     const MoveArgs a{view_of(cache, pages, pages_stride), k, v, offsets, starts, (int32_t)batch, (int32_t)tokens};
-    const dim3 grid((unsigned)groups), block(256);
+    const bool vec = in_pieces(k, type) && in_pieces(v, type);
     hipStream_t st = (hipStream_t)stream;
-    if (write) {
-        if (type == NGEMM_F32) hipLaunchKernelGGL(kv_write_kernel<F32>, grid, block, 0, st, a);
-        else if (type == NGEMM_F16) hipLaunchKernelGGL(kv_write_kernel<F16>, grid, block, 0, st, a);
-        else hipLaunchKernelGGL(kv_write_kernel<BF16>, grid, block, 0, st, a);
-    } else {
-        if (type == NGEMM_F32) hipLaunchKernelGGL(kv_read_kernel<F32>, grid, block, 0, st, a);
-        else if (type == NGEMM_F16) hipLaunchKernelGGL(kv_read_kernel<F16>, grid, block, 0, st, a);
-        else hipLaunchKernelGGL(kv_read_kernel<BF16>, grid, block, 0, st, a);
-    }
+    if (type == NGEMM_F32) launch_move<F32>(write, vec, (unsigned)groups, st, a);
+    else if (type == NGEMM_F16) launch_move<F16>(write, vec, (unsigned)groups, st, a);
+    else launch_move<BF16>(write, vec, (unsigned)groups, st, a);
     return launched();
 }
 
@@ -150,11 +161,8 @@ bool allow_prompt_form()
            allow_prompt_lds<BF16, C, true>() == hipSuccess && allow_prompt_lds<BF16, C, false>() == hipSuccess;
 }
 
-// 16-byte pieces: bases and strides of 16-byte multiples, and a tile's offsets within 31 bits.
-bool rows_in_pieces(const Rows &r)
-{
-    return ((uintptr_t)r.data & 15u) == 0 && r.token_stride % 8 == 0 && r.head_stride % 8 == 0 && r.token_stride < (1 << 23);
-}
+// Copies of 16-byte pieces, a tile's offsets within 31 bits.
+bool rows_in_pieces(const Rows &r) { return in_pieces(r, NGEMM_BF16) && r.token_stride < (1 << 23); }
 
 template <class E, class C>
 void launch_prompt_form(PromptArgs a, bool vec, hipStream_t st)

@@ -69,12 +69,7 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
     const int group = a.q_heads / a.kv_heads, D = a.head_dim;
 
     // Sequence b has the slots floor(rows before it / BM) + b .. : as many as its rows need or one more.
-    int lo = 0, hi = a.batch;
-    while (hi - lo > 1) {
-        const int mid = (lo + hi) / 2;
-        if (a.q_offsets[mid] * group / BM + mid <= slot) lo = mid; else hi = mid;
-    }
-    const int b = lo;
+    const int b = last_start(a.batch, slot, [&](int x) { return a.q_offsets[x] * group / BM + x; });
     const int q_first = min(max(a.q_offsets[b], 0), a.q_tokens), queries = min(max(a.q_offsets[b + 1], q_first), a.q_tokens) - q_first;
     const int row0 = (slot - (a.q_offsets[b] * group / BM + b)) * BM, rows = queries * group;
     if (row0 < 0 || row0 >= rows) return;
