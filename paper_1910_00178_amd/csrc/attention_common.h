@@ -46,4 +46,26 @@ __device__ __forceinline__ float sum_of_halves(float x)
     return __uint_as_float(s[0]) + __uint_as_float(s[1]);
 }
 
+// Work on one output that is split over workgroups: each stores its part in the workspace, and the one that finds the others' flags set joins
+// them.  A flag is set to the call's own number, which no workspace holds by chance, and cleared by who joins, so that a workspace needs no
+// clearing and a captured call can be replayed.  Nobody waits: whoever sets the last flag finds all of them, unless another that
+// found them too has begun to clear.  All threads of the workgroup call this after their stores; what it returns is the same in all of them.
+__device__ __forceinline__ bool all_parts_stored(uint64_t *flags, int parts, int mine, uint64_t call)
+{
+    __threadfence();
+    __syncthreads();
+    bool there = true;
+    if (threadIdx.x < 64) {
+        if (threadIdx.x == 0) (void)__hip_atomic_exchange(flags + mine, call, __ATOMIC_SEQ_CST, __HIP_MEMORY_SCOPE_AGENT);
+        for (int i = threadIdx.x; i < parts; i += 64)
+            there = there && __hip_atomic_load(flags + i, __ATOMIC_SEQ_CST, __HIP_MEMORY_SCOPE_AGENT) == call;
+    }
+    there = __syncthreads_and(there);
+    if (there) {
+        __threadfence();
+        for (int i = threadIdx.x; i < parts; i += blockDim.x) __hip_atomic_store(flags + i, 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
+    return there;
+}
+
 }  // namespace ngemm

@@ -11,6 +11,10 @@ struct PromptArgs {
     float scale;             // of the scores, times log2 e; not negative (Q's sign is turned instead)
     uint32_t q_xor;
     int32_t slots;           // tiles of query rows that the grid has room for
+    int32_t splits;          // workgroups that may share a tile's keys
+    uint64_t call;
+    uint64_t *flags;         // splits > 1: [slots][kv_heads][splits]
+    f4 *parts;               // as many times kPart
 };
 
 // DP: head_dim rounded up; NW wavefronts of 32 rows; BN keys per tile.
@@ -20,6 +24,7 @@ struct PromptCfg {
     static constexpr int BM = 32 * NW, CH = DP / 8;              // CH: 16-byte chunks of a row
     static constexpr int kTile = BN * DP * 2, kStage = 2 * kTile, kLds = 2 * kStage;
     static constexpr int LOADS = kTile / 1024 / NW;              // 1 KiB copies of K (and of V) per wavefront
+    static constexpr int kPart = NW * 64 * (DP / 8 + 1);         // 16-byte pieces of a part: sums, maximum and weight
     static_assert(kTile % (1024 * NW) == 0, "whole copies");
     // Where chunk c of key j lies: so that 16 consecutive keys' equal chunks of K, and the 64 bytes of four consecutive keys of V,
     // fall on different banks (64 banks of 4 bytes).
@@ -65,7 +70,8 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
     typedef typename E::T T;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int half = lane >> 5, col = lane & 31;
-    const int head = blockIdx.x % a.kv_heads, slot = a.slots - 1 - blockIdx.x / a.kv_heads;
+    const int head = blockIdx.x % a.kv_heads, split = blockIdx.x / a.kv_heads % a.splits;
+    const int slot = a.slots - 1 - blockIdx.x / a.kv_heads / a.splits;
     const int group = a.q_heads / a.kv_heads, D = a.head_dim;
 
     // Sequence b has the slots floor(rows before it / BM) + b .. : as many as its rows need or one more.
@@ -84,7 +90,12 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
     const int wave_first = min(row0 + 32 * wave, rows - 1), wave_last = min(row0 + 32 * wave + 31, rows - 1);
     const int seen_by_all = last_seen(wave_first), seen_by_any = last_seen(wave_last);
     const int group_seen_by_all = last_seen(row0), group_seen_by_any = last_seen(min(row0 + BM, rows) - 1);
-    const int tiles = (group_seen_by_any + BN) / BN;             // group_seen_by_any >= -1 or no tile
+    const int all_tiles = max(0, (group_seen_by_any + BN) / BN);
+    // the workgroups of a tile take equal runs of its key tiles, of at least 256 keys
+    const int run = a.splits > 1 ? max((all_tiles + a.splits - 1) / a.splits, 256 / BN) : all_tiles;
+    const int parts = a.splits > 1 ? max(1, (all_tiles + run - 1) / run) : 1;
+    if (split >= parts) return;
+    const int first_tile = split * run, tiles = min(all_tiles, first_tile + run);
 
     const T *kbase = (const T *)a.k.data + k_first * a.k.token_stride + head * a.k.head_stride;
     const T *vbase = (const T *)a.v.data + k_first * a.v.token_stride + head * a.v.head_stride;
@@ -123,7 +134,7 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
             }
         }
     };
-    if (tiles > 0) load_tile(0, 0);
+    if (first_tile < tiles) load_tile(first_tile, first_tile & 1);
 
     // ---- Q^T's operand: 8 elements of the lane's row per step ----
     u4 q[DP / 16];
@@ -163,7 +174,7 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
     // m: what the weights are relative to, in units of the scores; no less than a number whose product with the scale is finite
     float m = -3.0e38f / fmaxf(a.scale, 1.0f), l = 0.0f;
 
-    for (int tile = 0; tile < tiles; ++tile) {
+    for (int tile = first_tile; tile < tiles; ++tile) {
         const int stage = tile & 1;
         __builtin_amdgcn_s_waitcnt(0);
         __syncthreads();
@@ -250,8 +261,38 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
         }
     }
 
-    // ---- O = O^T / l: 4 consecutive elements per lane and quarter, exchanged between lane halves to 8 ----
     l = sum_of_halves(l);
+    if (parts > 1) {
+        const int64_t at = ((int64_t)slot * a.kv_heads + head) * a.splits;
+        f4 *mine = a.parts + (at + split) * C::kPart + tid;
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mine[(4 * t + i) * NW * 64] = (f4){o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
+        mine[DP / 8 * NW * 64] = (f4){m, l, 0.0f, 0.0f};
+        if (!all_parts_stored(a.flags + at, parts, split, a.call)) return;
+        const f4 *from = a.parts + at * C::kPart + tid;
+        float top = m;
+        for (int p = 0; p < parts; ++p) top = fmaxf(top, from[p * C::kPart + DP / 8 * NW * 64][0]);
+        l = 0.0f;
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t) o[t] = (f16v)(0.0f);
+        for (int p = 0; p < parts; ++p, from += C::kPart) {      // in their order, whoever joins them
+            const f4 stats = from[DP / 8 * NW * 64];
+            const float fall = __builtin_amdgcn_exp2f((stats[0] - top) * a.scale);
+            l += stats[1] * fall;
+#pragma unroll
+            for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const f4 x = from[(4 * t + i) * NW * 64];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[t][4 * i + e] += x[e] * fall;
+                }
+        }
+    }
+
+    // ---- O = O^T / l: 4 consecutive elements per lane and quarter, exchanged between lane halves to 8 ----
     const float by = seen < 0 ? 0.0f : 1.0f / l;
     T *out = (T *)a.o.data + (q_first + query) * a.o.token_stride + qhead * a.o.head_stride;
 #pragma unroll
