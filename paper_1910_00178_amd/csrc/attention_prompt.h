@@ -22,7 +22,7 @@ template <int DP_, int NW_, int BN_, int PER_CU_>
 struct PromptCfg {
     static constexpr int DP = DP_, NW = NW_, BN = BN_, PER_CU = PER_CU_;
     static constexpr int BM = 32 * NW, CH = DP / 8;              // CH: 16-byte chunks of a row
-    static constexpr int kTile = BN * DP * 2, kStage = 2 * kTile, kLds = 2 * kStage;
+    static constexpr int kTile = BN * DP * 2, kStage = 2 * kTile, kLds = 2 * kStage + 16;
     static constexpr int LOADS = kTile / 1024 / NW;              // 1 KiB copies of K (and of V) per wavefront
     static constexpr int kPart = NW * 64 * (DP / 8 + 1);         // 16-byte pieces of a part: sums, maximum and weight
     static_assert(kTile % (1024 * NW) == 0, "whole copies");
@@ -47,16 +47,22 @@ __device__ __forceinline__ uint32_t max_u16(uint32_t a, uint32_t b)
 template <class E> constexpr uint32_t kInfinity = 0x7f80;
 template <> constexpr uint32_t kInfinity<F16> = 0x7c00;
 
-// Copies memory -> LDS, 16 bytes a lane; what lies past the buffer's end becomes 0.  (No templates: the host pass, which cannot know the
-// copies' width, drops a template's instance with such a call in it.)
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void *from, int bytes)
+// Copies memory -> LDS, 16 bytes a lane from base + offset; what lies past the buffer's end becomes 0.  Written as the instruction: behind
+// the builtin, the compiler lets the transposing LDS reads wait for every copy in flight, those of the next tile among them.  No
+// register is written; who reads the LDS waits with copies_landed() and a barrier.
+typedef uint32_t Buffer __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ Buffer buffer_of(const void *from, int bytes)
 {
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(from), (short)0, bytes, 0x00020000);
+    const uint64_t at = (uint64_t)from;
+    return (Buffer){(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at), (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32)) & 0xffffu,
+                    (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
 }
-__device__ __forceinline__ void copy_to_lds(__amdgpu_buffer_rsrc_t from, uint8_t *to, uint32_t offset)
+__device__ __forceinline__ void copy_to_lds(Buffer from, uint32_t lds_at, uint32_t offset)
 {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(from, (lds_ptr)to, 16, offset, 0, 0, 0);
+    // (five wait states: what a vector instruction that wrote the descriptor's registers needs; M0 needs one)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_at), "v"(offset), "s"(from) : "memory");
 }
+__device__ __forceinline__ void copies_landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // Rows of a workgroup: the queries of a sequence times the q_heads / kv_heads heads that share a K/V head, heads fastest.  S^T = K Q^T
 // and O^T = V^T P^T on 32 x 32 x 16 matrix instructions: a lane holds scores of one row (lane % 32), so the softmax needs one exchange of
@@ -119,9 +125,10 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
             const int64_t stride = which ? a.v.token_stride : a.k.token_stride;
             uint8_t *to = lds + stage * C::kStage + which * C::kTile;
             if constexpr (VEC) {
-                const __amdgpu_buffer_rsrc_t rsrc = buffer_of(from, (int)((left - 1) * stride * 2 + D * 2));
+                const Buffer buffer = buffer_of(from, (int)((left - 1) * stride * 2 + D * 2));
 #pragma unroll
-                for (int i = 0; i < C::LOADS; ++i) copy_to_lds(rsrc, to + (i * NW + wave) * 1024, kv_off[which][i]);
+                for (int i = 0; i < C::LOADS; ++i)
+                    copy_to_lds(buffer, (uint32_t)(uintptr_t)(lds_ptr)(to + (i * NW + wave) * 1024), kv_off[which][i]);
             } else {
                 for (int i = 0; i < C::LOADS; ++i) {
                     const int s = (i * NW + wave) * 64 + lane, j = s / CH;
@@ -134,6 +141,8 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
             }
         }
     };
+    volatile int *odd_seen = (volatile int *)(lds + 2 * C::kStage);
+    if (tid < 2) odd_seen[tid] = 0;
     if (first_tile < tiles) load_tile(first_tile, first_tile & 1);
 
     // ---- Q^T's operand: 8 elements of the lane's row per step ----
@@ -156,17 +165,11 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
         }
     }
 
-    // ---- LDS addresses of the operands, which the two stages turn by a bit ----
-    int k_at[DP / 16], v_at[DP / 32][2];
-#pragma unroll
-    for (int s = 0; s < DP / 16; ++s) k_at[s] = col * DP * 2 + ((2 * s + half) ^ C::k_swizzle(col)) * 16;
-#pragma unroll
-    for (int t = 0; t < DP / 32; ++t)
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int i = lane & 15, j = 8 * h + 4 * half + (i >> 2), c = 4 * t + 2 * ((lane >> 4) & 1) + ((i & 3) >> 1);
-            v_at[t][h] = C::kTile + j * DP * 2 + (c ^ C::v_swizzle(j)) * 16 + (i & 1) * 8;
-        }
+    // ---- LDS places of the operands: a row's and, apart because of the swizzle, a chunk's ----
+    const int v_token = 4 * half + ((lane & 15) >> 2);           // of 8 or 16: the transposing read's lanes give 4 elements of a key each
+    const int k_row = col * DP * 2, v_row = C::kTile + v_token * DP * 2 + (lane & 1) * 8;
+    int k_chunk = (half ^ C::k_swizzle(col)) * 16;
+    int v_chunk = ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ C::v_swizzle(v_token)) * 16;
 
     f16v o[DP / 32];
 #pragma unroll
@@ -176,10 +179,12 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
 
     for (int tile = first_tile; tile < tiles; ++tile) {
         const int stage = tile & 1;
-        __builtin_amdgcn_s_waitcnt(0);
+        copies_landed();
         __syncthreads();
         if (tile + 1 < tiles) load_tile(tile + 1, stage ^ 1);
         const uint8_t *at = lds + stage * C::kStage;
+        // (not known to stay the same: one instruction per read is cheaper than the registers of all places)
+        asm volatile("" : "+v"(k_chunk), "+v"(v_chunk));
         const bool masked = tile * BN + BN - 1 > group_seen_by_all;          // for some row of the workgroup
         bool odd = false;
         if (masked) {                            // a value that some row does not see must not reach it through 0 * infinity
@@ -188,7 +193,10 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
                 const u4 x = *(const u4 *)(at + C::kTile + ((i * NW + wave) * 64 + lane) * 16) & 0x7fff7fffu;
                 most = max_u16(most, max_u16(max_u16(x[0], x[1]), max_u16(x[2], x[3])));
             }
-            odd = __syncthreads_or((most & 0xffff) >= kInfinity<E> || (most >> 16) >= kInfinity<E>);
+            if ((most & 0xffff) >= kInfinity<E> || (most >> 16) >= kInfinity<E>) odd_seen[tile & 1] = 1;
+            if (tid == 0) odd_seen[~tile & 1] = 0;       // read before this tile's first barrier, written behind the next tile's
+            __syncthreads();
+            odd = odd_seen[tile & 1] != 0;
         }
         if (tile * BN > seen_by_any) continue;
         f16v s[BN / 32];
@@ -197,7 +205,7 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
             s[t] = (f16v)(0.0f);
 #pragma unroll
             for (int u = 0; u < DP / 16; ++u)
-                s[t] = mfma32(E{}, *(const u4 *)(at + k_at[u] + t * 32 * DP * 2), q[u], s[t]);
+                s[t] = mfma32(E{}, *(const u4 *)(at + k_row + (k_chunk ^ 32 * u) + t * 32 * DP * 2), q[u], s[t]);
         }
         if (tile * BN + BN - 1 > seen_by_all) {
 #pragma unroll
@@ -230,33 +238,48 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
                 l += x + y;
                 p[2 * t + i / 8][(i % 8) / 2] = pack2<E>(x, y);
             }
+        auto v_operand = [&](int t, int u) {
+            const uint8_t *from = at + v_row + (v_chunk ^ 64 * t) + u * 16 * DP * 2;
+            const u2 v0 = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)from));
+            const u2 v1 = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(from + 8 * DP * 2)));
+            return (u4){v0[0], v0[1], v1[0], v1[1]};
+        };
+        if (!odd) {
 #pragma unroll
-        for (int u = 0; u < BN / 16; ++u)
+            for (int u = 0; u < BN / 16; ++u)
+#pragma unroll
+                for (int t = 0; t < DP / 32; ++t) o[t] = mfma32(E{}, v_operand(t, u), p[u], o[t]);
+        } else {                                 // infinities and NaN apart: how many of either sign a row sees
+            u4 sees[BN / 16];
+#pragma unroll
+            for (int u = 0; u < BN / 16; ++u)
+#pragma unroll
+                for (int i = 0; i < 8; i += 2) {
+                    const int key = tile * BN + 16 * u + 8 * (i / 4) + 4 * half + i % 4;
+                    sees[u][i / 2] = pack2<E>(key <= seen ? 1.0f : 0.0f, key + 1 <= seen ? 1.0f : 0.0f);
+                }
 #pragma unroll
             for (int t = 0; t < DP / 32; ++t) {
-                const u2 v0 = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(at + v_at[t][0] + u * 16 * DP * 2)));
-                const u2 v1 = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(at + v_at[t][1] + u * 16 * DP * 2)));
-                u4 v = {v0[0], v0[1], v1[0], v1[1]};
-                if (odd) {                       // infinities and NaN apart, below
+                f16v up = (f16v)(0.0f), down = (f16v)(0.0f);
+#pragma unroll
+                for (int u = 0; u < BN / 16; ++u) {
+                    u4 v = v_operand(t, u), plus, minus;
 #pragma unroll
                     for (int e = 0; e < 4; ++e) {
-                        if ((v[e] & 0x7fff) >= kInfinity<E>) v[e] &= 0xffff0000u;
-                        if ((v[e] >> 16 & 0x7fff) >= kInfinity<E>) v[e] &= 0xffffu;
+                        const uint32_t lo = v[e] & 0xffff, hi = v[e] >> 16;
+                        const uint32_t odd_lo = (lo & 0x7fff) >= kInfinity<E> ? 0xffffu : 0u, odd_hi = (hi & 0x7fff) >= kInfinity<E> ? 0xffff0000u : 0u;
+                        const uint32_t ones = (odd_lo | odd_hi) & (E::kOne | E::kOne << 16);
+                        plus[e] = ones & ((lo == (kInfinity<E> | 0x8000u) ? 0u : 0xffffu) | (hi == (kInfinity<E> | 0x8000u) ? 0u : 0xffff0000u));
+                        minus[e] = ones & ((lo == kInfinity<E> ? 0u : 0xffffu) | (hi == kInfinity<E> ? 0u : 0xffff0000u));
+                        v[e] &= ~(odd_lo | odd_hi);
                     }
+                    o[t] = mfma32(E{}, v, p[u], o[t]);
+                    up = mfma32(E{}, plus, sees[u], up);
+                    down = mfma32(E{}, minus, sees[u], down);
                 }
-                o[t] = mfma32(E{}, v, p[u], o[t]);
-            }
-        if (odd) {
-            for (int j = 0; j < BN; ++j) {
-                if (tile * BN + j > seen) break;
 #pragma unroll
-                for (int t = 0; t < DP / 32; ++t)
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        const int d = 32 * t + 8 * (i / 4) + 4 * half + i % 4;
-                        const uint16_t x = *(const uint16_t *)(at + C::kTile + j * DP * 2 + ((d / 8) ^ C::v_swizzle(j)) * 16 + d % 8 * 2);
-                        if ((x & 0x7fff) >= kInfinity<E>) o[t][i] += E::get(__builtin_bit_cast(T, x));
-                    }
+                for (int i = 0; i < 16; ++i)
+                    o[t][i] += (up[i] > 0.0f ? __builtin_inff() : 0.0f) - (down[i] > 0.0f ? __builtin_inff() : 0.0f);
             }
         }
     }

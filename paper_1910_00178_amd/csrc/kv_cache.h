@@ -41,11 +41,13 @@ struct F32 {
 };
 struct F16 {
     typedef _Float16 T;
+    static constexpr uint32_t kOne = 0x3c00;
     static __device__ __forceinline__ float get(T x) { return (float)x; }
     static __device__ __forceinline__ T put(float x) { return (_Float16)x; }
 };
 struct BF16 {
     typedef __bf16 T;
+    static constexpr uint32_t kOne = 0x3f80;
     static __device__ __forceinline__ float get(T x) { return (float)x; }
     static __device__ __forceinline__ T put(float x) { return (__bf16)x; }
 };
