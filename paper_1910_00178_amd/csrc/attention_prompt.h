@@ -199,13 +199,22 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
             odd = odd_seen[tile & 1] != 0;
         }
         if (tile * BN > seen_by_any) continue;
+        // operands are read a group ahead of the products that take them
         f16v s[BN / 32];
+        u4 k_ahead[2][DP / 16];
+        auto read_keys = [&](int t) {
+#pragma unroll
+            for (int u = 0; u < DP / 16; ++u) k_ahead[t & 1][u] = *(const u4 *)(at + k_row + (k_chunk ^ 32 * u) + t * 32 * DP * 2);
+        };
+        read_keys(0);
 #pragma unroll
         for (int t = 0; t < BN / 32; ++t) {
+            if (t + 1 < BN / 32) read_keys(t + 1);
+            __builtin_amdgcn_sched_barrier(0);
             s[t] = (f16v)(0.0f);
 #pragma unroll
-            for (int u = 0; u < DP / 16; ++u)
-                s[t] = mfma32(E{}, *(const u4 *)(at + k_row + (k_chunk ^ 32 * u) + t * 32 * DP * 2), q[u], s[t]);
+            for (int u = 0; u < DP / 16; ++u) s[t] = mfma32(E{}, k_ahead[t & 1][u], q[u], s[t]);
+            __builtin_amdgcn_sched_barrier(0);
         }
         if (tile * BN + BN - 1 > seen_by_all) {
 #pragma unroll
@@ -245,10 +254,20 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
             return (u4){v0[0], v0[1], v1[0], v1[1]};
         };
         if (!odd) {
+            u4 v_ahead[2][DP / 32];
 #pragma unroll
-            for (int u = 0; u < BN / 16; ++u)
+            for (int t = 0; t < DP / 32; ++t) v_ahead[0][t] = v_operand(t, 0);
 #pragma unroll
-                for (int t = 0; t < DP / 32; ++t) o[t] = mfma32(E{}, v_operand(t, u), p[u], o[t]);
+            for (int u = 0; u < BN / 16; ++u) {
+                if (u + 1 < BN / 16) {
+#pragma unroll
+                    for (int t = 0; t < DP / 32; ++t) v_ahead[(u + 1) & 1][t] = v_operand(t, u + 1);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+                for (int t = 0; t < DP / 32; ++t) o[t] = mfma32(E{}, v_ahead[u & 1][t], p[u], o[t]);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         } else {                                 // infinities and NaN apart: how many of either sign a row sees
             u4 sees[BN / 16];
 #pragma unroll
