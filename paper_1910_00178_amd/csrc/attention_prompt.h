@@ -229,7 +229,7 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
 #pragma unroll
             for (int i = 0; i < 16; ++i) most = fmaxf(most, s[t][i]);
         most = max_of_halves(most);
-        if (__any(most > m)) {
+        if (__any((most - m) * a.scale > 8.0f)) {            // weights up to 2^8 fit: most tiles leave the sums as they are
             const float fall = __builtin_amdgcn_exp2f((m - most) * a.scale);
             l *= fall;
 #pragma unroll
@@ -310,24 +310,25 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
 #pragma unroll
         for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) mine[(4 * t + i) * NW * 64] = (f4){o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
-        mine[DP / 8 * NW * 64] = (f4){m, l, 0.0f, 0.0f};
-        if (!all_parts_stored(a.flags + at, parts, split, a.call)) return;
+            for (int i = 0; i < 4; ++i)
+                store_part(mine + (4 * t + i) * NW * 64, (f4){o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]});
+        store_part(mine + DP / 8 * NW * 64, (f4){m, l, 0.0f, 0.0f});
+        if (!all_parts_stored(a.flags + at, parts, split, a.call, odd_seen + 2)) return;
         const f4 *from = a.parts + at * C::kPart + tid;
         float top = m;
-        for (int p = 0; p < parts; ++p) top = fmaxf(top, from[p * C::kPart + DP / 8 * NW * 64][0]);
+        for (int p = 0; p < parts; ++p) top = fmaxf(top, load_part(from + p * C::kPart + DP / 8 * NW * 64)[0]);
         l = 0.0f;
 #pragma unroll
         for (int t = 0; t < DP / 32; ++t) o[t] = (f16v)(0.0f);
         for (int p = 0; p < parts; ++p, from += C::kPart) {      // in their order, whoever joins them
-            const f4 stats = from[DP / 8 * NW * 64];
+            const f4 stats = load_part(from + DP / 8 * NW * 64);
             const float fall = __builtin_amdgcn_exp2f((stats[0] - top) * a.scale);
             l += stats[1] * fall;
 #pragma unroll
             for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const f4 x = from[(4 * t + i) * NW * 64];
+                    const f4 x = load_part(from + (4 * t + i) * NW * 64);
 #pragma unroll
                     for (int e = 0; e < 4; ++e) o[t][4 * i + e] += x[e] * fall;
                 }
