@@ -11,12 +11,7 @@ struct DecodeArgs {
     int32_t batch, q_heads, max_length;
     int32_t chunk, chunks;   // tokens of a workgroup, workgroups along a sequence
     float scale;             // of the scores, times log2 e
-    // chunks > 1, of every sequence, K/V head and 16 heads of it: flags, then parts of (16 head_dim + 32) floats at most
-    uint64_t call;
-    uint64_t *flags;
-    f4 *parts;
-    int32_t part_pieces;     // 16-byte pieces of a part
-    int32_t q_pieces, o_pieces;          // whether rows lie at 16-byte multiples
+    float *part;             // chunks > 1: [batch][q_heads][chunks][head_dim] sums, then [batch][q_heads][chunks][2] maxima and weights
 };
 
 constexpr int kDecodeWaves = 4;
@@ -111,17 +106,13 @@ __global__ __launch_bounds__(kDecodeWaves * 64, NJ == 1 ? 4 : NJ == 2 ? 3 : NJ =
         const T *row = (const T *)a.q.data + b * a.q.token_stride + qh * a.q.head_stride;
         float x[2 * NJ][8], most = 0.0f;
 #pragma unroll
-        for (int s = 0; s < 2 * NJ; ++s) {
-            const int d = 64 * (s / 2) + 16 * g + 8 * (s % 2);
-            const T *from = row + (d < D ? d : 0);
-            if (a.q_pieces) load8<E, true>(from, x[s]);
-            else load8<E, false>(from, x[s]);
+        for (int s = 0; s < 2 * NJ; ++s)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                if (d >= D || h >= heads) x[s][e] = 0.0f;
+                const int d = 64 * (s / 2) + 16 * g + 8 * (s % 2) + e;
+                x[s][e] = d < D && h < heads ? E::get(row[d < D ? d : 0]) : 0.0f;
                 most = fmaxf(most, fabsf(x[s][e]));
             }
-        }
         int turn = 0;
         if constexpr (sizeof(T) == 2 && !__is_same(T, _Float16)) {
             most = max_of_rows(most);
@@ -243,61 +234,52 @@ __global__ __launch_bounds__(kDecodeWaves * 64, NJ == 1 ? 4 : NJ == 2 ? 3 : NJ =
             if (16 * t < D) *(f4 *)(mine + 16 * t + 4 * g) = o[t] * (fall * unit);
     }
     __syncthreads();
-    // a thread's pieces of 4 elements: of all wavefronts, then of all chunks
-    const int pieces = heads * D / 4, length = min(a.lengths[b], a.max_length), parts = a.chunks > 1 ? max(1, (length + a.chunk - 1) / a.chunk) : 1;
-    const int64_t at = (((int64_t)b * kv_heads + head) * head_tiles + head_tile) * a.chunks;
-    auto of_waves = [&](int i, float &ref, float &weight) {
-        const int hh = 4 * i / D;
-        f4 sum = (f4)(0.0f);
-        weight = 0.0f;
-        ref = -3.0e38f;
+    for (int i = threadIdx.x; i < heads * D; i += NW * 64) {
+        const int hh = i / D, d = i - hh * D;
+        float sum = 0.0f, weight = 0.0f, ref = -3.0e38f;
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            sum += *(const f4 *)(os + w * heads * D + 4 * i);
+            sum += os[w * heads * D + i];
             weight += ls[16 * w + hh];
             ref = fmaxf(ref, ms[16 * w + hh]);
         }
-        return sum;
-    };
-    auto put = [&](int i, f4 sum, float weight) {
-        const int hh = 4 * i / D, d = 4 * i - hh * D;
-        float x[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) x[e] = weight == 0.0f ? 0.0f : sum[e] / weight;
-        T *to = (T *)a.o.data + b * a.o.token_stride + (q_head0 + hh) * a.o.head_stride + d;
-        if (a.o_pieces) store<E, 4, true>(to, x);
-        else store<E, 4, false>(to, x);
-    };
-    if (parts == 1) {
-        for (int i = threadIdx.x; i < pieces; i += NW * 64) {
-            float ref, weight;
-            const f4 sum = of_waves(i, ref, weight);
-            put(i, sum, weight);
+        const int qh = q_head0 + hh;
+        if (a.chunks > 1) {
+            const int64_t at = ((int64_t)b * a.q_heads + qh) * a.chunks + chunk;
+            a.part[at * D + d] = sum;
+            if (d == 0) {
+                float *stats = a.part + (int64_t)a.batch * a.q_heads * a.chunks * D + 2 * at;
+                stats[0] = ref;
+                stats[1] = weight;
+            }
+        } else {
+            ((T *)a.o.data)[b * a.o.token_stride + qh * a.o.head_stride + d] = E::put(weight == 0.0f ? 0.0f : sum / weight);
         }
-        return;
     }
-    f4 *mine = a.parts + (at + chunk) * a.part_pieces;
-    for (int i = threadIdx.x; i < pieces; i += NW * 64) {
-        float ref, weight;
-        const f4 sum = of_waves(i, ref, weight);
-        store_part(mine + heads + i, sum);
-        if (4 * i % D == 0) store_part(mine + 4 * i / D, (f4){ref, weight, 0.0f, 0.0f});
+}
+
+// The chunks of a sequence and query head, joined in their order.  A workgroup per sequence and head.
+template <class E>
+__global__ __launch_bounds__(256) void attention_decode_join_kernel(const DecodeArgs a)
+{
+    __shared__ float sums[256 * 4];
+    typedef typename E::T T;
+    const int D = a.cache.head_dim, b = blockIdx.x / a.q_heads, qh = blockIdx.x % a.q_heads;
+    const int length = min(a.lengths[b], a.max_length), chunks = length > 0 ? (length + a.chunk - 1) / a.chunk : 1;
+    const int64_t at = (int64_t)blockIdx.x * a.chunks;
+    const float *part = a.part + at * D, *stats = a.part + (int64_t)a.batch * a.q_heads * a.chunks * D + 2 * at;
+    float top = -3.0e38f;
+    for (int c = 0; c < chunks; ++c) top = fmaxf(top, stats[2 * c]);
+    const int d = threadIdx.x;
+    if (d >= D) return;
+    float sum = 0.0f, weight = 0.0f;
+    for (int c = 0; c < chunks; ++c) {
+        const float fall = __builtin_amdgcn_exp2f(stats[2 * c] - top);
+        sum += part[c * D + d] * fall;
+        weight += stats[2 * c + 1] * fall;
     }
-    if (!all_parts_stored(a.flags + at, parts, chunk, a.call, (int *)ms)) return;
-    const f4 *from = a.parts + at * a.part_pieces;
-    for (int i = threadIdx.x; i < pieces; i += NW * 64) {
-        const int hh = 4 * i / D;
-        float ref = -3.0e38f, weight = 0.0f;
-        for (int c = 0; c < parts; ++c) ref = fmaxf(ref, from[c * a.part_pieces + hh][0]);
-        f4 sum = (f4)(0.0f);
-        for (int c = 0; c < parts; ++c) {
-            const f4 stats = from[c * a.part_pieces + hh], x = from[c * a.part_pieces + heads + i];
-            const float fall = __builtin_amdgcn_exp2f(stats[0] - ref);
-            weight += stats[1] * fall;
-            sum += x * fall;
-        }
-        put(i, sum, weight);
-    }
+    (void)sums;
+    ((T *)a.o.data)[b * a.o.token_stride + qh * a.o.head_stride + d] = E::put(weight == 0.0f ? 0.0f : sum / weight);
 }
 
 }  // namespace ngemm
