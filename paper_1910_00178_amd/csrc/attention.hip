@@ -50,16 +50,6 @@ CacheView view_of(const ngemm_kv_cache *c, const int32_t *pages, int64_t pages_s
                      (int32_t)(c->page_tokens / kBlockTokens)};
 }
 
-// A number for the flags of a call's parts: no two calls of a context share one, and a workspace does not hold it by chance.
-uint64_t call_number(ngemm_ctx *ctx)
-{
-    uint64_t x = (uint64_t)(uintptr_t)ctx * 0x9e3779b97f4a7c15ull + ctx->calls.fetch_add(1, std::memory_order_relaxed) + 1;
-    x = (x ^ (x >> 30)) * 0xbf58476d1ce4e5b9ull;
-    x = (x ^ (x >> 27)) * 0x94d049bb133111ebull;
-    x ^= x >> 31;
-    return x ? x : 1;
-}
-
 ngemm_status launched() { return hipGetLastError() == hipSuccess ? NGEMM_OK : NGEMM_ERR_DEVICE; }
 
 // Whether 16-byte pieces of rows lie at 16-byte multiples.
@@ -109,14 +99,17 @@ ngemm_status move_rows(bool write, ngemm_ctx *ctx, const ngemm_kv_cache *cache, 
 // sequence of middling length leaves balanced.
 struct DecodeCut {
     int64_t chunk, chunks;
+    size_t bytes;
 };
-DecodeCut decode_cut(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t max_length)
+DecodeCut decode_cut(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t max_length)
 {
     constexpr int64_t round = 64 * kDecodeWaves;
-    const int64_t grid = batch * kv_heads * ((q_heads / kv_heads + 15) / 16);
+    const int64_t group = q_heads / kv_heads, grid = batch * kv_heads * ((group + 15) / 16);
     int64_t chunk = (max_length * grid / 2048 + round - 1) / round * round;
     chunk = std::min<int64_t>(std::max<int64_t>(chunk, round), 1024);
-    return DecodeCut{chunk, std::max<int64_t>(1, (max_length + chunk - 1) / chunk)};
+    DecodeCut cut{chunk, std::max<int64_t>(1, (max_length + chunk - 1) / chunk), 0};
+    if (cut.chunks > 1) cut.bytes = (size_t)(batch * q_heads * cut.chunks * (head_dim / 4 + 1) * 16);
+    return cut;
 }
 
 template <class E, int NJ>
@@ -174,21 +167,21 @@ bool allow_prompt_form()
 // Copies of 16-byte pieces, a tile's offsets within 31 bits.
 bool rows_in_pieces(const Rows &r) { return in_pieces(r, NGEMM_BF16) && r.token_stride < (1 << 23); }
 
-// Tiles of query rows that any lengths of the sequences can need, and over how many workgroups their keys are split: two per unit together if the rows
-// were spread evenly, no more than leaves 512 keys each of sequences of equal lengths.
+// Tiles of query rows that any lengths of the sequences can need, and over how many workgroups their keys are split: as many as the units take at once
+// if the rows were spread evenly, of no less than kLeastRun keys of sequences of equal lengths.
 struct PromptCut {
     int64_t slots, splits;
-    size_t part_bytes;
+    size_t bytes;
 };
 template <class C>
 PromptCut prompt_cut(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t q_tokens, int64_t k_tokens)
 {
     const int64_t rows = q_tokens * (q_heads / kv_heads), tiles = std::max<int64_t>(batch, (rows + C::BM - 1) / C::BM) * kv_heads;
-    PromptCut cut{rows / C::BM + batch, 1, (size_t)C::kPart * 16};
-    cut.splits = std::max<int64_t>(1, std::min(256 * C::PER_CU / tiles, k_tokens / batch / 512));
+    PromptCut cut{rows / C::BM + batch, 1, 0};
+    cut.splits = std::max<int64_t>(1, std::min(256 * C::PER_CU / tiles, k_tokens / batch / kLeastRun));
+    if (cut.splits > 1) cut.bytes = (size_t)(cut.slots * kv_heads * cut.splits) * C::kPart * 16;
     return cut;
 }
-size_t flag_bytes(int64_t flags) { return (size_t)((flags * 8 + 255) / 256 * 256); }
 
 template <class E, class C>
 void launch_prompt_form(PromptArgs a, bool vec, void *workspace, hipStream_t st)
@@ -196,13 +189,14 @@ void launch_prompt_form(PromptArgs a, bool vec, void *workspace, hipStream_t st)
     const PromptCut cut = prompt_cut<C>(a.batch, a.q_heads, a.kv_heads, a.q_tokens, a.k_tokens);
     a.slots = (int32_t)cut.slots;
     a.splits = (int32_t)cut.splits;
-    if (cut.splits > 1) {
-        a.flags = (uint64_t *)workspace;
-        a.parts = (f4 *)((uint8_t *)workspace + flag_bytes(cut.slots * a.kv_heads * cut.splits));
-    }
+    a.parts = (f4 *)workspace;
     const dim3 grid((unsigned)(cut.slots * a.kv_heads * cut.splits)), block(C::NW * 64);
     if (vec) hipLaunchKernelGGL((attention_prompt_kernel<E, C, true>), grid, block, C::kLds, st, a);
     else hipLaunchKernelGGL((attention_prompt_kernel<E, C, false>), grid, block, C::kLds, st, a);
+    if (cut.splits == 1) return;
+    const dim3 pieces((unsigned)(cut.slots * a.kv_heads * (C::DP / 8)));
+    if (vec) hipLaunchKernelGGL((attention_prompt_join_kernel<E, C, true>), pieces, block, 0, st, a);
+    else hipLaunchKernelGGL((attention_prompt_join_kernel<E, C, false>), pieces, block, 0, st, a);
 }
 
 template <class E>
@@ -282,8 +276,7 @@ size_t ngemm_attention_decode_workspace_bytes(int64_t batch, int64_t q_heads, in
     if (batch < 1 || q_heads < 1 || kv_heads < 1 || q_heads % kv_heads || !head_dim_ok(head_dim) || max_length < 0 || max_length > kMaxCount ||
         batch > kMaxCount || q_heads > 65536 || batch * q_heads > kMaxCount)
         return 0;
-    const DecodeCut cut = decode_cut(batch, q_heads, kv_heads, max_length);
-    return cut.chunks > 1 ? (size_t)(batch * q_heads * cut.chunks * (head_dim + 2) * 4) : 0;
+    return decode_cut(batch, q_heads, kv_heads, head_dim, max_length).bytes;
 }
 
 ngemm_status ngemm_attention_decode(ngemm_ctx *ctx, const ngemm_kv_cache *cache, ngemm_type type, int64_t batch, int64_t q_heads,
@@ -309,10 +302,10 @@ ngemm_status ngemm_attention_decode(ngemm_ctx *ctx, const ngemm_kv_cache *cache,
     if (need > 0 && ((uintptr_t)workspace_dev & 15u) != 0) return NGEMM_ERR_INVALID_ARG;
     DeviceGuard g(ctx->device);
     if (!g.ok) return NGEMM_ERR_DEVICE;
-    const DecodeCut cut = decode_cut(batch, q_heads, cache->kv_heads, max_length);
+    const DecodeCut cut = decode_cut(batch, q_heads, cache->kv_heads, cache->head_dim, max_length);
     if (batch * q_heads * cut.chunks > kMaxCount) return NGEMM_ERR_BAD_SHAPE;
     const DecodeArgs a{view_of(cache, pages_dev, pages_stride), q, o, lengths_dev, (int32_t)batch, (int32_t)q_heads, (int32_t)max_length,
-                       (int32_t)cut.chunk, (int32_t)cut.chunks, scale * 1.44269504f, (float *)workspace_dev};
+                       (int32_t)cut.chunk, (int32_t)cut.chunks, scale * 1.44269504f, (f4 *)workspace_dev, in_pieces(q, type), in_pieces(o, type)};
     hipStream_t st = (hipStream_t)hip_stream;
     if (type == NGEMM_F16) launch_decode<F16>(a, st);
     else launch_decode<BF16>(a, st);
@@ -327,9 +320,7 @@ size_t ngemm_attention_prompt_workspace_bytes(int64_t batch, int64_t q_heads, in
         return 0;
     size_t bytes = 0;
     with_prompt_form(head_dim, [&](auto form) {
-        const PromptCut cut = prompt_cut<decltype(form)>(batch, q_heads, kv_heads, q_tokens, k_tokens);
-        const int64_t parts = cut.slots * kv_heads * cut.splits;
-        if (cut.splits > 1) bytes = flag_bytes(parts) + parts * cut.part_bytes;
+        bytes = prompt_cut<decltype(form)>(batch, q_heads, kv_heads, q_tokens, k_tokens).bytes;
     });
     return bytes;
 }
@@ -365,7 +356,7 @@ ngemm_status ngemm_attention_prompt(ngemm_ctx *ctx, ngemm_type type, int64_t bat
     // the kernel's scale is not negative (the sign goes to Q), and not 0 (hidden scores are minus infinity)
     const float scale2 = std::fmax(std::fabs(scale) * 1.44269504f, 1.17549435e-38f);
     const PromptArgs a{q, k, v, o, q_offsets_dev, k_offsets_dev ? k_offsets_dev : q_offsets_dev, (int32_t)batch, (int32_t)q_heads, (int32_t)kv_heads,
-                       (int32_t)head_dim, (int32_t)q_tokens, (int32_t)k_tokens, causal != 0, scale2, std::signbit(scale) ? 0x80008000u : 0u, 0, 0, call_number(ctx), nullptr, nullptr};
+                       (int32_t)head_dim, (int32_t)q_tokens, (int32_t)k_tokens, causal != 0, scale2, std::signbit(scale) ? 0x80008000u : 0u, 0, 0, nullptr};
     const bool vec = rows_in_pieces(q) && rows_in_pieces(k) && rows_in_pieces(v) && rows_in_pieces(o);
     hipStream_t st = (hipStream_t)hip_stream;
     if (type == NGEMM_F16) launch_prompt<F16>(a, vec, workspace_dev, st);

@@ -11,7 +11,8 @@ struct DecodeArgs {
     int32_t batch, q_heads, max_length;
     int32_t chunk, chunks;   // tokens of a workgroup, workgroups along a sequence
     float scale;             // of the scores, times log2 e
-    float *part;             // chunks > 1: [batch][q_heads][chunks][head_dim] sums, then [batch][q_heads][chunks][2] maxima and weights
+    f4 *parts;               // chunks > 1: [batch][q_heads][chunks] times head_dim / 4 + 1: maximum and weight, sums
+    int32_t q_pieces, o_pieces;          // whether rows lie at 16-byte multiples
 };
 
 constexpr int kDecodeWaves = 4;
@@ -60,6 +61,18 @@ __device__ __forceinline__ void unrolled(F &&f)
     }
 }
 
+// Elements d .. d + 3 of an output row (0 where nothing was seen).
+template <class E>
+__device__ __forceinline__ void put_row(const DecodeArgs &a, int b, int qh, int d, f4 sum, float weight)
+{
+    float x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = weight == 0.0f ? 0.0f : sum[e] / weight;
+    typename E::T *to = (typename E::T *)a.o.data + b * a.o.token_stride + qh * a.o.head_stride + d;
+    if (a.o_pieces) store<E, 4, true>(to, x);
+    else store<E, 4, false>(to, x);
+}
+
 // A wavefront takes tiles of 64 tokens = 4 blocks: S^T = K Q^T and O^T = V^T P^T on 16 x 16 x 32 matrix instructions, up to 16 heads that share
 // a K/V head.  Row r of the first product's tile t is token 4 t + r % 4 of block r / 4, so that lane 16 g + h holds head h's scores of
 // block g's tokens, which is what the second product wants of it: the 16 tokens of a row of V in a block are the lane's 16-byte load.
@@ -106,13 +119,17 @@ __global__ __launch_bounds__(kDecodeWaves * 64, NJ == 1 ? 4 : NJ == 2 ? 3 : NJ =
         const T *row = (const T *)a.q.data + b * a.q.token_stride + qh * a.q.head_stride;
         float x[2 * NJ][8], most = 0.0f;
 #pragma unroll
-        for (int s = 0; s < 2 * NJ; ++s)
+        for (int s = 0; s < 2 * NJ; ++s) {
+            const int d = 64 * (s / 2) + 16 * g + 8 * (s % 2);
+            const T *from = row + (d < D ? d : 0);
+            if (a.q_pieces) load8<E, true>(from, x[s]);
+            else load8<E, false>(from, x[s]);
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const int d = 64 * (s / 2) + 16 * g + 8 * (s % 2) + e;
-                x[s][e] = d < D && h < heads ? E::get(row[d < D ? d : 0]) : 0.0f;
+                if (d >= D || h >= heads) x[s][e] = 0.0f;
                 most = fmaxf(most, fabsf(x[s][e]));
             }
+        }
         int turn = 0;
         if constexpr (sizeof(T) == 2 && !__is_same(T, _Float16)) {
             most = max_of_rows(most);
@@ -234,52 +251,63 @@ __global__ __launch_bounds__(kDecodeWaves * 64, NJ == 1 ? 4 : NJ == 2 ? 3 : NJ =
             if (16 * t < D) *(f4 *)(mine + 16 * t + 4 * g) = o[t] * (fall * unit);
     }
     __syncthreads();
-    for (int i = threadIdx.x; i < heads * D; i += NW * 64) {
-        const int hh = i / D, d = i - hh * D;
-        float sum = 0.0f, weight = 0.0f, ref = -3.0e38f;
+    // a thread's pieces of 4 elements
+    const int row_pieces = D / 4;
+    for (int i = threadIdx.x; i < heads * row_pieces; i += NW * 64) {
+        const int hh = i / row_pieces, piece = i - hh * row_pieces, qh = q_head0 + hh;
+        f4 sum = (f4)(0.0f);
+        float weight = 0.0f, ref = -3.0e38f;
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            sum += os[w * heads * D + i];
+            sum += *(const f4 *)(os + w * heads * D + 4 * i);
             weight += ls[16 * w + hh];
             ref = fmaxf(ref, ms[16 * w + hh]);
         }
-        const int qh = q_head0 + hh;
         if (a.chunks > 1) {
-            const int64_t at = ((int64_t)b * a.q_heads + qh) * a.chunks + chunk;
-            a.part[at * D + d] = sum;
-            if (d == 0) {
-                float *stats = a.part + (int64_t)a.batch * a.q_heads * a.chunks * D + 2 * at;
-                stats[0] = ref;
-                stats[1] = weight;
-            }
+            f4 *part = a.parts + (((int64_t)b * a.q_heads + qh) * a.chunks + chunk) * (row_pieces + 1);
+            part[1 + piece] = sum;
+            if (piece == 0) part[0] = (f4){ref, weight, 0.0f, 0.0f};
         } else {
-            ((T *)a.o.data)[b * a.o.token_stride + qh * a.o.head_stride + d] = E::put(weight == 0.0f ? 0.0f : sum / weight);
+            put_row<E>(a, b, qh, 4 * piece, sum, weight);
         }
     }
 }
 
-// The chunks of a sequence and query head, joined in their order.  A workgroup per sequence and head.
+// The chunks of a sequence and query head, joined in their order.  A workgroup per sequence and head; groups of head_dim / 4 lanes take the
+// chunks in turn, and the groups' sums are added in their order.
 template <class E>
 __global__ __launch_bounds__(256) void attention_decode_join_kernel(const DecodeArgs a)
 {
-    __shared__ float sums[256 * 4];
-    typedef typename E::T T;
-    const int D = a.cache.head_dim, b = blockIdx.x / a.q_heads, qh = blockIdx.x % a.q_heads;
+    __shared__ f4 sums[256];
+    __shared__ float weights[256 / 4 + 1];
+    const int row_pieces = a.cache.head_dim / 4, groups = min(256 / row_pieces, 16), tid = threadIdx.x;
+    const int b = blockIdx.x / a.q_heads, qh = blockIdx.x % a.q_heads;
     const int length = min(a.lengths[b], a.max_length), chunks = length > 0 ? (length + a.chunk - 1) / a.chunk : 1;
-    const int64_t at = (int64_t)blockIdx.x * a.chunks;
-    const float *part = a.part + at * D, *stats = a.part + (int64_t)a.batch * a.q_heads * a.chunks * D + 2 * at;
+    const f4 *parts = a.parts + (int64_t)blockIdx.x * a.chunks * (row_pieces + 1);
     float top = -3.0e38f;
-    for (int c = 0; c < chunks; ++c) top = fmaxf(top, stats[2 * c]);
-    const int d = threadIdx.x;
-    if (d >= D) return;
-    float sum = 0.0f, weight = 0.0f;
-    for (int c = 0; c < chunks; ++c) {
-        const float fall = __builtin_amdgcn_exp2f(stats[2 * c] - top);
-        sum += part[c * D + d] * fall;
-        weight += stats[2 * c + 1] * fall;
+    for (int c = tid & 63; c < chunks; c += 64) top = fmaxf(top, parts[(int64_t)c * (row_pieces + 1)][0]);
+    top = max_of_rows(max_in_row(top));
+    const int g = tid / row_pieces, piece = tid - g * row_pieces;
+    f4 sum = (f4)(0.0f);
+    float weight = 0.0f;
+    if (g < groups) {
+        for (int c = g; c < chunks; c += groups) {
+            const f4 *part = parts + (int64_t)c * (row_pieces + 1);
+            const f4 stats = part[0];
+            const float fall = __builtin_amdgcn_exp2f(stats[0] - top);
+            weight += stats[1] * fall;
+            sum += part[1 + piece] * fall;
+        }
+        sums[tid] = sum;
+        if (piece == 0) weights[g] = weight;
     }
-    (void)sums;
-    ((T *)a.o.data)[b * a.o.token_stride + qh * a.o.head_stride + d] = E::put(weight == 0.0f ? 0.0f : sum / weight);
+    __syncthreads();
+    if (g > 0) return;
+    for (int x = 1; x < groups; ++x) {
+        sum += sums[x * row_pieces + piece];
+        weight += weights[x];
+    }
+    put_row<E>(a, b, qh, 4 * piece, sum, weight);
 }
 
 }  // namespace ngemm

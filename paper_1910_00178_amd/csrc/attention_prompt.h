@@ -12,10 +12,10 @@ struct PromptArgs {
     uint32_t q_xor;
     int32_t slots;           // tiles of query rows that the grid has room for
     int32_t splits;          // workgroups that may share a tile's keys
-    uint64_t call;
-    uint64_t *flags;         // splits > 1: [slots][kv_heads][splits]
-    f4 *parts;               // as many times kPart
+    f4 *parts;               // splits > 1: [slots][kv_heads][splits] times kPart
 };
+
+constexpr int kLeastRun = 256;                                   // keys of a workgroup where a tile's are split
 
 // DP: head_dim rounded up; NW wavefronts of 32 rows; BN keys per tile.
 template <int DP_, int NW_, int BN_, int PER_CU_>
@@ -64,6 +64,34 @@ __device__ __forceinline__ void copy_to_lds(Buffer from, uint32_t lds_at, uint32
 }
 __device__ __forceinline__ void copies_landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
+// A tile of a sequence's rows, which are its queries times the heads that share a K/V head, heads fastest.
+template <class C>
+struct PromptTile {
+    int b, q_first, queries, row0, rows, k_first, keys, group, causal;
+    int key_tiles, run, parts;                                   // `parts` workgroups take `run` key tiles each
+    bool there;
+
+    __device__ __forceinline__ PromptTile(const PromptArgs &a, int slot)
+    {
+        group = a.q_heads / a.kv_heads;
+        causal = a.causal;
+        // Sequence b has the slots floor(rows before it / BM) + b .. : as many as its rows need or one more.
+        b = last_start(a.batch, slot, [&](int x) { return a.q_offsets[x] * group / C::BM + x; });
+        q_first = min(max(a.q_offsets[b], 0), a.q_tokens);
+        queries = min(max(a.q_offsets[b + 1], q_first), a.q_tokens) - q_first;
+        row0 = (slot - (a.q_offsets[b] * group / C::BM + b)) * C::BM;
+        rows = queries * group;
+        there = row0 >= 0 && row0 < rows;
+        k_first = min(max(a.k_offsets[b], 0), a.k_tokens);
+        keys = min(max(a.k_offsets[b + 1], k_first), a.k_tokens) - k_first;
+        key_tiles = max(0, (last_seen(min(row0 + C::BM, rows) - 1) + C::BN) / C::BN);
+        run = a.splits > 1 ? max((key_tiles + a.splits - 1) / a.splits, kLeastRun / C::BN) : key_tiles;
+        parts = a.splits > 1 ? max(1, (key_tiles + run - 1) / run) : 1;
+    }
+    // the last key that a row sees
+    __device__ __forceinline__ int last_seen(int row) const { return causal ? min(row / group + keys - queries, keys - 1) : keys - 1; }
+};
+
 // Rows of a workgroup: the queries of a sequence times the q_heads / kv_heads heads that share a K/V head, heads fastest.  S^T = K Q^T
 // and O^T = V^T P^T on 32 x 32 x 16 matrix instructions: a lane holds scores of one row (lane % 32), so the softmax needs one exchange of
 // lane halves per tile, and P^T's operand is what the lane holds, rounded, with the keys in the order in which the transposing LDS
@@ -72,7 +100,7 @@ template <class E, class C, bool VEC>
 __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_prompt_kernel(const PromptArgs a)
 {
     extern __shared__ __align__(1024) uint8_t lds[];
-    constexpr int DP = C::DP, NW = C::NW, BN = C::BN, BM = C::BM, CH = C::CH;
+    constexpr int DP = C::DP, NW = C::NW, BN = C::BN, CH = C::CH;
     typedef typename E::T T;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int half = lane >> 5, col = lane & 31;
@@ -80,28 +108,21 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
     const int slot = a.slots - 1 - blockIdx.x / a.kv_heads / a.splits;
     const int group = a.q_heads / a.kv_heads, D = a.head_dim;
 
-    // Sequence b has the slots floor(rows before it / BM) + b .. : as many as its rows need or one more.
-    const int b = last_start(a.batch, slot, [&](int x) { return a.q_offsets[x] * group / BM + x; });
-    const int q_first = min(max(a.q_offsets[b], 0), a.q_tokens), queries = min(max(a.q_offsets[b + 1], q_first), a.q_tokens) - q_first;
-    const int row0 = (slot - (a.q_offsets[b] * group / BM + b)) * BM, rows = queries * group;
-    if (row0 < 0 || row0 >= rows) return;
-    const int k_first = min(max(a.k_offsets[b], 0), a.k_tokens), keys = min(max(a.k_offsets[b + 1], k_first), a.k_tokens) - k_first;
-
-    // the last key that a row sees
-    auto last_seen = [&](int row) { return a.causal ? min(row / group + keys - queries, keys - 1) : keys - 1; };
+    const PromptTile<C> tile_of(a, slot);
+    const int q_first = tile_of.q_first, row0 = tile_of.row0, rows = tile_of.rows;
+    const int k_first = tile_of.k_first, keys = tile_of.keys;
+    if (!tile_of.there) return;
+    auto last_seen = [&](int row) { return tile_of.last_seen(row); };
     const int row = row0 + 32 * wave + col;
     const bool row_there = row < rows;
     const int query = min(row, rows - 1) / group, qhead = head * group + min(row, rows - 1) % group;
     const int seen = last_seen(min(row, rows - 1));
     const int wave_first = min(row0 + 32 * wave, rows - 1), wave_last = min(row0 + 32 * wave + 31, rows - 1);
     const int seen_by_all = last_seen(wave_first), seen_by_any = last_seen(wave_last);
-    const int group_seen_by_all = last_seen(row0), group_seen_by_any = last_seen(min(row0 + BM, rows) - 1);
-    const int all_tiles = max(0, (group_seen_by_any + BN) / BN);
-    // the workgroups of a tile take equal runs of its key tiles, of at least 256 keys
-    const int run = a.splits > 1 ? max((all_tiles + a.splits - 1) / a.splits, 256 / BN) : all_tiles;
-    const int parts = a.splits > 1 ? max(1, (all_tiles + run - 1) / run) : 1;
+    const int group_seen_by_all = last_seen(row0);
+    const int parts = tile_of.parts;
     if (split >= parts) return;
-    const int first_tile = split * run, tiles = min(all_tiles, first_tile + run);
+    const int first_tile = split * tile_of.run, tiles = min(tile_of.key_tiles, first_tile + tile_of.run);
 
     const T *kbase = (const T *)a.k.data + k_first * a.k.token_stride + head * a.k.head_stride;
     const T *vbase = (const T *)a.v.data + k_first * a.v.token_stride + head * a.v.head_stride;
@@ -305,34 +326,13 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
 
     l = sum_of_halves(l);
     if (parts > 1) {
-        const int64_t at = ((int64_t)slot * a.kv_heads + head) * a.splits;
-        f4 *mine = a.parts + (at + split) * C::kPart + tid;
+        f4 *mine = a.parts + (((int64_t)slot * a.kv_heads + head) * a.splits + split) * C::kPart + tid;
 #pragma unroll
         for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                store_part(mine + (4 * t + i) * NW * 64, (f4){o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]});
-        store_part(mine + DP / 8 * NW * 64, (f4){m, l, 0.0f, 0.0f});
-        if (!all_parts_stored(a.flags + at, parts, split, a.call, odd_seen + 2)) return;
-        const f4 *from = a.parts + at * C::kPart + tid;
-        float top = m;
-        for (int p = 0; p < parts; ++p) top = fmaxf(top, load_part(from + p * C::kPart + DP / 8 * NW * 64)[0]);
-        l = 0.0f;
-#pragma unroll
-        for (int t = 0; t < DP / 32; ++t) o[t] = (f16v)(0.0f);
-        for (int p = 0; p < parts; ++p, from += C::kPart) {      // in their order, whoever joins them
-            const f4 stats = load_part(from + DP / 8 * NW * 64);
-            const float fall = __builtin_amdgcn_exp2f((stats[0] - top) * a.scale);
-            l += stats[1] * fall;
-#pragma unroll
-            for (int t = 0; t < DP / 32; ++t)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const f4 x = load_part(from + (4 * t + i) * NW * 64);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[t][4 * i + e] += x[e] * fall;
-                }
-        }
+            for (int i = 0; i < 4; ++i) mine[(4 * t + i) * NW * 64] = (f4){o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
+        mine[DP / 8 * NW * 64] = (f4){m, l, 0.0f, 0.0f};
+        return;
     }
 
     // ---- O = O^T / l: 4 consecutive elements per lane and quarter, exchanged between lane halves to 8 ----
@@ -360,6 +360,35 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
                 }
             }
         }
+}
+
+// The parts of a tile, joined in their order: a workgroup per tile and piece of 4 elements of a lane.
+template <class E, class C, bool VEC>
+__global__ __launch_bounds__(C::NW * 64) void attention_prompt_join_kernel(const PromptArgs a)
+{
+    typedef typename E::T T;
+    constexpr int THREADS = C::NW * 64, PIECES = C::DP / 8;
+    const int piece = blockIdx.x % PIECES, head = blockIdx.x / PIECES % a.kv_heads, slot = blockIdx.x / PIECES / a.kv_heads;
+    const PromptTile<C> tile(a, slot);
+    const int tid = threadIdx.x, lane = tid & 63, row = tile.row0 + 32 * (tid >> 6) + (lane & 31);
+    const int d = 8 * piece + 4 * (lane >> 5);                   // 32 (piece / 4) + 8 (piece % 4) + ..
+    if (!tile.there || tile.parts <= 1 || row >= tile.rows || d >= a.head_dim) return;
+    const f4 *from = a.parts + ((int64_t)slot * a.kv_heads + head) * a.splits * C::kPart + tid;
+    float top = -3.0e38f;
+    for (int p = 0; p < tile.parts; ++p) top = fmaxf(top, from[p * C::kPart + PIECES * THREADS][0]);
+    float l = 0.0f;
+    f4 o = (f4)(0.0f);
+    for (int p = 0; p < tile.parts; ++p) {
+        const f4 stats = from[p * C::kPart + PIECES * THREADS], x = from[p * C::kPart + piece * THREADS];
+        const float fall = __builtin_amdgcn_exp2f((stats[0] - top) * a.scale);
+        l += stats[1] * fall;
+        o += x * fall;
+    }
+    float x[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x[e] = tile.last_seen(row) < 0 ? 0.0f : o[e] / l;
+    T *out = (T *)a.o.data + (tile.q_first + row / tile.group) * a.o.token_stride + (head * tile.group + row % tile.group) * a.o.head_stride;
+    store<E, 4, VEC>(out + d, x);
 }
 
 }  // namespace ngemm

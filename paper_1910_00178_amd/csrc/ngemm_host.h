@@ -3,7 +3,6 @@
 #include "ngemm.h"
 
 #include <hip/hip_runtime.h>
-#include <atomic>
 #include <vector>
 
 struct ngemm_ctx {
@@ -21,7 +20,6 @@ struct ngemm_ctx {
         bool wavek;          // what only the automatic choice launches (gemm_wavek_kernel, gemm_mid_kernel) was faster still
     };
     std::vector<Tuned> tuned;
-    std::atomic<uint64_t> calls{0};   // of the attention entry points, see call_number()
 };
 
 namespace ngemm {
