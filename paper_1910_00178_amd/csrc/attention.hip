@@ -105,37 +105,42 @@ DecodeCut decode_cut(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t h
 {
     constexpr int64_t round = 64 * kDecodeWaves;
     const int64_t group = q_heads / kv_heads, grid = batch * kv_heads * ((group + 15) / 16);
-    int64_t chunk = (max_length * grid / 2048 + round - 1) / round * round;
-    chunk = std::min<int64_t>(std::max<int64_t>(chunk, round), 1024);
+    int64_t chunk = (max_length * grid / 1024 + round - 1) / round * round;
+    chunk = std::min<int64_t>(std::max<int64_t>(chunk, round), 4096);
     DecodeCut cut{chunk, std::max<int64_t>(1, (max_length + chunk - 1) / chunk), 0};
     if (cut.chunks > 1) cut.bytes = (size_t)(batch * q_heads * cut.chunks * (head_dim / 4 + 1) * 16);
     return cut;
 }
 
-template <class E, int NJ>
-void launch_decode_form(const DecodeArgs &a, unsigned grid, size_t lds, hipStream_t st)
+template <class E, int D>
+hipError_t allow_decode_lds()
 {
-    hipLaunchKernelGGL((attention_decode_kernel<E, NJ>), dim3(grid), dim3(kDecodeWaves * 64), lds, st, a);
+    void (*const kernel)(DecodeArgs) = attention_decode_kernel<E, D>;
+    return hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kDecodeWaves * (32 + 16 * D) * 4);
+}
+
+// f(DecodeIndex<head_dim>{})
+template <int D = 256, class F>
+void with_head_dim(int64_t head_dim, F &&f)
+{
+    if (head_dim == D) f(DecodeIndex<D>{});
+    else if constexpr (D > 16) with_head_dim<D - 16>(head_dim, f);
+}
+
+template <class E, int D>
+void launch_decode_form(const DecodeArgs &a, hipStream_t st)
+{
+    const int group = a.q_heads / a.cache.kv_heads;
+    const unsigned grid = (unsigned)((int64_t)a.batch * a.cache.kv_heads * ((group + 15) / 16) * a.chunks);
+    const size_t lds = (size_t)kDecodeWaves * (32 + std::min(group, 16) * D) * 4;
+    hipLaunchKernelGGL((attention_decode_kernel<E, D>), dim3(grid), dim3(kDecodeWaves * 64), lds, st, a);
+    if (a.chunks > 1) hipLaunchKernelGGL((attention_decode_join_kernel<E, D>), dim3((unsigned)(a.batch * a.q_heads)), dim3(kJoinThreads), 0, st, a);
 }
 
 template <class E>
 void launch_decode(const DecodeArgs &a, hipStream_t st)
 {
-    const int group = a.q_heads / a.cache.kv_heads, D = a.cache.head_dim;
-    const unsigned grid = (unsigned)((int64_t)a.batch * a.cache.kv_heads * ((group + 15) / 16) * a.chunks);
-    const size_t lds = (size_t)kDecodeWaves * (32 + std::min(group, 16) * D) * 4;
-    if (D <= 64) launch_decode_form<E, 1>(a, grid, lds, st);
-    else if (D <= 128) launch_decode_form<E, 2>(a, grid, lds, st);
-    else if (D <= 192) launch_decode_form<E, 3>(a, grid, lds, st);
-    else launch_decode_form<E, 4>(a, grid, lds, st);
-    if (a.chunks > 1) hipLaunchKernelGGL(attention_decode_join_kernel<E>, dim3((unsigned)(a.batch * a.q_heads)), dim3(256), 0, st, a);
-}
-
-template <class E, int NJ>
-bool allow_decode_lds()
-{
-    void (*const kernel)(DecodeArgs) = attention_decode_kernel<E, NJ>;
-    return hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kDecodeWaves * (32 + 16 * 64 * NJ) * 4) == hipSuccess;
+    with_head_dim(a.cache.head_dim, [&](auto dim) { launch_decode_form<E, decltype(dim)::value>(a, st); });
 }
 
 // ---- prompts ----
@@ -209,7 +214,12 @@ void launch_prompt(const PromptArgs &a, bool vec, void *workspace, hipStream_t s
 
 bool ngemm::attention_setup()
 {
-    bool ok = allow_decode_lds<F16, 3>() && allow_decode_lds<F16, 4>() && allow_decode_lds<BF16, 3>() && allow_decode_lds<BF16, 4>();
+    bool ok = true;
+    for (int64_t d = 16; d <= 256; d += 16)
+        with_head_dim(d, [&](auto dim) {
+            constexpr int D = decltype(dim)::value;
+            ok = ok && allow_decode_lds<F16, D>() == hipSuccess && allow_decode_lds<BF16, D>() == hipSuccess;
+        });
     for (int64_t d : {64, 96, 128, 192, 256})
         with_prompt_form(d, [&](auto form) { ok = ok && allow_prompt_form<decltype(form)>(); });
     return ok;

@@ -16,6 +16,7 @@ struct DecodeArgs {
 };
 
 constexpr int kDecodeWaves = 4;
+constexpr int decode_waves_per_simd(int D) { return D <= 64 ? 4 : D <= 128 ? 2 : D <= 192 ? 2 : 1; }
 
 // 16 codes as 16-bit floats, in order.  A code with its sign bit turned, as the low byte under 0x64, is the float 1024 + 128 + code.
 __device__ __forceinline__ void codes_to_f16(u4 x, u4 (&out)[2])
@@ -76,16 +77,16 @@ __device__ __forceinline__ void put_row(const DecodeArgs &a, int b, int qh, int 
 // A wavefront takes tiles of 64 tokens = 4 blocks: S^T = K Q^T and O^T = V^T P^T on 16 x 16 x 32 matrix instructions, up to 16 heads that share
 // a K/V head.  Row r of the first product's tile t is token 4 t + r % 4 of block r / 4, so that lane 16 g + h holds head h's scores of
 // block g's tokens, which is what the second product wants of it: the 16 tokens of a row of V in a block are the lane's 16-byte load.
-// NJ: head_dim / 64, rounded up.
-template <class E, int NJ>
-__global__ __launch_bounds__(kDecodeWaves * 64, NJ == 1 ? 4 : NJ == 2 ? 3 : NJ == 3 ? 2 : 1) void attention_decode_kernel(const DecodeArgs a)
+// D: head_dim, known to the compiler so that the loads of a tile are one run without branches.
+template <class E, int D>
+__global__ __launch_bounds__(kDecodeWaves * 64, decode_waves_per_simd(D)) void attention_decode_kernel(const DecodeArgs a)
 {
     extern __shared__ __align__(16) float shared[];
-    constexpr int NW = kDecodeWaves;
+    constexpr int NW = kDecodeWaves, NJ = (D + 63) / 64, DT = D / 16;
     typedef typename E::T T;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = lane & 15, g = lane >> 4;
-    const int kv_heads = a.cache.kv_heads, D = a.cache.head_dim, group = a.q_heads / kv_heads, head_tiles = (group + 15) / 16;
+    const int kv_heads = a.cache.kv_heads, group = a.q_heads / kv_heads, head_tiles = (group + 15) / 16;
     int id = blockIdx.x;
     const int head_tile = id % head_tiles;
     id /= head_tiles;
@@ -99,7 +100,8 @@ __global__ __launch_bounds__(kDecodeWaves * 64, NJ == 1 ? 4 : NJ == 2 ? 3 : NJ =
     if (first >= end && chunk > 0) return;               // (an empty sequence's first workgroup writes its zeros)
 
     // the wavefront's blocks, 16 tiles ahead: lane l looks up block l % 4 of its tile l / 4
-    const int blocks_per_page = a.cache.page_blocks, block_bytes = a.cache.block_bytes();
+    constexpr int block_bytes = 32 * D + 128;
+    const int blocks_per_page = a.cache.page_blocks;
     auto look_up = [&](int tile) {
         const int index = (first + 64 * (tile + NW * (lane >> 2))) / 16 + (lane & 3);
         const int page = index / blocks_per_page;
@@ -143,36 +145,44 @@ __global__ __launch_bounds__(kDecodeWaves * 64, NJ == 1 ? 4 : NJ == 2 ? 3 : NJ =
                 q[s][e / 2] = pack2<F16>(__builtin_amdgcn_ldexpf(x[s][e], turn), __builtin_amdgcn_ldexpf(x[s][e + 1], turn));
     }
 
-    f4 o[4 * NJ];
+    f4 o[DT];
 #pragma unroll
-    for (int t = 0; t < 4 * NJ; ++t) o[t] = (f4)(0.0f);
+    for (int t = 0; t < DT; ++t) o[t] = (f4)(0.0f);
     float m = -3.0e38f, l = 0.0f;                        // the row's reference and this lane's part of the sum of its weights
     float unit = 0x1p-120f, per_unit = 0x1p120f;         // V's scales enter relative to a power of two, 2^6 at most
 
     const int tiles = end > first ? (end - first + 63) / 64 : 0;
     int places = tiles > wave ? look_up(wave) : -1;
-    for (int tile = wave, n = 0; tile < tiles; tile += NW, ++n) {
-        if (n == 16) {
-            places = look_up(tile);
-            n = 0;
-        }
-        // ---- loads ----
-        const int k_place = __shfl(places, 4 * n + (h >> 2)), v_place = __shfl(places, 4 * n + g);
+    // K of the next tile is on its way while this one's scores and values are worked on, V while the next one's scores are
+    u4 k[4][NJ], v[DT];
+    float ks = 0.0f, vs = 0.0f;
+    int v_place = -1;
+    const uint8_t *vb = a.cache.data;
+    auto load_keys = [&](int n) {
+        const int k_place = __shfl(places, 4 * n + (h >> 2));
+        v_place = __shfl(places, 4 * n + g);
         const uint8_t *kb = a.cache.data + (int64_t)max(k_place, 0) * block_bytes + (h & 3) * D;
-        const uint8_t *vb = a.cache.data + (int64_t)max(v_place, 0) * block_bytes;
-        u4 k[4][NJ], v[4 * NJ];
+        vb = a.cache.data + (int64_t)max(v_place, 0) * block_bytes + 16 * D;
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int j = 0; j < NJ; ++j) k[t][j] = *(const u4 *)(kb + 4 * t * D + min(64 * j + 16 * g, D - 16));
-        float ks = *(const float *)(vb + 32 * D + 4 * h), vs = *(const float *)(vb + 32 * D + 64 + 4 * h);
+        ks = *(const float *)(vb + 16 * D + 4 * h);
+        vs = *(const float *)(vb + 16 * D + 64 + 4 * h);
+    };
+    auto load_values = [&]() {
 #pragma unroll
-        for (int t = 0; t < 4 * NJ; ++t)
-            if (16 * t < D) v[t] = *(const u4 *)(vb + 16 * D + (16 * t + h) * 16);
-
+        for (int t = 0; t < DT; ++t) v[t] = *(const u4 *)(vb + (16 * t + h) * 16);
+    };
+    if (wave < tiles) {
+        load_keys(0);
+        load_values();
+    }
+    for (int tile = wave, n = 0; tile < tiles; tile += NW) {
         // ---- scores ----
         const int there = v_place < 0 ? 0 : end - (first + 64 * tile + 16 * g);     // tokens of block g that count
-        if (h >= there) ks = vs = 0.0f;
+        const float ks_now = h < there ? ks : 0.0f;
+        float vs_now = h < there ? vs : 0.0f;
         f4 s[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -185,9 +195,17 @@ __global__ __launch_bounds__(kDecodeWaves * 64, NJ == 1 ? 4 : NJ == 2 ? 3 : NJ =
                 s[t] = mfma16(x[1], q[2 * j + 1], s[t]);
             }
         }
+        const bool more = tile + NW < tiles;
+        if (more) {
+            if (++n == 16) {
+                places = look_up(tile + NW);
+                n = 0;
+            }
+            load_keys(n);
+        }
         unrolled<16>([&](auto i) {
             constexpr int I = decltype(i)::value;
-            s[I / 4][I % 4] = s[I / 4][I % 4] * of_row<I>(ks) * scale;
+            s[I / 4][I % 4] = s[I / 4][I % 4] * of_row<I>(ks_now) * scale;
         });
         if (!__all(there >= 16)) {
 #pragma unroll
@@ -202,36 +220,36 @@ __global__ __launch_bounds__(kDecodeWaves * 64, NJ == 1 ? 4 : NJ == 2 ? 3 : NJ =
             const float fall = __builtin_amdgcn_exp2f(m - most);
             l *= fall;
 #pragma unroll
-            for (int t = 0; t < 4 * NJ; ++t) o[t] *= fall;
+            for (int t = 0; t < DT; ++t) o[t] *= fall;
             m = most;
         }
-        if (__any(vs > 64.0f * unit)) {
-            float top = vs;
+        if (__any(vs_now > 64.0f * unit)) {
+            float top = vs_now;
             for (int x = 32; x; x /= 2) top = fmaxf(top, __shfl_xor(top, x));
             const int e = __builtin_amdgcn_frexp_expf(top);
             const float now = __builtin_amdgcn_ldexpf(1.0f, e), fall = unit * __builtin_amdgcn_ldexpf(1.0f, -e);
 #pragma unroll
-            for (int t = 0; t < 4 * NJ; ++t) o[t] *= fall;
+            for (int t = 0; t < DT; ++t) o[t] *= fall;
             unit = now;
             per_unit = __builtin_amdgcn_ldexpf(1.0f, -e);
         }
-        vs *= per_unit;
+        vs_now *= per_unit;
         u4 p[2];
         unrolled<8>([&](auto i) {
             constexpr int I = 2 * decltype(i)::value;
             const float x = __builtin_amdgcn_exp2f(s[I / 4][I % 4] - m), y = __builtin_amdgcn_exp2f(s[I / 4][I % 4 + 1] - m);
             l += x + y;
-            p[I / 8][I % 8 / 2] = pack2<F16>(x * of_row<I>(vs), y * of_row<I + 1>(vs));
+            p[I / 8][I % 8 / 2] = pack2<F16>(x * of_row<I>(vs_now), y * of_row<I + 1>(vs_now));
         });
         // ---- values ----
 #pragma unroll
-        for (int t = 0; t < 4 * NJ; ++t)
-            if (16 * t < D) {
-                u4 x[2];
-                codes_to_f16(v[t], x);
-                o[t] = mfma16(x[0], p[0], o[t]);
-                o[t] = mfma16(x[1], p[1], o[t]);
-            }
+        for (int t = 0; t < DT; ++t) {
+            u4 x[2];
+            codes_to_f16(v[t], x);
+            o[t] = mfma16(x[0], p[0], o[t]);
+            o[t] = mfma16(x[1], p[1], o[t]);
+        }
+        if (more) load_values();
     }
 
     // ---- the wavefronts' parts, joined in their order ----
@@ -247,8 +265,8 @@ __global__ __launch_bounds__(kDecodeWaves * 64, NJ == 1 ? 4 : NJ == 2 ? 3 : NJ =
     if (h < heads) {
         float *mine = os + (wave * heads + h) * D;
 #pragma unroll
-        for (int t = 0; t < 4 * NJ; ++t)
-            if (16 * t < D) *(f4 *)(mine + 16 * t + 4 * g) = o[t] * (fall * unit);
+        for (int t = 0; t < DT; ++t)
+            *(f4 *)(mine + 16 * t + 4 * g) = o[t] * (fall * unit);
     }
     __syncthreads();
     // a thread's pieces of 4 elements
@@ -273,38 +291,49 @@ __global__ __launch_bounds__(kDecodeWaves * 64, NJ == 1 ? 4 : NJ == 2 ? 3 : NJ =
     }
 }
 
-// The chunks of a sequence and query head, joined in their order.  A workgroup per sequence and head; groups of head_dim / 4 lanes take the
-// chunks in turn, and the groups' sums are added in their order.
-template <class E>
-__global__ __launch_bounds__(256) void attention_decode_join_kernel(const DecodeArgs a)
+// The chunks of a sequence and query head, joined in an order that depends on nothing but their number.  A workgroup per sequence and
+// head; groups of head_dim / 4 lanes take the chunks in turn, four at a time, and the groups' sums are added in their order.
+constexpr int kJoinThreads = 512;
+
+template <class E, int D>
+__global__ __launch_bounds__(kJoinThreads) void attention_decode_join_kernel(const DecodeArgs a)
 {
-    __shared__ f4 sums[256];
-    __shared__ float weights[256 / 4 + 1];
-    const int row_pieces = a.cache.head_dim / 4, groups = min(256 / row_pieces, 16), tid = threadIdx.x;
-    const int b = blockIdx.x / a.q_heads, qh = blockIdx.x % a.q_heads;
+    constexpr int PIECES = D / 4, GROUPS = kJoinThreads / PIECES < 32 ? kJoinThreads / PIECES : 32;
+    __shared__ f4 sums[GROUPS * PIECES];
+    __shared__ float weights[GROUPS];
+    const int tid = threadIdx.x, b = blockIdx.x / a.q_heads, qh = blockIdx.x % a.q_heads;
+    const f4 *parts = a.parts + (int64_t)blockIdx.x * a.chunks * (PIECES + 1);
     const int length = min(a.lengths[b], a.max_length), chunks = length > 0 ? (length + a.chunk - 1) / a.chunk : 1;
-    const f4 *parts = a.parts + (int64_t)blockIdx.x * a.chunks * (row_pieces + 1);
     float top = -3.0e38f;
-    for (int c = tid & 63; c < chunks; c += 64) top = fmaxf(top, parts[(int64_t)c * (row_pieces + 1)][0]);
+    for (int c = tid & 63; c < chunks; c += 64) top = fmaxf(top, parts[(int64_t)c * (PIECES + 1)][0]);
     top = max_of_rows(max_in_row(top));
-    const int g = tid / row_pieces, piece = tid - g * row_pieces;
+    const int g = tid / PIECES, piece = tid % PIECES;
     f4 sum = (f4)(0.0f);
     float weight = 0.0f;
-    if (g < groups) {
-        for (int c = g; c < chunks; c += groups) {
-            const f4 *part = parts + (int64_t)c * (row_pieces + 1);
-            const f4 stats = part[0];
-            const float fall = __builtin_amdgcn_exp2f(stats[0] - top);
-            weight += stats[1] * fall;
-            sum += part[1 + piece] * fall;
+    if (g < GROUPS) {
+        for (int c = g; c < chunks; c += 4 * GROUPS) {
+            f4 stats[4], x[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const f4 *part = parts + (int64_t)min(c + u * GROUPS, chunks - 1) * (PIECES + 1);
+                stats[u] = part[0];
+                x[u] = part[1 + piece];
+            }
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                if (c + u * GROUPS >= chunks) break;
+                const float fall = __builtin_amdgcn_exp2f(stats[u][0] - top);
+                weight += stats[u][1] * fall;
+                sum += x[u] * fall;
+            }
         }
         sums[tid] = sum;
         if (piece == 0) weights[g] = weight;
     }
     __syncthreads();
     if (g > 0) return;
-    for (int x = 1; x < groups; ++x) {
-        sum += sums[x * row_pieces + piece];
+    for (int x = 1; x < min(GROUPS, chunks); ++x) {
+        sum += sums[x * PIECES + piece];
         weight += weights[x];
     }
     put_row<E>(a, b, qh, 4 * piece, sum, weight);
