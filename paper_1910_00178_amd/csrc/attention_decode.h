@@ -106,44 +106,12 @@ __global__ __launch_bounds__(kDecodeWaves * 64, decode_waves_per_simd(D)) void a
         const int index = (first + 64 * (tile + NW * (lane >> 2))) / 16 + (lane & 3);
         const int page = index / blocks_per_page;
         int where = -1;
-        if (16 * index < end && page < a.cache.pages_stride) {
+        if (page < a.cache.pages_stride) {               // (past the sequence's end: looked at, but masked)
             const int id = a.cache.pages[b * a.cache.pages_stride + page];
             if (id >= 0 && id < a.cache.num_pages) where = (id * kv_heads + head) * blocks_per_page + (index - page * blocks_per_page);
         }
         return where;
     };
-
-    // Q as f16, relative to a power of two for a bf16 row: its 8 bits are exact there
-    u4 q[2 * NJ];
-    float scale = a.scale;
-    {
-        const int qh = q_head0 + min(h, heads - 1);
-        const T *row = (const T *)a.q.data + b * a.q.token_stride + qh * a.q.head_stride;
-        float x[2 * NJ][8], most = 0.0f;
-#pragma unroll
-        for (int s = 0; s < 2 * NJ; ++s) {
-            const int d = 64 * (s / 2) + 16 * g + 8 * (s % 2);
-            const T *from = row + (d < D ? d : 0);
-            if (a.q_pieces) load8<E, true>(from, x[s]);
-            else load8<E, false>(from, x[s]);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                if (d >= D || h >= heads) x[s][e] = 0.0f;
-                most = fmaxf(most, fabsf(x[s][e]));
-            }
-        }
-        int turn = 0;
-        if constexpr (sizeof(T) == 2 && !__is_same(T, _Float16)) {
-            most = max_of_rows(most);
-            if (most > 0.0f && most < __builtin_inff()) turn = 15 - __builtin_amdgcn_frexp_expf(most);
-            scale = __builtin_amdgcn_ldexpf(scale, -turn);
-        }
-#pragma unroll
-        for (int s = 0; s < 2 * NJ; ++s)
-#pragma unroll
-            for (int e = 0; e < 8; e += 2)
-                q[s][e / 2] = pack2<F16>(__builtin_amdgcn_ldexpf(x[s][e], turn), __builtin_amdgcn_ldexpf(x[s][e + 1], turn));
-    }
 
     f4 o[DT];
 #pragma unroll
@@ -153,6 +121,22 @@ __global__ __launch_bounds__(kDecodeWaves * 64, decode_waves_per_simd(D)) void a
 
     const int tiles = end > first ? (end - first + 63) / 64 : 0;
     int places = tiles > wave ? look_up(wave) : -1;
+    // the rows of Q, on their way before the cache's
+    typename E::T x[2 * NJ][8];
+    {
+        const int qh = q_head0 + min(h, heads - 1);
+        const T *row = (const T *)a.q.data + b * a.q.token_stride + qh * a.q.head_stride;
+#pragma unroll
+        for (int s = 0; s < 2 * NJ; ++s) {
+            const int d = 64 * (s / 2) + 16 * g + 8 * (s % 2);
+            const T *from = row + (d < D ? d : 0);
+            if (a.q_pieces) __builtin_memcpy(x[s], __builtin_assume_aligned(from, 16), 16);
+            else
+#pragma unroll
+                for (int e = 0; e < 8; ++e) x[s][e] = from[e];
+        }
+    }
+    __builtin_amdgcn_sched_barrier(0);
     // K of the next tile is on its way while this one's scores and values are worked on, V while the next one's scores are
     u4 k[4][NJ], v[DT];
     float ks = 0.0f, vs = 0.0f;
@@ -177,6 +161,37 @@ __global__ __launch_bounds__(kDecodeWaves * 64, decode_waves_per_simd(D)) void a
     if (wave < tiles) {
         load_keys(0);
         load_values();
+    }
+    __builtin_amdgcn_sched_barrier(0);
+
+    // Q as f16, relative to a power of two for a bf16 row: its 8 bits are exact there
+    u4 q[2 * NJ];
+    float scale = a.scale;
+    {
+        int turn = 0;
+#pragma unroll
+        for (int s = 0; s < 2 * NJ; ++s)
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (64 * (s / 2) + 16 * g + 8 * (s % 2) >= D || h >= heads) x[s][e] = (T)0.0f;
+        if constexpr (!__is_same(T, _Float16)) {
+            float most = 0.0f;
+#pragma unroll
+            for (int s = 0; s < 2 * NJ; ++s)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(E::get(x[s][e])));
+            most = max_of_rows(most);
+            if (most > 0.0f && most < __builtin_inff()) turn = 15 - __builtin_amdgcn_frexp_expf(most);
+            scale = __builtin_amdgcn_ldexpf(scale, -turn);
+#pragma unroll
+            for (int s = 0; s < 2 * NJ; ++s)
+#pragma unroll
+                for (int e = 0; e < 8; e += 2)
+                    q[s][e / 2] = pack2<F16>(__builtin_amdgcn_ldexpf(E::get(x[s][e]), turn), __builtin_amdgcn_ldexpf(E::get(x[s][e + 1]), turn));
+        } else {
+#pragma unroll
+            for (int s = 0; s < 2 * NJ; ++s) __builtin_memcpy(&q[s], x[s], 16);
+        }
     }
     for (int tile = wave, n = 0; tile < tiles; tile += NW) {
         // ---- scores ----
@@ -224,8 +239,7 @@ __global__ __launch_bounds__(kDecodeWaves * 64, decode_waves_per_simd(D)) void a
             m = most;
         }
         if (__any(vs_now > 64.0f * unit)) {
-            float top = vs_now;
-            for (int x = 32; x; x /= 2) top = fmaxf(top, __shfl_xor(top, x));
+            const float top = max_of_rows(max_in_row(vs_now));
             const int e = __builtin_amdgcn_frexp_expf(top);
             const float now = __builtin_amdgcn_ldexpf(1.0f, e), fall = unit * __builtin_amdgcn_ldexpf(1.0f, -e);
 #pragma unroll
