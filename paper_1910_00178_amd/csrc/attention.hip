@@ -149,11 +149,11 @@ void launch_decode(const DecodeArgs &a, hipStream_t st)
 template <class F>
 void with_prompt_form(int64_t head_dim, F &&f)
 {
-    if (head_dim <= 64) f(PromptCfg<64, 4, 64, 2>{});
-    else if (head_dim <= 96) f(PromptCfg<96, 4, 64, 2>{});
-    else if (head_dim <= 128) f(PromptCfg<128, 4, 64, 2>{});
-    else if (head_dim <= 192) f(PromptCfg<192, 4, 64, 1>{});
-    else f(PromptCfg<256, 4, 32, 1>{});
+    if (head_dim <= 64) f(PromptCfg<64, 4, 1, 64, 2>{});
+    else if (head_dim <= 96) f(PromptCfg<96, 4, 1, 64, 2>{});
+    else if (head_dim <= 128) f(PromptCfg<128, 4, 1, 64, 2>{});
+    else if (head_dim <= 192) f(PromptCfg<192, 4, 2, 64, 1>{});
+    else f(PromptCfg<256, 4, 2, 64, 1>{});
 }
 
 template <class E, class C, bool VEC>
@@ -199,9 +199,9 @@ void launch_prompt_form(PromptArgs a, bool vec, void *workspace, hipStream_t st)
     if (vec) hipLaunchKernelGGL((attention_prompt_kernel<E, C, true>), grid, block, C::kLds, st, a);
     else hipLaunchKernelGGL((attention_prompt_kernel<E, C, false>), grid, block, C::kLds, st, a);
     if (cut.splits == 1) return;
-    const dim3 pieces((unsigned)(cut.slots * a.kv_heads * (C::DP / 8)));
-    if (vec) hipLaunchKernelGGL((attention_prompt_join_kernel<E, C, true>), pieces, block, 0, st, a);
-    else hipLaunchKernelGGL((attention_prompt_join_kernel<E, C, false>), pieces, block, 0, st, a);
+    const dim3 pieces((unsigned)(cut.slots * a.kv_heads * (C::DP / 8))), threads(C::BM * 2);
+    if (vec) hipLaunchKernelGGL((attention_prompt_join_kernel<E, C, true>), pieces, threads, 0, st, a);
+    else hipLaunchKernelGGL((attention_prompt_join_kernel<E, C, false>), pieces, threads, 0, st, a);
 }
 
 template <class E>

@@ -46,4 +46,16 @@ __device__ __forceinline__ float sum_of_halves(float x)
     return __uint_as_float(s[0]) + __uint_as_float(s[1]);
 }
 
+// Over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
+__device__ __forceinline__ float max_of_rows(float x)
+{
+    const u2 s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return max_of_halves(fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1])));
+}
+__device__ __forceinline__ float sum_of_rows(float x)
+{
+    const u2 s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return sum_of_halves(__uint_as_float(s[0]) + __uint_as_float(s[1]));
+}
+
 }  // namespace ngemm

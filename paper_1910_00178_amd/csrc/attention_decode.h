@@ -39,18 +39,6 @@ __device__ __forceinline__ float of_row(float x)
     return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x150 + K, 0xf, 0xf, true));
 }
 
-// Over the four lanes l, l ^ 16, l ^ 32, l ^ 48.
-__device__ __forceinline__ float max_of_rows(float x)
-{
-    const u2 s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return max_of_halves(fmaxf(__uint_as_float(s[0]), __uint_as_float(s[1])));
-}
-__device__ __forceinline__ float sum_of_rows(float x)
-{
-    const u2 s = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return sum_of_halves(__uint_as_float(s[0]) + __uint_as_float(s[1]));
-}
-
 // f(IntC<0>) .. f(IntC<N - 1>)
 template <int I> struct DecodeIndex { static constexpr int value = I; };
 template <int N, int I = 0, class F>

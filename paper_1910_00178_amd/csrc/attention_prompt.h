@@ -17,15 +17,21 @@ struct PromptArgs {
 
 constexpr int kLeastRun = 256;                                   // keys of a workgroup where a tile's are split
 
-// DP: head_dim rounded up; NW wavefronts of 32 rows; BN keys per tile.
-template <int DP_, int NW_, int BN_, int PER_CU_>
+// DP: head_dim rounded up; RW groups of 32 rows, each of KS wavefronts that share out the BN keys of a tile; PER_CU workgroups to a unit.
+template <int DP_, int RW_, int KS_, int BN_, int PER_CU_>
 struct PromptCfg {
-    static constexpr int DP = DP_, NW = NW_, BN = BN_, PER_CU = PER_CU_;
-    static constexpr int BM = 32 * NW, CH = DP / 8;              // CH: 16-byte chunks of a row
-    static constexpr int kTile = BN * DP * 2, kStage = 2 * kTile, kLds = 2 * kStage + 16;
+    static constexpr int DP = DP_, RW = RW_, KS = KS_, BN = BN_, PER_CU = PER_CU_;
+    static constexpr int NW = RW * KS, BM = 32 * RW, KT = BN / 32 / KS;       // KT: 32-key blocks of a wavefront
+    static constexpr int CH = DP / 8;              // CH: 16-byte chunks of a row
+    static constexpr int kTile = BN * DP * 2, kStage = 2 * kTile, kFlags = 2 * kStage;
     static constexpr int LOADS = kTile / 1024 / NW;              // 1 KiB copies of K (and of V) per wavefront
-    static constexpr int kPart = NW * 64 * (DP / 8 + 1);         // 16-byte pieces of a part: sums, maximum and weight
-    static_assert(kTile % (1024 * NW) == 0, "whole copies");
+    static constexpr int AHEAD = DP == 96 ? 6 : DP == 64 || DP == 192 ? 4 : DP == 256 ? 2 : 8, V_AHEAD = DP == 96 ? 3 : DP == 64 || DP == 256 ? 2 : 4;     // operands read together
+    static_assert(KT * (DP / 16) % AHEAD == 0 && 2 * KT * (DP / 32) % V_AHEAD == 0, "whole groups");
+    static constexpr int kPart = BM * 2 * (DP / 8 + 1);          // 16-byte pieces of a part: sums, maximum and weight
+    static constexpr int kMerge = (KS - 1) * kPart * 16;
+    static constexpr int kLds = (kFlags > kMerge ? kFlags : kMerge) + 16;
+    static_assert(kLds >= NW * (DP + 64) * 4, "rows one by one");
+    static_assert(kTile % (1024 * NW) == 0 && KT * 32 * KS == BN, "whole copies and blocks");
     // Where chunk c of key j lies: so that 16 consecutive keys' equal chunks of K, and the 64 bytes of four consecutive keys of V,
     // fall on different banks (64 banks of 4 bytes).
     static __device__ __forceinline__ int k_swizzle(int j)
@@ -60,7 +66,7 @@ __device__ __forceinline__ Buffer buffer_of(const void *from, int bytes)
 __device__ __forceinline__ void copy_to_lds(Buffer from, uint32_t lds_at, uint32_t offset)
 {
     // (five wait states: what a vector instruction that wrote the descriptor's registers needs; M0 needs one)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds_at), "v"(offset), "s"(from) : "memory");
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane((int)lds_at)), "v"(offset), "s"(from) : "memory");
 }
 __device__ __forceinline__ void copies_landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
@@ -92,6 +98,61 @@ struct PromptTile {
     __device__ __forceinline__ int last_seen(int row) const { return causal ? min(row / group + keys - queries, keys - 1) : keys - 1; }
 };
 
+// The rows of a tile element by element: what a workgroup does whose keys hold an infinity or a NaN that not all of its rows see (0 times
+// it would reach the others in the matrix instructions).
+template <class E, class C>
+__device__ __forceinline__ void prompt_rows_one_by_one(const PromptArgs &a, const PromptTile<C> &tile, int head, int first_key, int end_key, f4 *part,
+                                                                 uint8_t *lds)
+{
+    typedef typename E::T T;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, D = a.head_dim;
+    float *q = (float *)lds + wave * (C::DP + 64), *p = q + C::DP;
+    const T *kr = (const T *)a.k.data + tile.k_first * a.k.token_stride + head * a.k.head_stride;
+    const T *vr = (const T *)a.v.data + tile.k_first * a.v.token_stride + head * a.v.head_stride;
+    for (int r = wave; r < C::BM; r += C::NW) {
+        const int row = min(tile.row0 + r, tile.rows - 1), token = tile.q_first + row / tile.group, qhead = head * tile.group + row % tile.group;
+        const T *qr = (const T *)a.q.data + token * a.q.token_stride + qhead * a.q.head_stride;
+        for (int d = lane; d < D; d += 64) q[d] = a.q_xor ? -E::get(qr[d]) : E::get(qr[d]);
+        const int end = min(end_key, tile.last_seen(row) + 1);
+        float m = -3.0e38f / fmaxf(a.scale, 1.0f), l = 0.0f, o[(C::DP + 63) / 64] = {};
+        __builtin_amdgcn_wave_barrier();
+        for (int t0 = first_key; t0 < end; t0 += 64) {
+            const int t = t0 + lane;
+            float s = -__builtin_inff();
+            if (t < end) {
+                s = 0.0f;
+                for (int d = 0; d < D; ++d) s += q[d] * E::get(kr[t * a.k.token_stride + d]);
+            }
+            const float most = fmaxf(max_of_rows(max_in_row(s)), m), fall = __builtin_amdgcn_exp2f((m - most) * a.scale);
+            const float w = t < end ? __builtin_amdgcn_exp2f((s - most) * a.scale) : 0.0f;
+            float sum = w;
+            for (int x = 32; x; x /= 2) sum += __shfl_xor(sum, x);
+            l = l * fall + sum;
+            m = most;
+            __builtin_amdgcn_wave_barrier();
+            p[lane] = w;
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int n = 0; n < (C::DP + 63) / 64; ++n) {
+                const int d = lane + 64 * n;
+                o[n] *= fall;
+                if (d < D)
+                    for (int j = 0; j < 64 && t0 + j < end; ++j) o[n] += p[j] * E::get(vr[(t0 + j) * a.v.token_stride + d]);
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+        const int place = r / 32 * 64 + r % 32;              // of the row's lower lane in a part
+#pragma unroll
+        for (int n = 0; n < (C::DP + 63) / 64; ++n) {
+            const int d = lane + 64 * n;
+            if (d >= D || tile.row0 + r >= tile.rows) continue;
+            if (part) ((float *)(part + d / 8 * C::BM * 2 + place + (d / 4 & 1) * 32))[d % 4] = o[n];
+            else ((T *)a.o.data)[token * a.o.token_stride + qhead * a.o.head_stride + d] = E::put(tile.last_seen(row) < 0 ? 0.0f : o[n] / l);
+        }
+        if (part && lane < 2) part[C::DP / 8 * C::BM * 2 + place + 32 * lane] = (f4){m, l, 0.0f, 0.0f};
+    }
+}
+
 // Rows of a workgroup: the queries of a sequence times the q_heads / kv_heads heads that share a K/V head, heads fastest.  S^T = K Q^T
 // and O^T = V^T P^T on 32 x 32 x 16 matrix instructions: a lane holds scores of one row (lane % 32), so the softmax needs one exchange of
 // lane halves per tile, and P^T's operand is what the lane holds, rounded, with the keys in the order in which the transposing LDS
@@ -100,10 +161,10 @@ template <class E, class C, bool VEC>
 __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_prompt_kernel(const PromptArgs a)
 {
     extern __shared__ __align__(1024) uint8_t lds[];
-    constexpr int DP = C::DP, NW = C::NW, BN = C::BN, CH = C::CH;
+    constexpr int DP = C::DP, NW = C::NW, BN = C::BN, CH = C::CH, KT = C::KT;
     typedef typename E::T T;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int half = lane >> 5, col = lane & 31;
+    const int half = lane >> 5, col = lane & 31, row_group = wave % C::RW, key0 = 32 * KT * (wave / C::RW);   // key0: its first of a tile
     const int head = blockIdx.x % a.kv_heads, split = blockIdx.x / a.kv_heads % a.splits;
     const int slot = a.slots - 1 - blockIdx.x / a.kv_heads / a.splits;
     const int group = a.q_heads / a.kv_heads, D = a.head_dim;
@@ -113,11 +174,11 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
     const int k_first = tile_of.k_first, keys = tile_of.keys;
     if (!tile_of.there) return;
     auto last_seen = [&](int row) { return tile_of.last_seen(row); };
-    const int row = row0 + 32 * wave + col;
+    const int row = row0 + 32 * row_group + col;
     const bool row_there = row < rows;
     const int query = min(row, rows - 1) / group, qhead = head * group + min(row, rows - 1) % group;
     const int seen = last_seen(min(row, rows - 1));
-    const int wave_first = min(row0 + 32 * wave, rows - 1), wave_last = min(row0 + 32 * wave + 31, rows - 1);
+    const int wave_first = min(row0 + 32 * row_group, rows - 1), wave_last = min(row0 + 32 * row_group + 31, rows - 1);
     const int seen_by_all = last_seen(wave_first), seen_by_any = last_seen(wave_last);
     const int group_seen_by_all = last_seen(row0);
     const int parts = tile_of.parts;
@@ -128,10 +189,12 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
     const T *vbase = (const T *)a.v.data + k_first * a.v.token_stride + head * a.v.head_stride;
 
     // ---- copies of a tile into LDS ----
-    uint32_t kv_off[2][C::LOADS];
+    // (where a round of copies takes whole periods of the swizzles, the lanes' offsets of all rounds differ by the same)
+    constexpr bool SAME = NW * 64 % (16 * CH) == 0;
+    uint32_t kv_off[2][SAME ? 1 : C::LOADS];
     if constexpr (VEC) {
 #pragma unroll
-        for (int i = 0; i < C::LOADS; ++i) {
+        for (int i = 0; i < (SAME ? 1 : C::LOADS); ++i) {
             const int s = (i * NW + wave) * 64 + lane, j = s / CH, p = s % CH;
             const int kc = p ^ C::k_swizzle(j), vc = p ^ C::v_swizzle(j);
             kv_off[0][i] = kc * 8 < D ? (uint32_t)(j * a.k.token_stride * 2 + kc * 16) : 0x80000000u;
@@ -149,7 +212,8 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
                 const Buffer buffer = buffer_of(from, (int)((left - 1) * stride * 2 + D * 2));
 #pragma unroll
                 for (int i = 0; i < C::LOADS; ++i)
-                    copy_to_lds(buffer, (uint32_t)(uintptr_t)(lds_ptr)(to + (i * NW + wave) * 1024), kv_off[which][i]);
+                    copy_to_lds(buffer, (uint32_t)(uintptr_t)(lds_ptr)(to + (i * NW + wave) * 1024),
+                                SAME ? kv_off[which][0] + i * (uint32_t)(NW * 64 / CH * stride * 2) : kv_off[which][SAME ? 0 : i]);
             } else {
                 for (int i = 0; i < C::LOADS; ++i) {
                     const int s = (i * NW + wave) * 64 + lane, j = s / CH;
@@ -162,7 +226,7 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
             }
         }
     };
-    volatile int *odd_seen = (volatile int *)(lds + 2 * C::kStage);
+    volatile int *odd_seen = (volatile int *)(lds + C::kLds - 16);
     if (tid < 2) odd_seen[tid] = 0;
     if (first_tile < tiles) load_tile(first_tile, first_tile & 1);
 
@@ -188,7 +252,7 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
 
     // ---- LDS places of the operands: a row's and, apart because of the swizzle, a chunk's ----
     const int v_token = 4 * half + ((lane & 15) >> 2);           // of 8 or 16: the transposing read's lanes give 4 elements of a key each
-    const int k_row = col * DP * 2, v_row = C::kTile + v_token * DP * 2 + (lane & 1) * 8;
+    const int k_row = (key0 + col) * DP * 2, v_row = C::kTile + (key0 + v_token) * DP * 2 + (lane & 1) * 8;
     int k_chunk = (half ^ C::k_swizzle(col)) * 16;
     int v_chunk = ((2 * ((lane >> 4) & 1) + ((lane & 3) >> 1)) ^ C::v_swizzle(v_token)) * 16;
 
@@ -198,6 +262,7 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
     // m: what the weights are relative to, in units of the scores; no less than a number whose product with the scale is finite
     float m = -3.0e38f / fmaxf(a.scale, 1.0f), l = 0.0f;
 
+    bool odd = false;
     for (int tile = first_tile; tile < tiles; ++tile) {
         const int stage = tile & 1;
         copies_landed();
@@ -207,7 +272,6 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
         // (not known to stay the same: one instruction per read is cheaper than the registers of all places)
         asm volatile("" : "+v"(k_chunk), "+v"(v_chunk));
         const bool masked = tile * BN + BN - 1 > group_seen_by_all;          // for some row of the workgroup
-        bool odd = false;
         if (masked) {                            // a value that some row does not see must not reach it through 0 * infinity
             uint32_t most = 0;
             for (int i = 0; i < C::LOADS; ++i) {
@@ -217,36 +281,45 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
             if ((most & 0xffff) >= kInfinity<E> || (most >> 16) >= kInfinity<E>) odd_seen[tile & 1] = 1;
             if (tid == 0) odd_seen[~tile & 1] = 0;       // read before this tile's first barrier, written behind the next tile's
             __syncthreads();
-            odd = odd_seen[tile & 1] != 0;
+            odd = __builtin_amdgcn_readfirstlane(odd_seen[tile & 1]) != 0;
+            if (odd) break;
         }
-        if (tile * BN > seen_by_any) continue;
+        if (tile * BN + key0 > seen_by_any) continue;
         // operands are read a group ahead of the products that take them
-        f16v s[BN / 32];
-        u4 k_ahead[2][DP / 16];
-        auto read_keys = [&](int t) {
+        f16v s[KT];
+        {
+            constexpr int STEPS = DP / 16, ALL = KT * STEPS, N = C::AHEAD;
+            u4 ahead[2][N];
+            auto read = [&](int group) {
 #pragma unroll
-            for (int u = 0; u < DP / 16; ++u) k_ahead[t & 1][u] = *(const u4 *)(at + k_row + (k_chunk ^ 32 * u) + t * 32 * DP * 2);
-        };
-        read_keys(0);
+                for (int i = 0; i < N; ++i) {
+                    const int t = (group * N + i) / STEPS, u = (group * N + i) % STEPS;
+                    ahead[group & 1][i] = *(const u4 *)(at + k_row + (k_chunk ^ 32 * u) + t * 32 * DP * 2);
+                }
+            };
+            read(0);
 #pragma unroll
-        for (int t = 0; t < BN / 32; ++t) {
-            if (t + 1 < BN / 32) read_keys(t + 1);
-            __builtin_amdgcn_sched_barrier(0);
-            s[t] = (f16v)(0.0f);
+            for (int group = 0; group < ALL / N; ++group) {
+                if (group + 1 < ALL / N) read(group + 1);
+                __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int u = 0; u < DP / 16; ++u) s[t] = mfma32(E{}, k_ahead[t & 1][u], q[u], s[t]);
-            __builtin_amdgcn_sched_barrier(0);
+                for (int i = 0; i < N; ++i) {
+                    const int t = (group * N + i) / STEPS, u = (group * N + i) % STEPS;
+                    s[t] = mfma32(E{}, ahead[group & 1][i], q[u], u == 0 ? (f16v)(0.0f) : s[t]);
+                }
+                __builtin_amdgcn_sched_barrier(0);
+            }
         }
-        if (tile * BN + BN - 1 > seen_by_all) {
+        if (tile * BN + key0 + 32 * KT - 1 > seen_by_all) {
 #pragma unroll
-            for (int t = 0; t < BN / 32; ++t)
+            for (int t = 0; t < KT; ++t)
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (tile * BN + 32 * t + 8 * (i / 4) + 4 * half + i % 4 > seen) s[t][i] = -__builtin_inff();
+                    if (tile * BN + key0 + 32 * t + 8 * (i / 4) + 4 * half + i % 4 > seen) s[t][i] = -__builtin_inff();
         }
         float most = m;
 #pragma unroll
-        for (int t = 0; t < BN / 32; ++t)
+        for (int t = 0; t < KT; ++t)
 #pragma unroll
             for (int i = 0; i < 16; ++i) most = fmaxf(most, s[t][i]);
         most = max_of_halves(most);
@@ -258,9 +331,9 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
             m = most;
         }
         const float ms = m * a.scale;
-        u4 p[BN / 16];
+        u4 p[2 * KT];
 #pragma unroll
-        for (int t = 0; t < BN / 32; ++t)
+        for (int t = 0; t < KT; ++t)
 #pragma unroll
             for (int i = 0; i < 16; i += 2) {
                 const float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][i], a.scale, -ms));
@@ -274,64 +347,70 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
             const u2 v1 = __builtin_bit_cast(u2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s4)(from + 8 * DP * 2)));
             return (u4){v0[0], v0[1], v1[0], v1[1]};
         };
-        if (!odd) {
-            u4 v_ahead[2][DP / 32];
+        {
+            constexpr int STEPS = DP / 32, ALL = 2 * KT * STEPS, N = C::V_AHEAD;
+            u4 ahead[2][N];
+            auto read = [&](int group) {
 #pragma unroll
-            for (int t = 0; t < DP / 32; ++t) v_ahead[0][t] = v_operand(t, 0);
+                for (int i = 0; i < N; ++i) ahead[group & 1][i] = v_operand((group * N + i) % STEPS, (group * N + i) / STEPS);
+            };
+            read(0);
 #pragma unroll
-            for (int u = 0; u < BN / 16; ++u) {
-                if (u + 1 < BN / 16) {
-#pragma unroll
-                    for (int t = 0; t < DP / 32; ++t) v_ahead[(u + 1) & 1][t] = v_operand(t, u + 1);
-                }
+            for (int group = 0; group < ALL / N; ++group) {
+                if (group + 1 < ALL / N) read(group + 1);
                 __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int t = 0; t < DP / 32; ++t) o[t] = mfma32(E{}, v_ahead[u & 1][t], p[u], o[t]);
+                for (int i = 0; i < N; ++i) {
+                    const int t = (group * N + i) % STEPS, u = (group * N + i) / STEPS;
+                    o[t] = mfma32(E{}, ahead[group & 1][i], p[u], o[t]);
+                }
                 __builtin_amdgcn_sched_barrier(0);
-            }
-        } else {                                 // infinities and NaN apart: how many of either sign a row sees
-            u4 sees[BN / 16];
-#pragma unroll
-            for (int u = 0; u < BN / 16; ++u)
-#pragma unroll
-                for (int i = 0; i < 8; i += 2) {
-                    const int key = tile * BN + 16 * u + 8 * (i / 4) + 4 * half + i % 4;
-                    sees[u][i / 2] = pack2<E>(key <= seen ? 1.0f : 0.0f, key + 1 <= seen ? 1.0f : 0.0f);
-                }
-#pragma unroll
-            for (int t = 0; t < DP / 32; ++t) {
-                f16v up = (f16v)(0.0f), down = (f16v)(0.0f);
-#pragma unroll
-                for (int u = 0; u < BN / 16; ++u) {
-                    u4 v = v_operand(t, u), plus, minus;
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) {
-                        const uint32_t lo = v[e] & 0xffff, hi = v[e] >> 16;
-                        const uint32_t odd_lo = (lo & 0x7fff) >= kInfinity<E> ? 0xffffu : 0u, odd_hi = (hi & 0x7fff) >= kInfinity<E> ? 0xffff0000u : 0u;
-                        const uint32_t ones = (odd_lo | odd_hi) & (E::kOne | E::kOne << 16);
-                        plus[e] = ones & ((lo == (kInfinity<E> | 0x8000u) ? 0u : 0xffffu) | (hi == (kInfinity<E> | 0x8000u) ? 0u : 0xffff0000u));
-                        minus[e] = ones & ((lo == kInfinity<E> ? 0u : 0xffffu) | (hi == kInfinity<E> ? 0u : 0xffff0000u));
-                        v[e] &= ~(odd_lo | odd_hi);
-                    }
-                    o[t] = mfma32(E{}, v, p[u], o[t]);
-                    up = mfma32(E{}, plus, sees[u], up);
-                    down = mfma32(E{}, minus, sees[u], down);
-                }
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    o[t][i] += (up[i] > 0.0f ? __builtin_inff() : 0.0f) - (down[i] > 0.0f ? __builtin_inff() : 0.0f);
             }
         }
     }
 
+    f4 *const part = parts > 1 ? a.parts + (((int64_t)slot * a.kv_heads + head) * a.splits + split) * C::kPart : nullptr;
+    if (odd) {
+        copies_landed();
+        __syncthreads();
+        prompt_rows_one_by_one<E, C>(a, tile_of, head, first_tile * BN, tiles * BN, part, lds);
+        return;
+    }
     l = sum_of_halves(l);
-    if (parts > 1) {
-        f4 *mine = a.parts + (((int64_t)slot * a.kv_heads + head) * a.splits + split) * C::kPart + tid;
+    if constexpr (C::KS == 2) {                          // the two wavefronts of a row group, through LDS
+        f4 *const there = (f4 *)lds + row_group * 64 + lane;
+        copies_landed();
+        __syncthreads();
+        if (wave >= C::RW) {
+#pragma unroll
+            for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    there[(4 * t + i) * C::BM * 2] = (f4){o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
+            there[DP / 8 * C::BM * 2] = (f4){m, l, 0.0f, 0.0f};
+        }
+        __syncthreads();
+        if (wave >= C::RW) return;
+        const f4 other = there[DP / 8 * C::BM * 2];
+        const float top = fmaxf(m, other[0]), mine = __builtin_amdgcn_exp2f((m - top) * a.scale), its = __builtin_amdgcn_exp2f((other[0] - top) * a.scale);
+        l = l * mine + other[1] * its;
+        m = top;
 #pragma unroll
         for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) mine[(4 * t + i) * NW * 64] = (f4){o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
-        mine[DP / 8 * NW * 64] = (f4){m, l, 0.0f, 0.0f};
+            for (int i = 0; i < 4; ++i) {
+                const f4 x = there[(4 * t + i) * C::BM * 2];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[t][4 * i + e] = o[t][4 * i + e] * mine + x[e] * its;
+            }
+    }
+    if (parts > 1) {
+        f4 *mine = part + tid;
+#pragma unroll
+        for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mine[(4 * t + i) * C::BM * 2] = (f4){o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
+        mine[DP / 8 * C::BM * 2] = (f4){m, l, 0.0f, 0.0f};
         return;
     }
 
@@ -364,10 +443,10 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
 
 // The parts of a tile, joined in their order: a workgroup per tile and piece of 4 elements of a lane.
 template <class E, class C, bool VEC>
-__global__ __launch_bounds__(C::NW * 64) void attention_prompt_join_kernel(const PromptArgs a)
+__global__ __launch_bounds__(C::BM * 2) void attention_prompt_join_kernel(const PromptArgs a)
 {
     typedef typename E::T T;
-    constexpr int THREADS = C::NW * 64, PIECES = C::DP / 8;
+    constexpr int THREADS = C::BM * 2, PIECES = C::DP / 8;
     const int piece = blockIdx.x % PIECES, head = blockIdx.x / PIECES % a.kv_heads, slot = blockIdx.x / PIECES / a.kv_heads;
     const PromptTile<C> tile(a, slot);
     const int tid = threadIdx.x, lane = tid & 63, row = tile.row0 + 32 * (tid >> 6) + (lane & 31);
