@@ -172,8 +172,10 @@ bool allow_prompt_form()
 // Copies of 16-byte pieces, a tile's offsets within 31 bits.
 bool rows_in_pieces(const Rows &r) { return in_pieces(r, NGEMM_BF16) && r.token_stride < (1 << 23); }
 
-// Tiles of query rows that any lengths of the sequences can need, and over how many workgroups their keys are split: as many as the units take at once
-// if the rows were spread evenly, of no less than kLeastRun keys of sequences of equal lengths.
+// Tiles of query rows that any lengths of the sequences can need, and over how many workgroups their keys are split: as many as give every unit one
+// if the rows were spread evenly, of no less than kLeastRun keys of sequences of equal lengths, where the context is long enough for the
+// join (a launch more) to pay.
+constexpr int64_t kUnits = 256;
 struct PromptCut {
     int64_t slots, splits;
     size_t bytes;
@@ -183,7 +185,7 @@ PromptCut prompt_cut(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t q
 {
     const int64_t rows = q_tokens * (q_heads / kv_heads), tiles = std::max<int64_t>(batch, (rows + C::BM - 1) / C::BM) * kv_heads;
     PromptCut cut{rows / C::BM + batch, 1, 0};
-    cut.splits = std::max<int64_t>(1, std::min(256 * C::PER_CU / tiles, k_tokens / batch / kLeastRun));
+    if (k_tokens / batch >= 4 * kLeastRun) cut.splits = std::max<int64_t>(1, std::min(kUnits / tiles, k_tokens / batch / kLeastRun));
     if (cut.splits > 1) cut.bytes = (size_t)(cut.slots * kv_heads * cut.splits) * C::kPart * 16;
     return cut;
 }

@@ -226,7 +226,7 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
             }
         }
     };
-    volatile int *odd_seen = (volatile int *)(lds + C::kLds - 16);
+    __attribute__((address_space(3))) volatile int *odd_seen = (__attribute__((address_space(3))) volatile int *)(lds_ptr)(lds + C::kLds - 16);
     if (tid < 2) odd_seen[tid] = 0;
     if (first_tile < tiles) load_tile(first_tile, first_tile & 1);
 
