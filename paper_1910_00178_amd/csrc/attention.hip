@@ -59,14 +59,21 @@ bool in_pieces(const Rows &r, int type)
     return ((uintptr_t)r.data & 15u) == 0 && r.token_stride % pieces == 0 && r.head_stride % pieces == 0;
 }
 
+template <class E, int N>
+void launch_move_form(bool write, bool vec, unsigned groups, hipStream_t st, const MoveArgs &a)
+{
+    const dim3 grid(groups), block(256);
+    if (write && vec) hipLaunchKernelGGL((kv_write_kernel<E, N, true>), grid, block, 0, st, a);
+    else if (write) hipLaunchKernelGGL((kv_write_kernel<E, N, false>), grid, block, 0, st, a);
+    else if (vec) hipLaunchKernelGGL((kv_read_kernel<E, N, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((kv_read_kernel<E, N, false>), grid, block, 0, st, a);
+}
+
 template <class E>
 void launch_move(bool write, bool vec, unsigned groups, hipStream_t st, const MoveArgs &a)
 {
-    const dim3 grid(groups), block(256);
-    if (write && vec) hipLaunchKernelGGL((kv_write_kernel<E, true>), grid, block, 0, st, a);
-    else if (write) hipLaunchKernelGGL((kv_write_kernel<E, false>), grid, block, 0, st, a);
-    else if (vec) hipLaunchKernelGGL((kv_read_kernel<E, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((kv_read_kernel<E, false>), grid, block, 0, st, a);
+    if (a.cache.head_dim <= 128) launch_move_form<E, 1>(write, vec, groups, st, a);
+    else launch_move_form<E, 2>(write, vec, groups, st, a);
 }
 
 ngemm_status move_rows(bool write, ngemm_ctx *ctx, const ngemm_kv_cache *cache, int type, int64_t batch, int64_t tokens, Rows k, Rows v,
@@ -80,11 +87,15 @@ ngemm_status move_rows(bool write, ngemm_ctx *ctx, const ngemm_kv_cache *cache, 
     if (!offsets || !pages) return NGEMM_ERR_INVALID_ARG;
     for (const Rows &r : {k, v})
         if (const ngemm_status s = check_rows(r, type, tokens, cache->kv_heads, cache->head_dim, !write); s != NGEMM_OK) return s;
-    const int64_t groups = move_slots(tokens, batch) * cache->kv_heads;
-    if (groups > kMaxCount || move_slots(tokens, batch) * 16 > kMaxCount) return NGEMM_ERR_BAD_SHAPE;
+    // heads of a workgroup: two of them share finding the place where that leaves some thousands of workgroups (40000 tokens of 8 heads
+    // read: 53 us with two, 58 with one, 55 with four; 1700 workgroups of one head or 850 of two the same, fewer are slower)
+    const int64_t slots = move_slots(tokens, batch);
+    if (slots * cache->kv_heads > kMaxCount || slots * 16 > kMaxCount) return NGEMM_ERR_BAD_SHAPE;
+    const int64_t heads = slots * cache->kv_heads >= 4096 ? std::min<int64_t>(cache->kv_heads, 2) : 1;
+    const int64_t groups = slots * ((cache->kv_heads + heads - 1) / heads);
     DeviceGuard g(ctx->device);
     if (!g.ok) return NGEMM_ERR_DEVICE;
-    const MoveArgs a{view_of(cache, pages, pages_stride), k, v, offsets, starts, (int32_t)batch, (int32_t)tokens};
+    const MoveArgs a{view_of(cache, pages, pages_stride), k, v, offsets, starts, (int32_t)batch, (int32_t)tokens, (int32_t)heads};
     const bool vec = in_pieces(k, type) && in_pieces(v, type);
     hipStream_t st = (hipStream_t)stream;
     if (type == NGEMM_F32) launch_move<F32>(write, vec, (unsigned)groups, st, a);

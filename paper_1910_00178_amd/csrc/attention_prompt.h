@@ -50,8 +50,6 @@ __device__ __forceinline__ uint32_t max_u16(uint32_t a, uint32_t b)
     typedef uint16_t V2 __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(V2, a), __builtin_bit_cast(V2, b)));
 }
-template <class E> constexpr uint32_t kInfinity = 0x7f80;
-template <> constexpr uint32_t kInfinity<F16> = 0x7c00;
 
 // Copies memory -> LDS, 16 bytes a lane from base + offset; what lies past the buffer's end becomes 0.  Written as the instruction: behind
 // the builtin, the compiler lets the transposing LDS reads wait for every copy in flight, those of the next tile among them.  No
@@ -82,14 +80,16 @@ struct PromptTile {
         group = a.q_heads / a.kv_heads;
         causal = a.causal;
         // Sequence b has the slots floor(rows before it / BM) + b .. : as many as its rows need or one more.
-        b = last_start(a.batch, slot, [&](int x) { return a.q_offsets[x] * group / C::BM + x; });
-        q_first = min(max(a.q_offsets[b], 0), a.q_tokens);
-        queries = min(max(a.q_offsets[b + 1], q_first), a.q_tokens) - q_first;
-        row0 = (slot - (a.q_offsets[b] * group / C::BM + b)) * C::BM;
+        int of[4];
+        b = find_sequence(a.batch, slot, {a.q_offsets, a.q_offsets + 1, a.k_offsets, a.k_offsets + 1}, of,
+                          [&](int offset, int x) { return offset * group / C::BM + x; });
+        q_first = min(max(of[0], 0), a.q_tokens);
+        queries = min(max(of[1], q_first), a.q_tokens) - q_first;
+        row0 = (slot - (of[0] * group / C::BM + b)) * C::BM;
         rows = queries * group;
         there = row0 >= 0 && row0 < rows;
-        k_first = min(max(a.k_offsets[b], 0), a.k_tokens);
-        keys = min(max(a.k_offsets[b + 1], k_first), a.k_tokens) - k_first;
+        k_first = min(max(of[2], 0), a.k_tokens);
+        keys = min(max(of[3], k_first), a.k_tokens) - k_first;
         key_tiles = max(0, (last_seen(min(row0 + C::BM, rows) - 1) + C::BN) / C::BN);
         run = a.splits > 1 ? max((key_tiles + a.splits - 1) / a.splits, kLeastRun / C::BN) : key_tiles;
         parts = a.splits > 1 ? max(1, (key_tiles + run - 1) / run) : 1;
@@ -278,7 +278,7 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
                 const u4 x = *(const u4 *)(at + C::kTile + ((i * NW + wave) * 64 + lane) * 16) & 0x7fff7fffu;
                 most = max_u16(most, max_u16(max_u16(x[0], x[1]), max_u16(x[2], x[3])));
             }
-            if ((most & 0xffff) >= kInfinity<E> || (most >> 16) >= kInfinity<E>) odd_seen[tile & 1] = 1;
+            if ((most & 0xffff) >= E::kInfinityBits || (most >> 16) >= E::kInfinityBits) odd_seen[tile & 1] = 1;
             if (tid == 0) odd_seen[~tile & 1] = 0;       // read before this tile's first barrier, written behind the next tile's
             __syncthreads();
             odd = __builtin_amdgcn_readfirstlane(odd_seen[tile & 1]) != 0;
