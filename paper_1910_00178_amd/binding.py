@@ -410,12 +410,13 @@ def ngemm_attention_prompt(ctx, type, batch, q_heads, kv_heads, head_dim, q_toke
            "ngemm_attention_prompt")
 
 
-# The calls above that a program makes per product, weight or batch: natively where all arguments are of the usual types,
+# The calls above that a program makes per product, weight, batch or step: natively where all arguments are of the usual types,
 # else as above.
 _kinds = {"ngemm_run_u8s8s32": "run", "ngemm_run_s8s8s32": "run", "ngemm_run_u8u8s32": "run", "ngemm_run_s16s16s32": "run",
           "ngemm_run_u8s8s32_static": "static", "ngemm_run_u8s8u8_requant": "requant", "ngemm_run_u8s8u8_requant_channel": "channel",
           "ngemm_run_u8s8s32_unpacked": "unpacked", "ngemm_run_batched_u8s8s32": "batched", "ngemm_pack_b": "pack", "ngemm_pack_b_u8": "pack",
-          "ngemm_pack_b_s16": "pack", "ngemm_packed_b_free": "free"}
+          "ngemm_pack_b_s16": "pack", "ngemm_packed_b_free": "free", "ngemm_kv_write": "move", "ngemm_kv_read": "move",
+          "ngemm_attention_decode": "decode", "ngemm_attention_prompt": "prompt"}
 _native = hasattr(_calls, "Call")
 if _native:
     for _name in _kinds:

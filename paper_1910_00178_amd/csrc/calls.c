@@ -15,7 +15,8 @@
 
 #if PY_VERSION_HEX >= 0x030A0000 && PY_VERSION_HEX < 0x030B0000      /* (other versions' functions are laid out otherwise: all calls by ctypes there) */
 
-enum { KIND_RUN, KIND_STATIC, KIND_REQUANT, KIND_CHANNEL, KIND_UNPACKED, KIND_BATCHED, KIND_PACK, KIND_FREE, KIND_COUNT };
+enum { KIND_RUN, KIND_STATIC, KIND_REQUANT, KIND_CHANNEL, KIND_UNPACKED, KIND_BATCHED, KIND_PACK, KIND_FREE,
+       KIND_MOVE, KIND_DECODE, KIND_PROMPT, KIND_COUNT };
 
 /* One letter per Python argument: h handle, l int64, i int32, z size_t, f float, b truth, d device pointer, s stream, p problems.
  * `need` of them have to be there; the rest are pointers, sizes and streams that default to nothing. */
@@ -24,8 +25,10 @@ static const struct { const char *name, *spec; int need; } kinds[KIND_COUNT] = {
     {"requant", "hldlihifidldzs", 11},    {"channel", "hldlihidddbidldzs", 14},
     {"unpacked", "hllldlidlidldzs", 14},  {"batched", "hpdzs", 2},
     {"pack", "hlldldzs", 7},              {"free", "h", 1},
+    {"move", "hhilldlldlldddls", 15},     {"decode", "hhilldlldldlfdlldzs", 16},
+    {"prompt", "hillllldllldlldllddbfdlldzs", 24},
 };
-#define MAX_ARGS 17
+#define MAX_ARGS 27
 
 typedef union { int64_t l; int32_t i; size_t z; float f; void *p; } Value;
 
@@ -232,6 +235,20 @@ static PyObject *call(PyObject *self, PyObject *const *args, size_t nargsf, PyOb
             break;
         case KIND_PACK:
             status = ((int (*)(P, L, L, P, L, P, size_t, P, P *))c->fn)(v[0].p, v[1].l, v[2].l, v[3].p, v[4].l, v[5].p, v[6].z, v[7].p, &handle);
+            break;
+        case KIND_MOVE:
+            status = ((int (*)(P, P, int, L, L, P, L, L, P, L, L, P, P, P, L, P))c->fn)(v[0].p, v[1].p, v[2].i, v[3].l, v[4].l, v[5].p, v[6].l, v[7].l, v[8].p,
+                                                                                       v[9].l, v[10].l, v[11].p, v[12].p, v[13].p, v[14].l, v[15].p);
+            break;
+        case KIND_DECODE:
+            status = ((int (*)(P, P, int, L, L, P, L, L, P, L, P, L, float, P, L, L, P, size_t, P))c->fn)(
+                v[0].p, v[1].p, v[2].i, v[3].l, v[4].l, v[5].p, v[6].l, v[7].l, v[8].p, v[9].l, v[10].p, v[11].l, v[12].f, v[13].p, v[14].l, v[15].l,
+                v[16].p, v[17].z, v[18].p);
+            break;
+        case KIND_PROMPT:
+            status = ((int (*)(P, int, L, L, L, L, L, P, L, L, L, P, L, L, P, L, L, P, P, int, float, P, L, L, P, size_t, P))c->fn)(
+                v[0].p, v[1].i, v[2].l, v[3].l, v[4].l, v[5].l, v[6].l, v[7].p, v[8].l, v[9].l, v[10].l, v[11].p, v[12].l, v[13].l, v[14].p, v[15].l,
+                v[16].l, v[17].p, v[18].p, v[19].i, v[20].f, v[21].p, v[22].l, v[23].l, v[24].p, v[25].z, v[26].p);
             break;
         default:
             status = ((int (*)(P))c->fn)(v[0].p);
