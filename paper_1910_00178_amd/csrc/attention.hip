@@ -106,52 +106,64 @@ ngemm_status move_rows(bool write, ngemm_ctx *ctx, const ngemm_kv_cache *cache, 
 
 // ---- one token per sequence ----
 
-// How a sequence is cut: chunks of whole rounds of a workgroup's tiles, so long that the grid has some workgroups per unit, and no longer than a
-// sequence of middling length leaves balanced.
+// How a sequence is cut.  Whole, by eight wavefronts, where the sequences and heads give half of the units a workgroup and no wavefront takes more than
+// four tiles: the join, a launch more, costs what the split gains (32 sequences of up to 1000 tokens, 12 heads of 64: 8.7 us whole,
+// 10.8 in chunks of 512; 64 of 2000, 8 K/V heads of 64: 25 and 34; heads of more than 192 have no registers for it: 26.8 and 25.2).  Else in
+// chunks, by four wavefronts: as many as give every unit four workgroups, of 256 to 4096 tokens (a few sequences of 100000 tokens: 355 us,
+// 367 with chunks of up to 2048; 64 sequences of very different lengths lose 5 of 60 us by it).
+constexpr int64_t kUnits = 256;
+constexpr int kWideHeadDim = 192;
+
 struct DecodeCut {
-    int64_t chunk, chunks;
+    int64_t waves, chunk, chunks;
     size_t bytes;
 };
 DecodeCut decode_cut(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t max_length)
 {
-    constexpr int64_t round = 64 * kDecodeWaves;
     const int64_t group = q_heads / kv_heads, grid = batch * kv_heads * ((group + 15) / 16);
-    int64_t chunk = (max_length * grid / 1024 + round - 1) / round * round;
-    chunk = std::min<int64_t>(std::max<int64_t>(chunk, round), 4096);
-    DecodeCut cut{chunk, std::max<int64_t>(1, (max_length + chunk - 1) / chunk), 0};
+    if (grid >= kUnits / 2 && max_length > 256 && max_length <= 4 * 64 * 8 && head_dim <= kWideHeadDim)
+        return DecodeCut{8, (max_length + 511) / 512 * 512, 1, 0};
+    DecodeCut cut{4, std::min<int64_t>(std::max<int64_t>((max_length * grid / (4 * kUnits) + 255) / 256 * 256, 256), 4096), 1, 0};
+    cut.chunks = std::max<int64_t>(1, (max_length + cut.chunk - 1) / cut.chunk);
     if (cut.chunks > 1) cut.bytes = (size_t)(batch * q_heads * cut.chunks * (head_dim / 4 + 1) * 16);
     return cut;
 }
 
-template <class E, int D>
+template <class E, int D, int NW>
 hipError_t allow_decode_lds()
 {
-    void (*const kernel)(DecodeArgs) = attention_decode_kernel<E, D>;
-    return hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kDecodeWaves * (32 + 16 * D) * 4);
+    void (*const kernel)(DecodeArgs) = attention_decode_kernel<E, D, NW>;
+    return hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, NW * (32 + 16 * D) * 4);
 }
 
-// f(DecodeIndex<head_dim>{})
+// f(Index<head_dim>{})
 template <int D = 256, class F>
 void with_head_dim(int64_t head_dim, F &&f)
 {
-    if (head_dim == D) f(DecodeIndex<D>{});
+    if (head_dim == D) f(Index<D>{});
     else if constexpr (D > 16) with_head_dim<D - 16>(head_dim, f);
 }
 
-template <class E, int D>
+template <class E, int D, int NW>
 void launch_decode_form(const DecodeArgs &a, hipStream_t st)
 {
     const int group = a.q_heads / a.cache.kv_heads;
     const unsigned grid = (unsigned)((int64_t)a.batch * a.cache.kv_heads * ((group + 15) / 16) * a.chunks);
-    const size_t lds = (size_t)kDecodeWaves * (32 + std::min(group, 16) * D) * 4;
-    hipLaunchKernelGGL((attention_decode_kernel<E, D>), dim3(grid), dim3(kDecodeWaves * 64), lds, st, a);
+    const size_t lds = (size_t)NW * (32 + std::min(group, 16) * D) * 4;
+    hipLaunchKernelGGL((attention_decode_kernel<E, D, NW>), dim3(grid), dim3(NW * 64), lds, st, a);
     if (a.chunks > 1) hipLaunchKernelGGL((attention_decode_join_kernel<E, D>), dim3((unsigned)(a.batch * a.q_heads)), dim3(kJoinThreads), 0, st, a);
 }
 
 template <class E>
-void launch_decode(const DecodeArgs &a, hipStream_t st)
+void launch_decode(const DecodeArgs &a, int64_t waves, hipStream_t st)
 {
-    with_head_dim(a.cache.head_dim, [&](auto dim) { launch_decode_form<E, decltype(dim)::value>(a, st); });
+    with_head_dim(a.cache.head_dim, [&](auto dim) {
+        constexpr int D = decltype(dim)::value;
+        if constexpr (D <= kWideHeadDim) {
+            if (waves == 8) return launch_decode_form<E, D, 8>(a, st);
+        }
+        launch_decode_form<E, D, 4>(a, st);
+    });
 }
 
 // ---- prompts ----
@@ -186,7 +198,6 @@ bool rows_in_pieces(const Rows &r) { return in_pieces(r, NGEMM_BF16) && r.token_
 // Tiles of query rows that any lengths of the sequences can need, and over how many workgroups their keys are split: as many as give every unit one
 // if the rows were spread evenly, of no less than kLeastRun keys of sequences of equal lengths, where the context is long enough for the
 // join (a launch more) to pay.
-constexpr int64_t kUnits = 256;
 struct PromptCut {
     int64_t slots, splits;
     size_t bytes;
@@ -231,7 +242,8 @@ bool ngemm::attention_setup()
     for (int64_t d = 16; d <= 256; d += 16)
         with_head_dim(d, [&](auto dim) {
             constexpr int D = decltype(dim)::value;
-            ok = ok && allow_decode_lds<F16, D>() == hipSuccess && allow_decode_lds<BF16, D>() == hipSuccess;
+            ok = ok && allow_decode_lds<F16, D, 4>() == hipSuccess && allow_decode_lds<BF16, D, 4>() == hipSuccess;
+            if constexpr (D <= kWideHeadDim) ok = ok && allow_decode_lds<F16, D, 8>() == hipSuccess && allow_decode_lds<BF16, D, 8>() == hipSuccess;
         });
     for (int64_t d : {64, 96, 128, 192, 256})
         with_prompt_form(d, [&](auto form) { ok = ok && allow_prompt_form<decltype(form)>(); });
@@ -330,8 +342,8 @@ ngemm_status ngemm_attention_decode(ngemm_ctx *ctx, const ngemm_kv_cache *cache,
     const DecodeArgs a{view_of(cache, pages_dev, pages_stride), q, o, lengths_dev, (int32_t)batch, (int32_t)q_heads, (int32_t)max_length,
                        (int32_t)cut.chunk, (int32_t)cut.chunks, scale * 1.44269504f, (f4 *)workspace_dev, in_pieces(q, type), in_pieces(o, type)};
     hipStream_t st = (hipStream_t)hip_stream;
-    if (type == NGEMM_F16) launch_decode<F16>(a, st);
-    else launch_decode<BF16>(a, st);
+    if (type == NGEMM_F16) launch_decode<F16>(a, cut.waves, st);
+    else launch_decode<BF16>(a, cut.waves, st);
     return launched();
 }
 

@@ -15,8 +15,7 @@ struct DecodeArgs {
     int32_t q_pieces, o_pieces;          // whether rows lie at 16-byte multiples
 };
 
-constexpr int kDecodeWaves = 4;
-constexpr int decode_waves_per_simd(int D) { return D <= 64 ? 4 : D <= 128 ? 2 : D <= 192 ? 2 : 1; }
+constexpr int decode_waves_per_simd(int D) { return D <= 64 ? 4 : D <= 192 ? 2 : 1; }
 
 // 16 codes as 16-bit floats, in order.  A code with its sign bit turned, as the low byte under 0x64, is the float 1024 + 128 + code.
 __device__ __forceinline__ void codes_to_f16(u4 x, u4 (&out)[2])
@@ -40,12 +39,12 @@ __device__ __forceinline__ float of_row(float x)
 }
 
 // f(IntC<0>) .. f(IntC<N - 1>)
-template <int I> struct DecodeIndex { static constexpr int value = I; };
+template <int I> struct Index { static constexpr int value = I; };
 template <int N, int I = 0, class F>
 __device__ __forceinline__ void unrolled(F &&f)
 {
     if constexpr (I < N) {
-        f(DecodeIndex<I>{});
+        f(Index<I>{});
         unrolled<N, I + 1>(f);
     }
 }
@@ -66,11 +65,12 @@ __device__ __forceinline__ void put_row(const DecodeArgs &a, int b, int qh, int 
 // a K/V head.  Row r of the first product's tile t is token 4 t + r % 4 of block r / 4, so that lane 16 g + h holds head h's scores of
 // block g's tokens, which is what the second product wants of it: the 16 tokens of a row of V in a block are the lane's 16-byte load.
 // D: head_dim, known to the compiler so that the loads of a tile are one run without branches.
-template <class E, int D>
-__global__ __launch_bounds__(kDecodeWaves * 64, decode_waves_per_simd(D)) void attention_decode_kernel(const DecodeArgs a)
+// NW wavefronts of a workgroup take the chunk's tiles in turn.
+template <class E, int D, int NW>
+__global__ __launch_bounds__(NW * 64, decode_waves_per_simd(D)) void attention_decode_kernel(const DecodeArgs a)
 {
     extern __shared__ __align__(16) float shared[];
-    constexpr int NW = kDecodeWaves, NJ = (D + 63) / 64, DT = D / 16;
+    constexpr int NJ = (D + 63) / 64, DT = D / 16;
     typedef typename E::T T;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = lane & 15, g = lane >> 4;
@@ -220,20 +220,23 @@ __global__ __launch_bounds__(kDecodeWaves * 64, decode_waves_per_simd(D)) void a
         for (int i = 3; i < 16; ++i) most = fmaxf(most, s[i / 4][i % 4]);
         if (__any(most > m + 8.0f)) {                    // weights up to 2^8 fit
             most = fmaxf(max_of_rows(most), m);
-            const float fall = __builtin_amdgcn_exp2f(m - most);
-            l *= fall;
+            if (tile > wave) {                           // (nothing to scale yet in the first tile)
+                const float fall = __builtin_amdgcn_exp2f(m - most);
+                l *= fall;
 #pragma unroll
-            for (int t = 0; t < DT; ++t) o[t] *= fall;
+                for (int t = 0; t < DT; ++t) o[t] *= fall;
+            }
             m = most;
         }
         if (__any(vs_now > 64.0f * unit)) {
             const float top = max_of_rows(max_in_row(vs_now));
             const int e = __builtin_amdgcn_frexp_expf(top);
-            const float now = __builtin_amdgcn_ldexpf(1.0f, e), fall = unit * __builtin_amdgcn_ldexpf(1.0f, -e);
-#pragma unroll
-            for (int t = 0; t < DT; ++t) o[t] *= fall;
-            unit = now;
             per_unit = __builtin_amdgcn_ldexpf(1.0f, -e);
+            if (tile > wave) {
+#pragma unroll
+                for (int t = 0; t < DT; ++t) o[t] *= unit * per_unit;
+            }
+            unit = __builtin_amdgcn_ldexpf(1.0f, e);
         }
         vs_now *= per_unit;
         u4 p[2];
