@@ -109,8 +109,9 @@ ngemm_status move_rows(bool write, ngemm_ctx *ctx, const ngemm_kv_cache *cache, 
 // How a sequence is cut.  Whole, by eight wavefronts, where the sequences and heads give half of the units a workgroup and no wavefront takes more than
 // four tiles: the join, a launch more, costs what the split gains (32 sequences of up to 1000 tokens, 12 heads of 64: 8.7 us whole,
 // 10.8 in chunks of 512; 64 of 2000, 8 K/V heads of 64: 25 and 34; heads of more than 192 have no registers for it: 26.8 and 25.2).  Else in
-// chunks, by four wavefronts: as many as give every unit four workgroups, of 256 to 4096 tokens (a few sequences of 100000 tokens: 355 us,
-// 367 with chunks of up to 2048; 64 sequences of very different lengths lose 5 of 60 us by it).
+// chunks, by four wavefronts: as many as give every unit two workgroups, of 256 to 4096 tokens (8 sequences of 100000 to 131072 tokens: 362 us,
+// with half as long ones 377, with 512 tokens 413; 16 of 8192 with heads of 256: 62 us, with half as long ones 73; only 64 sequences of
+// very different lengths would rather have 1024 tokens: 73 us for 79).
 constexpr int64_t kUnits = 256;
 constexpr int kWideHeadDim = 192;
 
@@ -123,7 +124,7 @@ DecodeCut decode_cut(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t h
     const int64_t group = q_heads / kv_heads, grid = batch * kv_heads * ((group + 15) / 16);
     if (grid >= kUnits / 2 && max_length > 256 && max_length <= 4 * 64 * 8 && head_dim <= kWideHeadDim)
         return DecodeCut{8, (max_length + 511) / 512 * 512, 1, 0};
-    DecodeCut cut{4, std::min<int64_t>(std::max<int64_t>((max_length * grid / (4 * kUnits) + 255) / 256 * 256, 256), 4096), 1, 0};
+    DecodeCut cut{4, std::min<int64_t>(std::max<int64_t>((max_length * grid / (2 * kUnits) + 255) / 256 * 256, 256), 4096), 1, 0};
     cut.chunks = std::max<int64_t>(1, (max_length + cut.chunk - 1) / cut.chunk);
     if (cut.chunks > 1) cut.bytes = (size_t)(batch * q_heads * cut.chunks * (head_dim / 4 + 1) * 16);
     return cut;

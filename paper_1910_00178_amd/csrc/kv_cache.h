@@ -307,12 +307,15 @@ __global__ __launch_bounds__(256) void kv_write_kernel(const MoveArgs a)
     }
 }
 
-// Four codes times a scale.
+// Four codes times a scale, as floats (the compiler would round some products to 16 bits in one step, others in two).
 __device__ __forceinline__ void values4(uint32_t codes, float scale, float *x)
 {
     const uint32_t y = codes ^ 0x80808080u;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x[e] = ((float)(y >> (8 * e) & 255u) - 128.0f) * scale;
+    for (int e = 0; e < 4; ++e) {
+        x[e] = ((float)(y >> (8 * e) & 255u) - 128.0f) * scale;
+        asm("" : "+v"(x[e]));
+    }
 }
 
 // K: 16 lanes a token, as above.  V: a thread takes four tokens of four elements and transposes their bytes.

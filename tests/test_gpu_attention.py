@@ -133,6 +133,43 @@ def test_write_and_read(ctx, shape, dtype, how):
 
 
 @pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_read_rounds_floats(ctx, dtype):
+    """Every element is the float product of code and scale, rounded to the type: half a million products of any bits."""
+    P, page, H, D = 32, 64, 4, 64
+    g = gen(4)
+    want = Cache(P, page, H, D)
+    k, v, ks, vs = want.views()
+    k.copy_(torch.randint(-127, 128, k.shape, generator=g))
+    v.copy_(torch.randint(-127, 128, v.shape, generator=g))
+    ks.copy_(torch.rand(ks.shape, generator=g) + 0.01)
+    vs.copy_(torch.rand(vs.shape, generator=g) + 0.01)
+    raw = want.raw.cuda()
+    c = handle(ctx, want, raw)
+    n = P * page
+    ko, vo = (torch.empty(n, H, D, dtype=dtype, device="cuda") for _ in range(2))
+    ng.ngemm_kv_read(ctx, c, number(dtype), 1, n, ko, H * D, D, vo, H * D, D, ints([0, n]), None, ints([list(range(P))]), P)
+    torch.cuda.synchronize()
+    for out, codes, scales in ((ko, k, ks), (vo, v, vs)):
+        rows = (codes.float() * scales.unsqueeze(-1)).permute(0, 2, 3, 1, 4).reshape(n, H, D).to(dtype)
+        assert torch.equal(out.cpu(), rows)
+    ng.ngemm_kv_cache_free(c)
+
+
+def test_prompt_infinities_where_keys_are_split(ctx):
+    """As below, in a tile of a split context: one part's workgroup goes row by row, the others do not."""
+    heads, n, m = (4, 2, 128), [40], [3000]
+    q, k, v = prompt_rows(2, heads, n, m, BF16)
+    clean = prompt_wanted(q, k, v, n, m, 1, 0.1)
+    v[2990, 1, 7] = math.inf                               # seen by queries 30 .. 39
+    k[2999] = math.nan                                     # seen by the last query alone
+    got = prompt(ctx, q, k, v, n, m, 1, 0.1).double()
+    assert bool(torch.isnan(got[39]).all()) and bool((got[30:39, 2:, 7] == math.inf).all())
+    want, size = clean
+    got[30:39, 2:, 7], want[30:39, 2:, 7] = 0, 0
+    check(got[:39], want[:39], size[:39], BF16)
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
 def test_write_extreme_rows(ctx, dtype):
     """Rows of zeros, of one element, the largest and the smallest numbers, ties, infinities and NaN."""
     D, H = 64, 1
