@@ -436,7 +436,8 @@ ngemm_status ngemm_kv_read(ngemm_ctx *ctx, const ngemm_kv_cache *cache, ngemm_ty
  * One new token per sequence attends to the cache (f16 or bf16):
  *     O[b][h] = sum_t p_t V_t / sum_t p_t,  p_t = exp(scale <Q[b][h], K_t> - max),  t < lengths[b],
  * with the K and V of head h / (q_heads / kv_heads) (q_heads a multiple of the cache's kv_heads).  lengths_dev: int32
- * [batch], the tokens of each sequence in the cache, the new one included; at most max_length of them are read.  A
+ * [batch], the tokens of each sequence in the cache, the new one included; at most max_length (up to 2^30) of them are read, which also
+ * sizes the launch and the workspace: the longest of the lengths.  A
  * sequence without tokens gives 0; tokens in a page that is not one of the cache's are left out.  Softmax
  * statistics and sums are float; the weights p_t times V's scales enter the second product as f16, relative
  * to the largest.  Scores are products of the 8-bit codes and the query as f16 (bf16 queries relative to a power of

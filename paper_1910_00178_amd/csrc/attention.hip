@@ -21,6 +21,8 @@ namespace {
 
 constexpr uint32_t kCacheMagic = 0x4e474b56u;   // "NGKV"
 constexpr int64_t kMaxCount = 0x7fffffff - 4096;
+constexpr int64_t kMaxLength = 1 << 30;         // tokens of a sequence in the cache
+constexpr int64_t kMaxGroups = (1 << 23) - 1;   // workgroups of a launch: with 512 threads each, a launch counts threads in 32 bits
 constexpr int64_t kMaxStride = 1ll << 40;       // elements; products with a row's number stay within 64 bits
 
 bool cache_ok(const ngemm_kv_cache *c) { return c && c->magic == kCacheMagic; }
@@ -91,8 +93,9 @@ ngemm_status move_rows(bool write, ngemm_ctx *ctx, const ngemm_kv_cache *cache, 
     // read: 53 us with two, 58 with one, 55 with four; 1700 workgroups of one head or 850 of two the same, fewer are slower)
     const int64_t slots = move_slots(tokens, batch);
     if (slots * cache->kv_heads > kMaxCount || slots * 16 > kMaxCount) return NGEMM_ERR_BAD_SHAPE;
-    const int64_t heads = slots * cache->kv_heads >= 4096 ? std::min<int64_t>(cache->kv_heads, 2) : 1;
+    const int64_t heads = std::min<int64_t>(cache->kv_heads, std::max<int64_t>(slots * cache->kv_heads >= 4096 ? 2 : 1, slots * cache->kv_heads / kMaxGroups + 1));
     const int64_t groups = slots * ((cache->kv_heads + heads - 1) / heads);
+    if (groups > kMaxGroups) return NGEMM_ERR_BAD_SHAPE;
     DeviceGuard g(ctx->device);
     if (!g.ok) return NGEMM_ERR_DEVICE;
     const MoveArgs a{view_of(cache, pages, pages_stride), k, v, offsets, starts, (int32_t)batch, (int32_t)tokens, (int32_t)heads};
@@ -169,6 +172,8 @@ void launch_decode(const DecodeArgs &a, int64_t waves, hipStream_t st)
 
 // ---- prompts ----
 
+constexpr int64_t kPromptRows = 128;            // of a tile in all forms
+
 // f(PromptCfg<...>{}) for the smallest DP that holds head_dim.
 template <class F>
 void with_prompt_form(int64_t head_dim, F &&f)
@@ -217,6 +222,7 @@ template <class E, class C>
 void launch_prompt_form(PromptArgs a, bool vec, void *workspace, hipStream_t st)
 {
     const PromptCut cut = prompt_cut<C>(a.batch, a.q_heads, a.kv_heads, a.q_tokens, a.k_tokens);
+    static_assert(C::BM == kPromptRows, "one height of tiles");
     a.slots = (int32_t)cut.slots;
     a.splits = (int32_t)cut.splits;
     a.parts = (f4 *)workspace;
@@ -309,7 +315,7 @@ ngemm_status ngemm_kv_read(ngemm_ctx *ctx, const ngemm_kv_cache *cache, ngemm_ty
 
 size_t ngemm_attention_decode_workspace_bytes(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t max_length)
 {
-    if (batch < 1 || q_heads < 1 || kv_heads < 1 || q_heads % kv_heads || !head_dim_ok(head_dim) || max_length < 0 || max_length > kMaxCount ||
+    if (batch < 1 || q_heads < 1 || kv_heads < 1 || q_heads % kv_heads || !head_dim_ok(head_dim) || max_length < 0 || max_length > kMaxLength ||
         batch > kMaxCount || q_heads > 65536 || batch * q_heads > kMaxCount)
         return 0;
     return decode_cut(batch, q_heads, kv_heads, head_dim, max_length).bytes;
@@ -324,7 +330,7 @@ ngemm_status ngemm_attention_decode(ngemm_ctx *ctx, const ngemm_kv_cache *cache,
 {
     if (!ctx_ok(ctx) || !cache_ok(cache) || cache->device != ctx->device) return NGEMM_ERR_INVALID_ARG;
     if ((type != NGEMM_F16 && type != NGEMM_BF16) || !std::isfinite(scale)) return NGEMM_ERR_INVALID_ARG;
-    if (batch < 0 || batch > kMaxCount || q_heads < 1 || q_heads > 65536 || q_heads % cache->kv_heads || max_length < 0 || max_length > kMaxCount ||
+    if (batch < 0 || batch > kMaxCount || q_heads < 1 || q_heads > 65536 || q_heads % cache->kv_heads || max_length < 0 || max_length > kMaxLength ||
         pages_stride < 0 || pages_stride > kMaxCount || batch * q_heads > kMaxCount)
         return NGEMM_ERR_BAD_SHAPE;
     if (batch == 0) return NGEMM_OK;
@@ -339,7 +345,7 @@ ngemm_status ngemm_attention_decode(ngemm_ctx *ctx, const ngemm_kv_cache *cache,
     DeviceGuard g(ctx->device);
     if (!g.ok) return NGEMM_ERR_DEVICE;
     const DecodeCut cut = decode_cut(batch, q_heads, cache->kv_heads, cache->head_dim, max_length);
-    if (batch * q_heads * cut.chunks > kMaxCount) return NGEMM_ERR_BAD_SHAPE;
+    if (batch * q_heads * cut.chunks > kMaxGroups) return NGEMM_ERR_BAD_SHAPE;
     const DecodeArgs a{view_of(cache, pages_dev, pages_stride), q, o, lengths_dev, (int32_t)batch, (int32_t)q_heads, (int32_t)max_length,
                        (int32_t)cut.chunk, (int32_t)cut.chunks, scale * 1.44269504f, (f4 *)workspace_dev, in_pieces(q, type), in_pieces(o, type)};
     hipStream_t st = (hipStream_t)hip_stream;
@@ -376,6 +382,7 @@ ngemm_status ngemm_attention_prompt(ngemm_ctx *ctx, ngemm_type type, int64_t bat
         return NGEMM_ERR_BAD_SHAPE;
     if (q_tokens == 0) return NGEMM_OK;
     if (batch == 0 || (!k_offsets_dev && k_tokens != q_tokens)) return NGEMM_ERR_BAD_SHAPE;
+    if ((q_tokens * (q_heads / kv_heads) / kPromptRows + batch) * kv_heads > kMaxGroups) return NGEMM_ERR_BAD_SHAPE;
     if (!q_offsets_dev) return NGEMM_ERR_INVALID_ARG;
     const Rows q{const_cast<void *>(Q_dev), q_token_stride, q_head_stride}, k{const_cast<void *>(K_dev), k_token_stride, k_head_stride},
         v{const_cast<void *>(V_dev), v_token_stride, v_head_stride}, o{O_dev, o_token_stride, o_head_stride};
