@@ -61,21 +61,22 @@ bool in_pieces(const Rows &r, int type)
     return ((uintptr_t)r.data & 15u) == 0 && r.token_stride % pieces == 0 && r.head_stride % pieces == 0;
 }
 
-template <class E, int N>
+template <class E, int LANES, int N>
 void launch_move_form(bool write, bool vec, unsigned groups, hipStream_t st, const MoveArgs &a)
 {
-    const dim3 grid(groups), block(256);
-    if (write && vec) hipLaunchKernelGGL((kv_write_kernel<E, N, true>), grid, block, 0, st, a);
-    else if (write) hipLaunchKernelGGL((kv_write_kernel<E, N, false>), grid, block, 0, st, a);
-    else if (vec) hipLaunchKernelGGL((kv_read_kernel<E, N, true>), grid, block, 0, st, a);
-    else hipLaunchKernelGGL((kv_read_kernel<E, N, false>), grid, block, 0, st, a);
+    const dim3 grid(groups), block(16 * LANES);
+    if (write && vec) hipLaunchKernelGGL((kv_write_kernel<E, LANES, N, true>), grid, block, 0, st, a);
+    else if (write) hipLaunchKernelGGL((kv_write_kernel<E, LANES, N, false>), grid, block, 0, st, a);
+    else if (vec) hipLaunchKernelGGL((kv_read_kernel<E, LANES, N, true>), grid, block, 0, st, a);
+    else hipLaunchKernelGGL((kv_read_kernel<E, LANES, N, false>), grid, block, 0, st, a);
 }
 
 template <class E>
 void launch_move(bool write, bool vec, unsigned groups, hipStream_t st, const MoveArgs &a)
 {
-    if (a.cache.head_dim <= 128) launch_move_form<E, 1>(write, vec, groups, st, a);
-    else launch_move_form<E, 2>(write, vec, groups, st, a);
+    if (a.cache.head_dim <= 64) launch_move_form<E, 8, 1>(write, vec, groups, st, a);
+    else if (a.cache.head_dim <= 128) launch_move_form<E, 16, 1>(write, vec, groups, st, a);
+    else launch_move_form<E, 16, 2>(write, vec, groups, st, a);
 }
 
 ngemm_status move_rows(bool write, ngemm_ctx *ctx, const ngemm_kv_cache *cache, int type, int64_t batch, int64_t tokens, Rows k, Rows v,

@@ -229,7 +229,7 @@ __global__ __launch_bounds__(NW * 64, decode_waves_per_simd(D)) void attention_d
             m = most;
         }
         if (__any(vs_now > 64.0f * unit)) {
-            const float top = max_of_rows(max_in_row(vs_now));
+            const float top = max_of_rows(max_of_lanes<16>(vs_now));
             const int e = __builtin_amdgcn_frexp_expf(top);
             per_unit = __builtin_amdgcn_ldexpf(1.0f, -e);
             if (tile > wave) {
@@ -311,7 +311,7 @@ __global__ __launch_bounds__(kJoinThreads) void attention_decode_join_kernel(con
     const int length = min(a.lengths[b], a.max_length), chunks = length > 0 ? (length + a.chunk - 1) / a.chunk : 1;
     float top = -3.0e38f;
     for (int c = tid & 63; c < chunks; c += 64) top = fmaxf(top, parts[(int64_t)c * (PIECES + 1)][0]);
-    top = max_of_rows(max_in_row(top));
+    top = max_of_rows(max_of_lanes<16>(top));
     const int g = tid / PIECES, piece = tid % PIECES;
     f4 sum = (f4)(0.0f);
     float weight = 0.0f;

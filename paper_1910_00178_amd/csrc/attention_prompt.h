@@ -123,7 +123,7 @@ __device__ __forceinline__ void prompt_rows_one_by_one(const PromptArgs &a, cons
                 s = 0.0f;
                 for (int d = 0; d < D; ++d) s += q[d] * E::get(kr[t * a.k.token_stride + d]);
             }
-            const float most = fmaxf(max_of_rows(max_in_row(s)), m), fall = __builtin_amdgcn_exp2f((m - most) * a.scale);
+            const float most = fmaxf(max_of_rows(max_of_lanes<16>(s)), m), fall = __builtin_amdgcn_exp2f((m - most) * a.scale);
             const float w = t < end ? __builtin_amdgcn_exp2f((s - most) * a.scale) : 0.0f;
             float sum = w;
             for (int x = 32; x; x /= 2) sum += __shfl_xor(sum, x);

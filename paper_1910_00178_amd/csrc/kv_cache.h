@@ -173,16 +173,16 @@ __device__ __forceinline__ void store(typename E::T *to, const float (&x)[N])
     }
 }
 
-// Over the 16 lanes of a row.
-template <class T>
-__device__ __forceinline__ T max_in_row(T x)
+// Over aligned groups of 16 or 8 lanes.
+template <int LANES, class T>
+__device__ __forceinline__ T max_of_lanes(T x)
 {
-#define NGEMM_TURN(n) x = max(x, __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), 0x120 + n, 0xf, 0xf, true)))
-    NGEMM_TURN(8);
-    NGEMM_TURN(4);
-    NGEMM_TURN(2);
-    NGEMM_TURN(1);
-#undef NGEMM_TURN
+#define NGEMM_WITH(dpp) x = max(x, __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), dpp, 0xf, 0xf, true)))
+    if constexpr (LANES == 16) NGEMM_WITH(0x140);        // lane 15 - i's
+    NGEMM_WITH(0x141);                                   // of 8 lanes, lane 7 - i's
+    NGEMM_WITH(0x1b);                                    // of 4, lane 3 - i's
+    NGEMM_WITH(0xb1);                                    // of 2, the other's
+#undef NGEMM_WITH
     return x;
 }
 
@@ -229,18 +229,18 @@ __device__ __forceinline__ u2 quantise(const Piece<E> &p, float most, bool finit
     return codes;
 }
 
-// A thread holds N pieces of eight elements of a token of K and of V, 16 lanes a token (N: head_dim / 128, rounded up).  V's codes pass LDS so
-// that a thread holds four tokens of four elements, whose bytes it transposes.
-template <class E, int N, bool VEC>
-__global__ __launch_bounds__(256) void kv_write_kernel(const MoveArgs a)
+// A thread holds N pieces of eight elements of a token of K and of V, LANES lanes a token: 8 for heads of up to 64 elements, else 16.  V's codes
+// pass LDS so that a thread holds four tokens of four elements, whose bytes it transposes.
+template <class E, int LANES, int N, bool VEC>
+__global__ __launch_bounds__(16 * LANES) void kv_write_kernel(const MoveArgs a)
 {
-    __shared__ __align__(16) uint32_t turned[2][16][32 * N + 1];
+    __shared__ __align__(16) uint32_t turned[2][16][2 * LANES * N + 1];
     typedef typename E::T T;
     const int groups = (a.cache.kv_heads + a.heads - 1) / a.heads, head0 = blockIdx.x % groups * a.heads;
     const int D = a.cache.head_dim, tid = threadIdx.x;
     const MoveBlock m(a, blockIdx.x / groups);
     if (m.begin >= m.end) return;
-    const int token = tid >> 4, piece = tid & 15;
+    const int token = tid / LANES, piece = tid % LANES;
     const bool there = token >= m.begin && token < m.end;
     const int64_t head_bytes = (int64_t)a.cache.page_blocks * a.cache.block_bytes();
     Piece<E> x[2][N];
@@ -251,7 +251,7 @@ __global__ __launch_bounds__(256) void kv_write_kernel(const MoveArgs a)
             const T *row = (const T *)r.data + (m.row0 + token) * r.token_stride + head * r.head_stride;
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                const int c = piece + 16 * n;
+                const int c = piece + LANES * n;
                 if (there && 8 * c < D) x[which][n] = load_piece<E, VEC>(row + 8 * c);
                 else x[which][n] = Piece<E>{};
             }
@@ -269,12 +269,12 @@ __global__ __launch_bounds__(256) void kv_write_kernel(const MoveArgs a)
             uint32_t bits = 0;
 #pragma unroll
             for (int n = 0; n < N; ++n) bits = max(bits, most_bits(x[which][n]));
-            bits = max_in_row(bits);
+            bits = max_of_lanes<LANES>(bits);
             const float most = E::of_bits(bits);
             const bool finite = bits < E::kInfinityBits;
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                const int c = piece + 16 * n;
+                const int c = piece + LANES * n;
                 if (8 * c >= D) break;
                 const u2 codes = quantise<E>(x[which][n], most, finite);
                 if (which) {
@@ -287,7 +287,7 @@ __global__ __launch_bounds__(256) void kv_write_kernel(const MoveArgs a)
             if (there && piece == 0) ((float *)(block + 32 * D))[16 * which + token] = finite ? most / 127.0f : __builtin_nanf("");
         }
         __syncthreads();                                 // (the next head writes the other half)
-        for (int i = tid; i < D; i += 256) {             // tokens 4 t .. 4 t + 3 of elements 4 q .. 4 q + 3
+        for (int i = tid; i < D; i += 16 * LANES) {             // tokens 4 t .. 4 t + 3 of elements 4 q .. 4 q + 3
             const int t = i & 3, q = i >> 2;
             uint32_t y[4];
 #pragma unroll
@@ -318,9 +318,9 @@ __device__ __forceinline__ void values4(uint32_t codes, float scale, float *x)
     }
 }
 
-// K: 16 lanes a token, as above.  V: a thread takes four tokens of four elements and transposes their bytes.
-template <class E, int N, bool VEC>
-__global__ __launch_bounds__(256) void kv_read_kernel(const MoveArgs a)
+// K: LANES lanes a token, as above.  V: a thread takes four tokens of four elements and transposes their bytes.
+template <class E, int LANES, int N, bool VEC>
+__global__ __launch_bounds__(16 * LANES) void kv_read_kernel(const MoveArgs a)
 {
     typedef typename E::T T;
     const int groups = (a.cache.kv_heads + a.heads - 1) / a.heads, head0 = blockIdx.x % groups * a.heads;
@@ -329,7 +329,7 @@ __global__ __launch_bounds__(256) void kv_read_kernel(const MoveArgs a)
     if (m.begin >= m.end) return;
     const uint8_t *const block0 = m.block(a);
     const bool there = block0 != nullptr;                // rows of places that do not exist are 0
-    const int token = tid >> 4, piece = tid & 15, t = tid & 3, q = tid >> 2;
+    const int token = tid / LANES, piece = tid % LANES, t = tid & 3, q = tid >> 2;
     for (int head = head0; head < min(head0 + a.heads, a.cache.kv_heads); ++head) {
         const uint8_t *block = block0 + head * ((int64_t)a.cache.page_blocks * a.cache.block_bytes());
         u2 k[N] = {};
@@ -340,7 +340,7 @@ __global__ __launch_bounds__(256) void kv_read_kernel(const MoveArgs a)
             k_scale = ((const float *)(block + 32 * D))[token];
 #pragma unroll
             for (int n = 0; n < N; ++n)
-                if (8 * (piece + 16 * n) < D) k[n] = *(const u2 *)(block + token * D + 8 * (piece + 16 * n));
+                if (8 * (piece + LANES * n) < D) k[n] = *(const u2 *)(block + token * D + 8 * (piece + LANES * n));
             if (tid < D) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) v[j] = *(const uint32_t *)(block + 16 * D + 64 * q + 4 * t + 16 * j);
@@ -351,11 +351,11 @@ __global__ __launch_bounds__(256) void kv_read_kernel(const MoveArgs a)
             T *row = (T *)a.k.data + (m.row0 + token) * a.k.token_stride + head * a.k.head_stride;
 #pragma unroll
             for (int n = 0; n < N; ++n) {
-                if (8 * (piece + 16 * n) >= D) break;
+                if (8 * (piece + LANES * n) >= D) break;
                 float x[8];
                 values4(k[n][0], k_scale, x);
                 values4(k[n][1], k_scale, x + 4);
-                store<E, 8, VEC>(row + 8 * (piece + 16 * n), x);
+                store<E, 8, VEC>(row + 8 * (piece + LANES * n), x);
             }
         }
         if (tid < D) {
