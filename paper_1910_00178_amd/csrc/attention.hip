@@ -202,20 +202,25 @@ bool allow_prompt_form()
 // Copies of 16-byte pieces, a tile's offsets within 31 bits.
 bool rows_in_pieces(const Rows &r) { return in_pieces(r, NGEMM_BF16) && r.token_stride < (1 << 23); }
 
-// Tiles of query rows that any lengths of the sequences can need, and over how many workgroups their keys are split: as many as give every unit one
-// if the rows were spread evenly, of no less than kLeastRun keys of sequences of equal lengths, where the context is long enough for the
-// join (a launch more) to pay.
+// Tiles of query rows that any lengths of the sequences can need; and where these are few and the context is long enough for the join (a launch
+// more) to pay, the units that share out the keys, with the workgroups that this takes: a tile has as many parts as its share of the units,
+// rounded down, but at least one.  Shares follow the lengths on the device: 8 rows behind 20000, 1500, 900, 500, 400 and 300 keys take 36 us, 88
+// with equal shares for all; sequences of equal lengths the same either way.  Two workgroups a unit write twice the parts: 16 heads on one K/V head,
+// 1144 rows, 40 us for 28; 8 rows behind 32768 keys 43 for 38; only 256 rows behind 8192 keys gain, 55 for 60.
 struct PromptCut {
-    int64_t slots, splits;
+    int64_t tiles, slots, units;
     size_t bytes;
 };
 template <class C>
 PromptCut prompt_cut(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t q_tokens, int64_t k_tokens)
 {
     const int64_t rows = q_tokens * (q_heads / kv_heads), tiles = std::max<int64_t>(batch, (rows + C::BM - 1) / C::BM) * kv_heads;
-    PromptCut cut{rows / C::BM + batch, 1, 0};
-    if (k_tokens / batch >= 4 * kLeastRun) cut.splits = std::max<int64_t>(1, std::min(kUnits / tiles, k_tokens / batch / kLeastRun));
-    if (cut.splits > 1) cut.bytes = (size_t)(cut.slots * kv_heads * cut.splits) * C::kPart * 16;
+    PromptCut cut{rows / C::BM + batch, rows / C::BM + batch, 0, 0};
+    if (tiles > kUnits / 2 || k_tokens / batch < 4 * kLeastRun) return cut;
+    static_assert(kUnits / 2 <= kMostSplit, "sequences");
+    cut.units = kUnits;
+    cut.slots += (cut.units + kv_heads - 1) / kv_heads + cut.tiles / 256 + 2;
+    cut.bytes = (size_t)(cut.slots * kv_heads) * C::kPart * 16;
     return cut;
 }
 
@@ -225,13 +230,13 @@ void launch_prompt_form(PromptArgs a, bool vec, void *workspace, hipStream_t st)
     const PromptCut cut = prompt_cut<C>(a.batch, a.q_heads, a.kv_heads, a.q_tokens, a.k_tokens);
     static_assert(C::BM == kPromptRows, "one height of tiles");
     a.slots = (int32_t)cut.slots;
-    a.splits = (int32_t)cut.splits;
+    a.share = (float)cut.units / (float)a.kv_heads;
     a.parts = (f4 *)workspace;
-    const dim3 grid((unsigned)(cut.slots * a.kv_heads * cut.splits)), block(C::NW * 64);
+    const dim3 grid((unsigned)(cut.slots * a.kv_heads)), block(C::NW * 64);
     if (vec) hipLaunchKernelGGL((attention_prompt_kernel<E, C, true>), grid, block, C::kLds, st, a);
     else hipLaunchKernelGGL((attention_prompt_kernel<E, C, false>), grid, block, C::kLds, st, a);
-    if (cut.splits == 1) return;
-    const dim3 pieces((unsigned)(cut.slots * a.kv_heads * (C::DP / 8))), threads(C::BM * 2);
+    if (cut.units == 0) return;
+    const dim3 pieces((unsigned)(cut.tiles * a.kv_heads * (C::DP / 8))), threads(C::BM * 2);
     if (vec) hipLaunchKernelGGL((attention_prompt_join_kernel<E, C, true>), pieces, threads, 0, st, a);
     else hipLaunchKernelGGL((attention_prompt_join_kernel<E, C, false>), pieces, threads, 0, st, a);
 }

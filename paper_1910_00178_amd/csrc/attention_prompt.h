@@ -10,12 +10,13 @@ struct PromptArgs {
     int32_t batch, q_heads, kv_heads, head_dim, q_tokens, k_tokens, causal;
     float scale;             // of the scores, times log2 e; not negative (Q's sign is turned instead)
     uint32_t q_xor;
-    int32_t slots;           // tiles of query rows that the grid has room for
-    int32_t splits;          // workgroups that may share a tile's keys
-    f4 *parts;               // splits > 1: [slots][kv_heads][splits] times kPart
+    int32_t slots;           // workgroups of a K/V head
+    float share;             // of the units, where the keys are split: a K/V head's; else 0
+    f4 *parts;               // keys split: [slots][kv_heads] times kPart
 };
 
 constexpr int kLeastRun = 256;                                   // keys of a workgroup where a tile's are split
+constexpr int kMostSplit = 128;                                  // sequences of a call that are
 
 // DP: head_dim rounded up; RW groups of 32 rows, each of KS wavefronts that share out the BN keys of a tile; PER_CU workgroups to a unit.
 template <int DP_, int RW_, int KS_, int BN_, int PER_CU_>
@@ -68,32 +69,107 @@ __device__ __forceinline__ void copy_to_lds(Buffer from, uint32_t lds_at, uint32
 }
 __device__ __forceinline__ void copies_landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
+// Sums over a wavefront's lanes up to and with each.
+template <class T>
+__device__ __forceinline__ T sums_up_to(T x)
+{
+#define NGEMM_WITH(dpp, rows) x += __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), dpp, rows, 0xf, true))
+    NGEMM_WITH(0x111, 0xf);                              // in rows of 16 lanes: the lane's 1, 2, 4, 8 before
+    NGEMM_WITH(0x112, 0xf);
+    NGEMM_WITH(0x114, 0xf);
+    NGEMM_WITH(0x118, 0xf);
+    NGEMM_WITH(0x142, 0xa);                              // rows 0 and 2 to the next
+    NGEMM_WITH(0x143, 0xc);                              // row 1 to rows 2 and 3
+#undef NGEMM_WITH
+    return x;
+}
+
 // A tile of a sequence's rows, which are its queries times the heads that share a K/V head, heads fastest.
 template <class C>
 struct PromptTile {
-    int b, q_first, queries, row0, rows, k_first, keys, group, causal;
-    int key_tiles, run, parts;                                   // `parts` workgroups take `run` key tiles each
+    int q_first, queries, row0, rows, k_first, keys, group, causal;
+    int key_tiles, part, parts, part0;                           // `parts` workgroups share out the key tiles; of them this one, and the first one's number
     bool there;
 
-    __device__ __forceinline__ PromptTile(const PromptArgs &a, int slot)
+    // Where a workgroup takes all keys: tile `number`.  Sequence b has the slots floor(rows before it / BM) + b .. : as many as its rows
+    // need or one more.
+    __device__ __forceinline__ PromptTile(const PromptArgs &a, int number) : group(a.q_heads / a.kv_heads), causal(a.causal), part(0), parts(1), part0(0)
     {
-        group = a.q_heads / a.kv_heads;
-        causal = a.causal;
-        // Sequence b has the slots floor(rows before it / BM) + b .. : as many as its rows need or one more.
         int of[4];
-        b = find_sequence(a.batch, slot, {a.q_offsets, a.q_offsets + 1, a.k_offsets, a.k_offsets + 1}, of,
-                          [&](int offset, int x) { return offset * group / C::BM + x; });
+        const int b = find_sequence(a.batch, number, {a.q_offsets, a.q_offsets + 1, a.k_offsets, a.k_offsets + 1}, of,
+                                    [&](int offset, int x) { return offset * group / C::BM + x; });
+        take(a, of);
+        row0 = (number - (of[0] * group / C::BM + b)) * C::BM;
+        there = row0 >= 0 && row0 < rows;
+        key_tiles = tiles_of_keys(min(row0 + C::BM, rows) - 1);
+    }
+    // Where the keys of up to kMostSplit sequences are shared out: workgroup `number` of a head (JOIN: tile `number`).  If each tile took what its
+    // sequence's last one does, which sees the most, all units would have the same; tiles that see less are cut into as many parts.
+    template <int JOIN>
+    __device__ __forceinline__ PromptTile(const PromptArgs &a, int number, Index<JOIN>) : group(a.q_heads / a.kv_heads), causal(a.causal)
+    {
+        constexpr int TURNS = kMostSplit / 64;
+        const int lane = threadIdx.x & 63;
+        int of[TURNS][4] = {}, tiles[TURNS] = {}, most[TURNS] = {};
+        float work = 0.0f;
+#pragma unroll
+        for (int i = 0; i < TURNS; ++i) {
+            if (64 * i >= a.batch) break;
+            const int b = min(64 * i + lane, a.batch - 1);
+            of[i][0] = a.q_offsets[b], of[i][1] = a.q_offsets[b + 1], of[i][2] = a.k_offsets[b], of[i][3] = a.k_offsets[b + 1];
+            take(a, of[i]);
+            tiles[i] = 64 * i + lane < a.batch ? (rows + C::BM - 1) / C::BM : 0;
+            most[i] = tiles_of_keys(rows - 1);
+            work += (float)tiles[i] * (float)most[i];
+        }
+        work = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sums_up_to(work)), 63));
+        const float share = a.share / fmaxf(work, 1.0f);
+        int tile = 0, each = 1, tiles_before = 0, parts_before = 0;
+        part = part0 = 0;
+        there = false;
+#pragma unroll
+        for (int i = 0; i < TURNS; ++i) {
+            if (64 * i >= a.batch) break;
+            // (a whole number of parts may come out as a little less)
+            const int cut = max(1, min((int)((float)most[i] * share + 0x1p-8f), most[i] / (kLeastRun / C::BN))), all = tiles[i] * cut;
+            const int tiles_to = tiles_before + sums_up_to(tiles[i]), parts_to = parts_before + sums_up_to(all);
+            const int begin = JOIN ? tiles_to - tiles[i] : parts_to - all, end = JOIN ? tiles_to : parts_to;
+            const uint64_t here = __ballot(begin <= number && number < end);
+            if (here) {
+                const int l = __builtin_ctzll(here);
+                const int mine[4] = {__builtin_amdgcn_readlane(of[i][0], l), __builtin_amdgcn_readlane(of[i][1], l), __builtin_amdgcn_readlane(of[i][2], l),
+                                     __builtin_amdgcn_readlane(of[i][3], l)};
+                take(a, mine);
+                each = __builtin_amdgcn_readlane(cut, l);
+                const int at = number - __builtin_amdgcn_readlane(begin, l);
+                tile = JOIN ? at : at / each;
+                part = JOIN ? 0 : at % each;
+                part0 = __builtin_amdgcn_readlane(parts_to - all, l) + tile * each;
+                tile = __builtin_amdgcn_readlane(tiles[i], l) - 1 - tile;          // the longest first
+                there = true;
+            }
+            tiles_before = __builtin_amdgcn_readlane(tiles_to, 63);
+            parts_before = __builtin_amdgcn_readlane(parts_to, 63);
+        }
+        row0 = tile * C::BM;
+        key_tiles = there ? tiles_of_keys(min(row0 + C::BM, rows) - 1) : 0;
+        parts = max(1, min(each, key_tiles / (kLeastRun / C::BN)));              // no less than kLeastRun keys a part
+        there = there && part < parts && part0 >= 0 && part0 + parts <= a.slots;  // (places past the end: offsets that fall)
+        // (the same in all lanes, which the compiler does not see)
+        for (int *const x : {&q_first, &queries, &row0, &rows, &k_first, &keys, &key_tiles, &part, &parts, &part0}) *x = __builtin_amdgcn_readfirstlane(*x);
+        there = __builtin_amdgcn_readfirstlane(there);
+    }
+    __device__ __forceinline__ void take(const PromptArgs &a, const int (&of)[4])
+    {
         q_first = min(max(of[0], 0), a.q_tokens);
         queries = min(max(of[1], q_first), a.q_tokens) - q_first;
-        row0 = (slot - (of[0] * group / C::BM + b)) * C::BM;
         rows = queries * group;
-        there = row0 >= 0 && row0 < rows;
         k_first = min(max(of[2], 0), a.k_tokens);
         keys = min(max(of[3], k_first), a.k_tokens) - k_first;
-        key_tiles = max(0, (last_seen(min(row0 + C::BM, rows) - 1) + C::BN) / C::BN);
-        run = a.splits > 1 ? max((key_tiles + a.splits - 1) / a.splits, kLeastRun / C::BN) : key_tiles;
-        parts = a.splits > 1 ? max(1, (key_tiles + run - 1) / run) : 1;
     }
+    __device__ __forceinline__ int tiles_of_keys(int row) const { return row < 0 ? 0 : max(0, (last_seen(row) + C::BN) / C::BN); }
+    __device__ __forceinline__ int first_tile() const { return (int)((int64_t)key_tiles * part / parts); }
+    __device__ __forceinline__ int end_tile() const { return (int)((int64_t)key_tiles * (part + 1) / parts); }
     // the last key that a row sees
     __device__ __forceinline__ int last_seen(int row) const { return causal ? min(row / group + keys - queries, keys - 1) : keys - 1; }
 };
@@ -165,11 +241,10 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
     typedef typename E::T T;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int half = lane >> 5, col = lane & 31, row_group = wave % C::RW, key0 = 32 * KT * (wave / C::RW);   // key0: its first of a tile
-    const int head = blockIdx.x % a.kv_heads, split = blockIdx.x / a.kv_heads % a.splits;
-    const int slot = a.slots - 1 - blockIdx.x / a.kv_heads / a.splits;
+    const int head = blockIdx.x % a.kv_heads, number = blockIdx.x / a.kv_heads;
     const int group = a.q_heads / a.kv_heads, D = a.head_dim;
 
-    const PromptTile<C> tile_of(a, slot);
+    const PromptTile<C> tile_of = a.share > 0.0f ? PromptTile<C>(a, number, Index<0>{}) : PromptTile<C>(a, a.slots - 1 - number);
     const int q_first = tile_of.q_first, row0 = tile_of.row0, rows = tile_of.rows;
     const int k_first = tile_of.k_first, keys = tile_of.keys;
     if (!tile_of.there) return;
@@ -181,9 +256,7 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
     const int wave_first = min(row0 + 32 * row_group, rows - 1), wave_last = min(row0 + 32 * row_group + 31, rows - 1);
     const int seen_by_all = last_seen(wave_first), seen_by_any = last_seen(wave_last);
     const int group_seen_by_all = last_seen(row0);
-    const int parts = tile_of.parts;
-    if (split >= parts) return;
-    const int first_tile = split * tile_of.run, tiles = min(tile_of.key_tiles, first_tile + tile_of.run);
+    const int parts = tile_of.parts, first_tile = tile_of.first_tile(), tiles = tile_of.end_tile();
 
     const T *kbase = (const T *)a.k.data + k_first * a.k.token_stride + head * a.k.head_stride;
     const T *vbase = (const T *)a.v.data + k_first * a.v.token_stride + head * a.v.head_stride;
@@ -369,7 +442,7 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
         }
     }
 
-    f4 *const part = parts > 1 ? a.parts + (((int64_t)slot * a.kv_heads + head) * a.splits + split) * C::kPart : nullptr;
+    f4 *const part = parts > 1 ? a.parts + (int64_t)blockIdx.x * C::kPart : nullptr;
     if (odd) {
         copies_landed();
         __syncthreads();
@@ -447,21 +520,36 @@ __global__ __launch_bounds__(C::BM * 2) void attention_prompt_join_kernel(const 
 {
     typedef typename E::T T;
     constexpr int THREADS = C::BM * 2, PIECES = C::DP / 8;
-    const int piece = blockIdx.x % PIECES, head = blockIdx.x / PIECES % a.kv_heads, slot = blockIdx.x / PIECES / a.kv_heads;
-    const PromptTile<C> tile(a, slot);
+    const int piece = blockIdx.x % PIECES, head = blockIdx.x / PIECES % a.kv_heads;
+    const PromptTile<C> tile(a, blockIdx.x / PIECES / a.kv_heads, Index<1>{});
     const int tid = threadIdx.x, lane = tid & 63, row = tile.row0 + 32 * (tid >> 6) + (lane & 31);
     const int d = 8 * piece + 4 * (lane >> 5);                   // 32 (piece / 4) + 8 (piece % 4) + ..
     if (!tile.there || tile.parts <= 1 || row >= tile.rows || d >= a.head_dim) return;
-    const f4 *from = a.parts + ((int64_t)slot * a.kv_heads + head) * a.splits * C::kPart + tid;
-    float top = -3.0e38f;
-    for (int p = 0; p < tile.parts; ++p) top = fmaxf(top, from[p * C::kPart + PIECES * THREADS][0]);
-    float l = 0.0f;
+    const f4 *from = a.parts + ((int64_t)tile.part0 * a.kv_heads + head) * C::kPart + tid;
+    float top = -3.0e38f, l = 0.0f;
     f4 o = (f4)(0.0f);
-    for (int p = 0; p < tile.parts; ++p) {
-        const f4 stats = from[p * C::kPart + PIECES * THREADS], x = from[p * C::kPart + piece * THREADS];
-        const float fall = __builtin_amdgcn_exp2f((stats[0] - top) * a.scale);
-        l += stats[1] * fall;
-        o += x * fall;
+    for (int p0 = 0; p0 < tile.parts; p0 += 8) {                 // eight on their way together
+        f4 stats[8], x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const f4 *part = from + (int64_t)min(p0 + i, tile.parts - 1) * a.kv_heads * C::kPart;
+            stats[i] = part[PIECES * THREADS];
+            x[i] = part[piece * THREADS];
+        }
+        float now = top;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) now = fmaxf(now, stats[i][0]);
+        const float fall = __builtin_amdgcn_exp2f((top - now) * a.scale);
+        l *= fall;
+        o *= fall;
+        top = now;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const float by = p0 + i < tile.parts ? __builtin_amdgcn_exp2f((stats[i][0] - top) * a.scale) : 0.0f;
+            l += p0 + i < tile.parts ? stats[i][1] * by : 0.0f;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] += p0 + i < tile.parts ? x[i][e] * by : 0.0f;
+        }
     }
     float x[4];
 #pragma unroll

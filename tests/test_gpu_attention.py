@@ -155,6 +155,29 @@ def test_read_rounds_floats(ctx, dtype):
     ng.ngemm_kv_cache_free(c)
 
 
+SHARED_OUT = {                                             # contexts long enough for several workgroups a tile: some long, some empty or short
+    "one long": ([40, 3, 0, 300, 17], [9000, 3, 0, 300, 900]),
+    "long last": ([1, 5, 200], [1, 7, 6000]),
+    "rows without keys": ([130, 9, 4], [0, 5000, 2]),
+    "more rows than keys": ([500, 8], [30, 4000]),
+    "many": ([b % 3 for b in range(70)], [(b * 677) % 3000 if b % 5 else 0 for b in range(70)]),
+    "most": ([1] * 128, [17 * b for b in range(128)]),
+}
+
+
+@pytest.mark.parametrize("causal", [0, 1])
+@pytest.mark.parametrize("lengths", SHARED_OUT)
+@pytest.mark.parametrize("heads", [(1, 1, 16), (3, 1, 96), (4, 1, 256)], ids=lambda h: "x".join(map(str, h)))
+def test_prompt_shares_keys_out(ctx, heads, lengths, causal):
+    """Each tile's parts are as many as its share of the keys of all sequences."""
+    n, m = SHARED_OUT[lengths]
+    assert ng.ngemm_attention_prompt_workspace_bytes(len(n), *heads, sum(n), sum(m)) > 0
+    q, k, v = prompt_rows(len(n), heads, n, m, F16, 1.5)
+    scale = 1 / math.sqrt(heads[2])
+    got = prompt(ctx, q, k, v, n, m, causal, scale)
+    check(got, *prompt_wanted(q, k, v, n, m, causal, scale), F16)
+
+
 def test_prompt_infinities_where_keys_are_split(ctx):
     """As below, in a tile of a split context: one part's workgroup goes row by row, the others do not."""
     heads, n, m = (4, 2, 128), [40], [3000]
