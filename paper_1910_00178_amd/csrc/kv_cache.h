@@ -231,6 +231,10 @@ __device__ __forceinline__ u2 quantise(const Piece<E> &p, float most, bool finit
 
 // A thread holds N pieces of eight elements of a token of K and of V, LANES lanes a token: 8 for heads of up to 64 elements, else 16.  V's codes
 // pass LDS so that a thread holds four tokens of four elements, whose bytes it transposes.
+//
+// Bound by memory: each row is read once, stays in registers while its maximum is found, and leaves as codes.  15800 tokens of 8 heads of 128
+// (bf16): 25 us, 3.9 TB/s read and written, where a large copy reaches 4.85; 64 sequences of a token each 4.7 us, a launch and four trips to
+// memory one behind the other (offsets, page, rows and the stores).
 template <class E, int LANES, int N, bool VEC>
 __global__ __launch_bounds__(16 * LANES) void kv_write_kernel(const MoveArgs a)
 {
@@ -319,6 +323,9 @@ __device__ __forceinline__ void values4(uint32_t codes, float scale, float *x)
 }
 
 // K: LANES lanes a token, as above.  V: a thread takes four tokens of four elements and transposes their bytes.
+//
+// Bound by memory: 39700 tokens of 8 heads of 128 to bf16 53 us, 4.65 TB/s; 46000 of 16 heads of 64 in 64 us, 4.5 TB/s (82 with 16 lanes a token,
+// of which half had nothing); up to 4 x 1000 tokens 5.5 us.
 template <class E, int LANES, int N, bool VEC>
 __global__ __launch_bounds__(16 * LANES) void kv_read_kernel(const MoveArgs a)
 {
