@@ -178,6 +178,27 @@ def test_prompt_shares_keys_out(ctx, heads, lengths, causal):
     check(got, *prompt_wanted(q, k, v, n, m, causal, scale), F16)
 
 
+MANY_TILES = {                                             # more tiles than the chip has room for at once, of several sequences
+    "ragged": ([500, 40, 0, 300, 1, 260, 129], [500, 40, 0, 300, 1, 260, 129]),
+    "equal": ([270] * 4, [270] * 4),
+    "behind": ([10, 600, 64, 500], [700, 601, 64, 900]),
+    "ahead": ([600, 500, 7], [100, 0, 500]),
+    "most": ([20 + b for b in range(64)], [20 + b + 3 * (b % 5) for b in range(64)]),
+}
+
+
+@pytest.mark.parametrize("causal", [0, 1])
+@pytest.mark.parametrize("lengths", MANY_TILES)
+@pytest.mark.parametrize("heads", [(64, 16, 32), (32, 16, 144)], ids=lambda h: "x".join(map(str, h)))
+def test_prompt_more_tiles_than_places(ctx, heads, lengths, causal):
+    n, m = MANY_TILES[lengths]
+    assert ng.ngemm_attention_prompt_workspace_bytes(len(n), *heads, sum(n), sum(m)) == 0
+    q, k, v = prompt_rows(len(n), heads, n, m, BF16, 1.5)
+    scale = 1 / math.sqrt(heads[2])
+    got = prompt(ctx, q, k, v, n, m, causal, scale)
+    check(got, *prompt_wanted(q, k, v, n, m, causal, scale), BF16)
+
+
 def test_prompt_infinities_where_keys_are_split(ctx):
     """As below, in a tile of a split context: one part's workgroup goes row by row, the others do not."""
     heads, n, m = (4, 2, 128), [40], [3000]
