@@ -112,7 +112,10 @@ __global__ __launch_bounds__(NW * 64, decode_waves_per_simd(D)) void attention_d
 #pragma unroll
     for (int t = 0; t < DT; ++t) o[t] = (f4)(0.0f);
     float m = -3.0e38f, l = 0.0f;                        // the row's reference and this lane's part of the sum of its weights
-    float unit = 0x1p-120f, per_unit = 0x1p120f;         // V's scales enter relative to a power of two, 2^6 at most
+    // The second product takes weight times V's scale times f, the row's factor: it follows the largest of these products, not V's scales
+    // alone, so that a token of little weight does not push the others out of float16's range, however large its values.
+    constexpr float kMostFactor = 0x1p120f;
+    float f = kMostFactor;
 
     const int tiles = end > first ? (end - first + 63) / 64 : 0;
     int places = tiles > wave ? look_up(wave) : -1;
@@ -192,7 +195,7 @@ __global__ __launch_bounds__(NW * 64, decode_waves_per_simd(D)) void attention_d
         // ---- scores ----
         const int there = v_place < 0 ? 0 : end - (first + 64 * tile + 16 * g);     // tokens of block g that count
         const float ks_now = h < there ? ks : 0.0f;
-        float vs_now = h < there ? vs : 0.0f;
+        const float vs_now = h < there ? vs : 0.0f;
         f4 s[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -225,34 +228,39 @@ __global__ __launch_bounds__(NW * 64, decode_waves_per_simd(D)) void attention_d
         float most = fmaxf(fmaxf(s[0][0], s[0][1]), s[0][2]);
 #pragma unroll
         for (int i = 3; i < 16; ++i) most = fmaxf(most, s[i / 4][i % 4]);
-        if (__any(most > m + 8.0f)) {                    // weights up to 2^8 fit
-            most = fmaxf(max_of_rows(most), m);
-            if (tile > wave) {                           // (nothing to scale yet in the first tile)
-                const float fall = __builtin_amdgcn_exp2f(m - most);
-                l *= fall;
+        if (__any(most > m)) {                           // weights are 1 at most, and 2^-8 or more for the largest
+            most = max_of_rows(most);
+            const float next = most > m ? most + 8.0f : m, fall = __builtin_amdgcn_exp2f(m - next), grown = f * __builtin_amdgcn_exp2f(next - m);
+            l *= fall;
+            m = next;
+            // the values' sums stay: their weights' factor grows by as much as the weights fall, up to its limit
+            if (tile > wave && __any(grown > kMostFactor)) {
+                const float keep = grown > kMostFactor ? fall * (kMostFactor / f) : 1.0f;
 #pragma unroll
-                for (int t = 0; t < DT; ++t) o[t] *= fall;
+                for (int t = 0; t < DT; ++t) o[t] *= keep;
             }
-            m = most;
+            f = fminf(grown, kMostFactor);
         }
-        if (__any(vs_now > 64.0f * unit)) {
-            const float top = max_of_rows(max_of_lanes<16>(vs_now));
-            const int e = __builtin_amdgcn_frexp_expf(top);
-            per_unit = __builtin_amdgcn_ldexpf(1.0f, -e);
+        float top = 0.0f;
+        unrolled<16>([&](auto i) {
+            constexpr int I = decltype(i)::value;
+            const float x = __builtin_amdgcn_exp2f(s[I / 4][I % 4] - m);
+            l += x;
+            s[I / 4][I % 4] = x * of_row<I>(vs_now);
+            top = fmaxf(top, s[I / 4][I % 4]);
+        });
+        if (__any(top * f > 64.0f)) {                    // (what has been summed then is scaled: not for every small rise)
+            top = max_of_rows(top);
+            const float next = top * f > 64.0f ? __builtin_amdgcn_ldexpf(1.0f, 1 - __builtin_amdgcn_frexp_expf(top)) : f, keep = next / f;
             if (tile > wave) {
 #pragma unroll
-                for (int t = 0; t < DT; ++t) o[t] *= unit * per_unit;
+                for (int t = 0; t < DT; ++t) o[t] *= keep;
             }
-            unit = __builtin_amdgcn_ldexpf(1.0f, e);
+            f = next;
         }
-        vs_now *= per_unit;
         u4 p[2];
-        unrolled<8>([&](auto i) {
-            constexpr int I = 2 * decltype(i)::value;
-            const float x = __builtin_amdgcn_exp2f(s[I / 4][I % 4] - m), y = __builtin_amdgcn_exp2f(s[I / 4][I % 4 + 1] - m);
-            l += x + y;
-            p[I / 8][I % 8 / 2] = pack2<F16>(x * of_row<I>(vs_now), y * of_row<I + 1>(vs_now));
-        });
+#pragma unroll
+        for (int i = 0; i < 16; i += 2) p[i / 8][i % 8 / 2] = pack2<F16>(s[i / 4][i % 4] * f, s[i / 4][i % 4 + 1] * f);
         // ---- values ----
 #pragma unroll
         for (int t = 0; t < DT; ++t) {
@@ -278,7 +286,7 @@ __global__ __launch_bounds__(NW * 64, decode_waves_per_simd(D)) void attention_d
         float *mine = os + (wave * heads + h) * D;
 #pragma unroll
         for (int t = 0; t < DT; ++t)
-            *(f4 *)(mine + 16 * t + 4 * g) = o[t] * (fall * unit);
+            *(f4 *)(mine + 16 * t + 4 * g) = o[t] * (fall / f);
     }
     __syncthreads();
     // a thread's pieces of 4 elements

@@ -1,0 +1,63 @@
+"""Attention over the cache where weights and values lie many powers of two apart."""
+import math
+
+import pytest
+import torch
+
+from attention_ref import check, quantise
+from test_gpu_attention import F16, BF16, ctx, decode, decode_wanted, filled_cache, gen  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+FORMS = {                                                  # lengths and heads: sequences in chunks, and whole ones
+    "chunks": ([300, 64, 700, 1025], (4, 2, 64)),
+    "whole": ([257 + 9 * b for b in range(32)], (8, 4, 64)),
+    "whole, wide": ([400 + 7 * b for b in range(16)], (24, 8, 128)),
+}
+
+
+def put(cache, table, b, at, k, v, v_size=1.0):
+    """Token `at` of sequence b: rows [head][D] of K and V, and V's scales times v_size."""
+    page = cache.shape[1]
+    where = cache.place(int(table[b, at // page]), at % page)
+    codes = cache.views()
+    for x, c, s in ((k, codes[0], codes[2]), (v, codes[1], codes[3])):
+        c[where], s[where] = quantise(x)
+    codes[3][where] = codes[3][where] * v_size
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("ratio", [16, 20, 24, 28, 60])
+@pytest.mark.parametrize("form", FORMS)
+def test_decode_large_values_of_no_weight(ctx, form, ratio, dtype):  # noqa: F811
+    """A token whose values are 2^ratio times the others' and whose weight is some 2^-200 of theirs is without effect."""
+    lengths, (Hq, H, D) = FORMS[form]
+    g = gen(ratio)
+    cache, table = filled_cache(g, lengths, 16, H, D)
+    u = torch.where(torch.rand(D, generator=g) < 0.5, 1.0, -1.0)
+    q = (u + 0.25 * torch.randn(len(lengths), Hq, D, generator=g)).to(dtype)
+    scale = 1 / math.sqrt(D)
+    for b, n in enumerate(lengths):                        # among the first tokens, in the middle, the last one
+        at = (3, n // 2, n - 1)[b % 3]
+        put(cache, table, b, at, (-140 / (scale * D) * u).expand(H, D), torch.randn(H, D, generator=g), 2.0 ** ratio)
+    got = decode(ctx, cache, table, q, lengths, scale)
+    check(got, *decode_wanted(cache, table, q, lengths, scale), dtype, weights=F16)
+
+
+@pytest.mark.parametrize("size", [2.0 ** -110, 2.0 ** -60, 2.0 ** 60, 2.0 ** 110])
+@pytest.mark.parametrize("form", FORMS)
+def test_decode_sizes_of_all_values(ctx, form, size):  # noqa: F811
+    """All values very small or very large, the weights falling from token to token or rising."""
+    lengths, (Hq, H, D) = FORMS[form]
+    g = gen(3)
+    cache, table = filled_cache(g, lengths, 32, H, D)
+    u = torch.where(torch.rand(D, generator=g) < 0.5, 1.0, -1.0)
+    q = (u + 0.05 * torch.randn(len(lengths), Hq, D, generator=g)).to(BF16)
+    scale = 1 / math.sqrt(D)
+    for b, n in enumerate(lengths):
+        for at in range(0, n, 7):
+            put(cache, table, b, at, ((at if b % 2 else n - at) * 100 / n / (scale * D) * u).expand(H, D), torch.randn(H, D, generator=g))
+    cache.views()[3].mul_(size)
+    got = decode(ctx, cache, table, q, lengths, scale)
+    want, bound = decode_wanted(cache, table, q, lengths, scale)
+    check(got.double() / size, want / size, bound / size, BF16, weights=F16)
