@@ -440,8 +440,8 @@ ngemm_status ngemm_kv_read(ngemm_ctx *ctx, const ngemm_kv_cache *cache, ngemm_ty
  * sizes the launch and the workspace: the longest of the lengths.  A
  * sequence without tokens gives 0; tokens in a page that is not one of the cache's are left out.  Softmax
  * statistics and sums are float; the weights p_t times V's scales enter the second product as f16, relative
- * to the largest of these products (a token of no weight does not count, whatever its values).  Scores are products of the 8-bit codes and the query as f16 (bf16 queries relative to a power of
- * two per head).  Long sequences are split over workgroups; the parts meet in the workspace and are joined in their order, so that
+ * to the largest of these products (a token of no weight does not count, whatever its values): 11 bits of each that is at least 2^-38 of the
+ * largest.  Scores are products of the 8-bit codes and the query as f16 (bf16 queries relative to a power of two per head).  Long sequences are split over workgroups; the parts meet in the workspace and are joined in their order, so that
  * equal calls give equal bits.  The workspace has to be 16-byte aligned and must not be in use by a call on another stream.
  */
 size_t ngemm_attention_decode_workspace_bytes(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t max_length);

@@ -15,20 +15,29 @@ struct DecodeArgs {
     int32_t q_pieces, o_pieces;          // whether rows lie at 16-byte multiples
 };
 
-constexpr int decode_waves_per_simd(int D) { return D <= 64 ? 4 : D <= 192 ? 2 : 1; }
+// (what the registers allow; told to the compiler, which otherwise takes some more for the rare branch of the tile loop)
+constexpr int decode_waves_per_simd(int D) { return D <= 64 ? 4 : D <= 96 ? 3 : D <= 192 ? 2 : 1; }
 
 // 16 codes as 16-bit floats, in order.  A code with its sign bit turned, as the low byte under 0x64, is the float 1024 + 128 + code.
-__device__ __forceinline__ void codes_to_f16(u4 x, u4 (&out)[2])
+constexpr uint32_t kCodeSigns = 0x80808080u;
+__device__ __forceinline__ void codes_to_f16(u4 x, u4 (&out)[2], uint32_t signs = kCodeSigns)
 {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const uint32_t y = x[e] ^ 0x80808080u;
+        const uint32_t y = x[e] ^ signs;
         const h2 base = {(_Float16)-1152.0f, (_Float16)-1152.0f};
         const h2 lo = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, y, 0x04010400u)) + base;
         const h2 hi = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, y, 0x04030402u)) + base;
         out[e / 2][2 * (e % 2)] = __builtin_bit_cast(uint32_t, lo);
         out[e / 2][2 * (e % 2) + 1] = __builtin_bit_cast(uint32_t, hi);
     }
+}
+
+// Of two 16-bit floats those without a sign, else 0.
+__device__ __forceinline__ uint32_t positive_halves(uint32_t x)
+{
+    typedef int16_t V2 __attribute__((ext_vector_type(2)));
+    return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(V2, x), (V2)(int16_t)0));
 }
 
 // Lane 16 r + K's value in all lanes 16 r .. 16 r + 15.
@@ -113,7 +122,9 @@ __global__ __launch_bounds__(NW * 64, decode_waves_per_simd(D)) void attention_d
     for (int t = 0; t < DT; ++t) o[t] = (f4)(0.0f);
     float m = -3.0e38f, l = 0.0f;                        // the row's reference and this lane's part of the sum of its weights
     // The second product takes weight times V's scale times f, the row's factor: it follows the largest of these products, not V's scales
-    // alone, so that a token of little weight does not push the others out of float16's range, however large its values.
+    // alone, so that a token of little weight does not push the others out of float16's range, however large its values.  Products so
+    // small that they would lose bits all the same enter apart, so that many of them behind a large one are not lost: 11 bits of each down to 2^-38
+    // of the largest.
     constexpr float kMostFactor = 0x1p120f;
     float f = kMostFactor;
 
@@ -145,21 +156,18 @@ __global__ __launch_bounds__(NW * 64, decode_waves_per_simd(D)) void attention_d
         v_place = __shfl(places, 4 * n + g);
         const uint8_t *kb = a.cache.data + (int64_t)max(k_place, 0) * block_bytes + (h & 3) * D;
         vb = a.cache.data + (int64_t)max(v_place, 0) * block_bytes + 16 * D;
+        ks = *(const float *)(vb + 16 * D + 4 * h);
+        vs = *(const float *)(vb + 16 * D + 64 + 4 * h);
 #pragma unroll
         for (int t = 0; t < 4; ++t)
 #pragma unroll
             for (int j = 0; j < NJ; ++j) k[t][j] = *(const u4 *)(kb + 4 * t * D + min(64 * j + 16 * g, D - 16));
-        ks = *(const float *)(vb + 16 * D + 4 * h);
-        vs = *(const float *)(vb + 16 * D + 64 + 4 * h);
     };
     auto load_values = [&]() {
 #pragma unroll
         for (int t = 0; t < DT; ++t) v[t] = *(const u4 *)(vb + (16 * t + h) * 16);
     };
-    if (wave < tiles) {
-        load_keys(0);
-        load_values();
-    }
+    if (wave < tiles) load_keys(0);
     __builtin_amdgcn_sched_barrier(0);
 
     // Q as f16, relative to a power of two for a bf16 row: its 8 bits are exact there
@@ -192,10 +200,13 @@ __global__ __launch_bounds__(NW * 64, decode_waves_per_simd(D)) void attention_d
         }
     }
     for (int tile = wave, n = 0; tile < tiles; tile += NW) {
+        load_values();
+        __builtin_amdgcn_sched_barrier(0);
         // ---- scores ----
         const int there = v_place < 0 ? 0 : end - (first + 64 * tile + 16 * g);     // tokens of block g that count
-        const float ks_now = h < there ? ks : 0.0f;
-        const float vs_now = h < there ? vs : 0.0f;
+        float ks_now = h < there ? ks : 0.0f, vs_now = h < there ? vs : 0.0f;
+        // (here, so that the next tile's take the registers of this one's: moved at the loop's end, they would be waited for)
+        asm volatile("" : "+v"(ks_now), "+v"(vs_now));
         f4 s[4];
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -220,7 +231,8 @@ __global__ __launch_bounds__(NW * 64, decode_waves_per_simd(D)) void attention_d
             constexpr int I = decltype(i)::value;
             s[I / 4][I % 4] = s[I / 4][I % 4] * of_row<I>(ks_now) * scale;
         });
-        if (!__all(there >= 16)) {
+        const bool whole = __all(there >= 16);
+        if (!whole) {
 #pragma unroll
             for (int i = 0; i < 16; ++i)
                 if (i >= there) s[i / 4][i % 4] = -__builtin_inff();
@@ -241,26 +253,62 @@ __global__ __launch_bounds__(NW * 64, decode_waves_per_simd(D)) void attention_d
             }
             f = fminf(grown, kMostFactor);
         }
-        float top = 0.0f;
+        float top = 0.0f, low = __builtin_inff();
         unrolled<16>([&](auto i) {
             constexpr int I = decltype(i)::value;
             const float x = __builtin_amdgcn_exp2f(s[I / 4][I % 4] - m);
             l += x;
             s[I / 4][I % 4] = x * of_row<I>(vs_now);
             top = fmaxf(top, s[I / 4][I % 4]);
+            low = fminf(low, s[I / 4][I % 4]);
         });
-        if (__any(top * f > 64.0f)) {                    // (what has been summed then is scaled: not for every small rise)
-            top = max_of_rows(top);
-            const float next = top * f > 64.0f ? __builtin_amdgcn_ldexpf(1.0f, 1 - __builtin_amdgcn_frexp_expf(top)) : f, keep = next / f;
-            if (tile > wave) {
+        bool apart = false;
+        if (__any(top * f > 0x1p15f || low * f < 0x1p-14f)) {
+            if (__any(top * f > 0x1p15f)) {              // to 2^12 .. 2^13 (what has been summed then is scaled: not for every small rise)
+                top = max_of_rows(top);
+                const float next = top * f > 0x1p15f ? __builtin_amdgcn_ldexpf(1.0f, 13 - __builtin_amdgcn_frexp_expf(top)) : f, keep = next / f;
+                if (tile > wave) {
 #pragma unroll
-                for (int t = 0; t < DT; ++t) o[t] *= keep;
+                    for (int t = 0; t < DT; ++t) o[t] *= keep;
+                }
+                f = next;
             }
-            f = next;
+            if (!whole) {
+                low = __builtin_inff();
+#pragma unroll
+                for (int i = 0; i < 16; ++i)
+                    if (i < there) low = fminf(low, s[i / 4][i % 4]);
+            }
+            if (__any(low * f < 0x1p-14f)) {             // below float16's normal numbers: apart, times 2^12, and until then marked by the sign
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    const float x = s[i / 4][i % 4];
+                    s[i / 4][i % 4] = x * f < 0x1p-14f ? x * -0x1p12f : x;
+                }
+                apart = true;
+            }
         }
         u4 p[2];
 #pragma unroll
         for (int i = 0; i < 16; i += 2) p[i / 8][i % 8 / 2] = pack2<F16>(s[i / 4][i % 4] * f, s[i / 4][i % 4 + 1] * f);
+        if (__builtin_expect(apart, 0)) {
+            u4 small[2];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t both = p[i / 4][i % 4];
+                small[i / 4][i % 4] = positive_halves(both ^ 0x80008000u);
+                p[i / 4][i % 4] = positive_halves(both);
+            }
+#pragma unroll
+            for (int t = 0; t < DT; ++t) {
+                u4 x[2];
+                uint32_t signs = kCodeSigns;
+                asm volatile("" : "+s"(signs));          // (converted again below: all of them kept would be too many registers)
+                codes_to_f16(v[t], x, signs);
+                o[t] = mfma16(x[1], small[1], mfma16(x[0], small[0], o[t] * 0x1p12f)) * 0x1p-12f;
+                __builtin_amdgcn_sched_barrier(0);
+            }
+        }
         // ---- values ----
 #pragma unroll
         for (int t = 0; t < DT; ++t) {
@@ -269,7 +317,6 @@ __global__ __launch_bounds__(NW * 64, decode_waves_per_simd(D)) void attention_d
             o[t] = mfma16(x[0], p[0], o[t]);
             o[t] = mfma16(x[1], p[1], o[t]);
         }
-        if (more) load_values();
     }
 
     // ---- the wavefronts' parts, joined in their order ----

@@ -44,6 +44,22 @@ def test_decode_large_values_of_no_weight(ctx, form, ratio, dtype):  # noqa: F81
     check(got, *decode_wanted(cache, table, q, lengths, scale), dtype, weights=F16)
 
 
+@pytest.mark.parametrize("weight", [-30, -12, 0, 12])
+@pytest.mark.parametrize("form", FORMS)
+def test_decode_large_values_of_some_weight(ctx, form, weight):  # noqa: F811
+    """The same with 2^20 times the values and weights of about 2^weight: sometimes they count, sometimes the others do."""
+    lengths, (Hq, H, D) = FORMS[form]
+    g = gen(100 + weight)
+    cache, table = filled_cache(g, lengths, 32, H, D)
+    u = torch.where(torch.rand(D, generator=g) < 0.5, 1.0, -1.0)
+    q = (u + 0.05 * torch.randn(len(lengths), Hq, D, generator=g)).to(BF16)
+    scale = 1 / math.sqrt(D)
+    for b, n in enumerate(lengths):
+        put(cache, table, b, (n - 1, 3, n // 2)[b % 3], (weight * math.log(2) / (scale * D) * u).expand(H, D), torch.randn(H, D, generator=g), 2.0 ** 20)
+    got = decode(ctx, cache, table, q, lengths, scale)
+    check(got, *decode_wanted(cache, table, q, lengths, scale), BF16, weights=F16)
+
+
 @pytest.mark.parametrize("size", [2.0 ** -110, 2.0 ** -60, 2.0 ** 60, 2.0 ** 110])
 @pytest.mark.parametrize("form", FORMS)
 def test_decode_sizes_of_all_values(ctx, form, size):  # noqa: F811
@@ -61,3 +77,23 @@ def test_decode_sizes_of_all_values(ctx, form, size):  # noqa: F811
     got = decode(ctx, cache, table, q, lengths, scale)
     want, bound = decode_wanted(cache, table, q, lengths, scale)
     check(got.double() / size, want / size, bound / size, BF16, weights=F16)
+
+
+@pytest.mark.parametrize("below", [20.5, 25.2, 30.5])
+@pytest.mark.parametrize("values", ["small", "half", "none"])
+@pytest.mark.parametrize("form", [([40000], (2, 1, 64)), ([2000 - 3 * b for b in range(32)], (8, 4, 64))], ids=["chunks", "whole"])
+def test_decode_many_small_weights(ctx, form, values, below):  # noqa: F811
+    """One token of weight 1, whose values are small or 0 in half of the elements or everywhere, before or behind many of weight 2^-below."""
+    lengths, (Hq, H, D) = form
+    g = gen(17)
+    cache, table = filled_cache(g, lengths, 16, H, D)
+    cache.views()[0].zero_()                               # keys: score 0
+    u = torch.where(torch.rand(D, generator=g) < 0.5, 1.0, -1.0)
+    q = u.expand(len(lengths), Hq, D).to(BF16).contiguous()
+    scale = 1 / math.sqrt(D)
+    for b, n in enumerate(lengths):
+        v = torch.randn(H, D, generator=g)
+        v[:, ::2] *= 0 if values == "half" else 1
+        put(cache, table, b, (0, n - 1, n // 3)[b % 3], (below * math.log(2) / (scale * D) * u).expand(H, D), v, {"small": 2.0 ** -10, "half": 1.0, "none": 0.0}[values])
+    got = decode(ctx, cache, table, q, lengths, scale)
+    check(got, *decode_wanted(cache, table, q, lengths, scale), BF16, weights=F16)
