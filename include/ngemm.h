@@ -458,7 +458,8 @@ ngemm_status ngemm_attention_decode(ngemm_ctx *ctx, const ngemm_kv_cache *cache,
  * [batch + 1] on the device; k_offsets_dev NULL: the same as the queries').  With n queries and m keys, query i sees the
  * keys j <= i + m - n when `causal` is not 0, all of them when it is 0; a query that sees none gives 0, and what the K and V rows that
  * it does not see hold is without effect, infinities and NaN included.  q_heads a multiple of kv_heads, head_dim a multiple of 16 up to 256.
- * Softmax statistics and sums are float; the weights enter the second product in the rows' type.
+ * Softmax statistics and sums are float; the weights enter the second product in the rows' type (f16: 11 bits of each that is at least 2^-25 of the
+ * row's largest; smaller ones are off by up to 2^-36 of it).
  */
 size_t ngemm_attention_prompt_workspace_bytes(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
                                               int64_t q_tokens, int64_t k_tokens);

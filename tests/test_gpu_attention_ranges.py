@@ -1,11 +1,11 @@
-"""Attention over the cache where weights and values lie many powers of two apart."""
+"""Attention where weights and values lie many powers of two apart."""
 import math
 
 import pytest
 import torch
 
 from attention_ref import check, quantise
-from test_gpu_attention import F16, BF16, ctx, decode, decode_wanted, filled_cache, gen  # noqa: F401
+from test_gpu_attention import F16, BF16, ctx, decode, decode_wanted, filled_cache, gen, prompt, prompt_rows, prompt_wanted  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -97,3 +97,37 @@ def test_decode_many_small_weights(ctx, form, values, below):  # noqa: F811
         put(cache, table, b, (0, n - 1, n // 3)[b % 3], (below * math.log(2) / (scale * D) * u).expand(H, D), v, {"small": 2.0 ** -10, "half": 1.0, "none": 0.0}[values])
     got = decode(ctx, cache, table, q, lengths, scale)
     check(got, *decode_wanted(cache, table, q, lengths, scale), BF16, weights=F16)
+
+
+@pytest.mark.parametrize("below", [20.2, 24.2, 30.2])
+@pytest.mark.parametrize("values", ["small", "half", "none"])
+@pytest.mark.parametrize("at", ["first", "middle", "last"])
+@pytest.mark.parametrize("sizes", [(3, 20000, (2, 1, 64)), (70, 1000, (4, 2, 128)), (5, 9000, (2, 1, 256))], ids=lambda s: f"{s[0]}x{s[1]}x{s[2][2]}")
+def test_prompt_many_small_weights(ctx, sizes, at, values, below):  # noqa: F811
+    """float16: one key of weight 1, whose values are small or 0 in half of the elements or everywhere, among many of weight 2^-below."""
+    n, m, heads = sizes
+    q, k, v = prompt_rows(n, heads, [n], [m], F16)
+    u = torch.where(torch.rand(heads[2], generator=gen(1)) < 0.5, 1.0, -1.0)
+    q[:], k[:] = u.to(F16), 0
+    where = {"first": 0, "middle": m // 2, "last": m - 1}[at]
+    k[where] = u.to(F16)
+    v[where] *= 2.0 ** -10 if values == "small" else 0.0 if values == "none" else 1.0
+    v[where, :, ::2] *= 0 if values == "half" else 1
+    scale = below * math.log(2) / heads[2]
+    got = prompt(ctx, q, k, v, [n], [m], 0, scale)
+    want, size = prompt_wanted(q, k, v, [n], [m], 0, scale)
+    if below > 25:                                         # weights on a grid: 2^-36 each, in the bound's units of its factor of size
+        size = size + 2.0 ** -36 / (2.0 ** -11 + 2.0 ** -13) * v.double().abs().sum(0).repeat_interleave(heads[0] // heads[1], 0)
+    check(got, want, size, F16)
+
+
+def test_prompt_parts_row_by_row_in_float16(ctx):  # noqa: F811
+    """One part of a split context goes row by row because of an infinity, the others do not: their sums have the same factor."""
+    heads, n, m = (4, 2, 128), [40], [3000]
+    q, k, v = prompt_rows(2, heads, n, m, F16)
+    want, size = prompt_wanted(q, k, v, n, m, 1, 0.1)
+    v[2990, 1, 7] = math.inf                               # seen by queries 30 .. 39
+    got = prompt(ctx, q, k, v, n, m, 1, 0.1).double()
+    assert bool((got[30:, 2:, 7] == math.inf).all())
+    got[30:, 2:, 7], want[30:, 2:, 7] = 0, 0
+    check(got, want, size, F16)
