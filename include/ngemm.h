@@ -381,7 +381,8 @@ ngemm_status ngemm_run_batched_u8s8s32(ngemm_ctx *ctx, int count, const ngemm_pr
  * quantised into a cache as they are written, and queries attend to them there, or to rows that are not in a cache.
  *
  * Element types of rows (queries, keys, values, outputs).  A token's row of one head is head_dim consecutive
- * elements; tokens and heads lie token_stride and head_stride elements apart, in any order.
+ * elements; tokens and heads lie token_stride and head_stride elements apart, in any order, up to 2^40 each and 2^60 from the first
+ * element to the last.  Sizes that would take more than 2^23 workgroups are refused as NGEMM_ERR_BAD_SHAPE like others that are out of range.
  */
 typedef enum {
     NGEMM_F32 = 0,               /* kv_write and kv_read only */

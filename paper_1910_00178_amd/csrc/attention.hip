@@ -23,7 +23,8 @@ constexpr uint32_t kCacheMagic = 0x4e474b56u;   // "NGKV"
 constexpr int64_t kMaxCount = 0x7fffffff - 4096;
 constexpr int64_t kMaxLength = 1 << 30;         // tokens of a sequence in the cache
 constexpr int64_t kMaxGroups = (1 << 23) - 1;   // workgroups of a launch: with 512 threads each, a launch counts threads in 32 bits
-constexpr int64_t kMaxStride = 1ll << 40;       // elements; products with a row's number stay within 64 bits
+constexpr int64_t kMaxStride = 1ll << 40;       // elements
+constexpr int64_t kMaxReach = 1ll << 60;        // elements from the first row's first to the last row's last: in bytes within 63 bits
 
 bool cache_ok(const ngemm_kv_cache *c) { return c && c->magic == kCacheMagic; }
 
@@ -36,8 +37,9 @@ ngemm_status check_rows(const Rows &r, int type, int64_t tokens, int64_t heads, 
 {
     if (tokens == 0) return NGEMM_OK;
     if (!r.data || ((uintptr_t)r.data & (elem_bytes(type) - 1)) != 0) return NGEMM_ERR_INVALID_ARG;
-    const int64_t t = r.token_stride, h = r.head_stride;
+    const __int128 t = r.token_stride, h = r.head_stride;
     if (t < 0 || h < 0 || t > kMaxStride || h > kMaxStride) return NGEMM_ERR_BAD_SHAPE;
+    if ((tokens - 1) * t + (heads - 1) * h + head_dim > kMaxReach) return NGEMM_ERR_BAD_SHAPE;
     if (written) {                                       // no two elements at one place: heads inside tokens or tokens inside heads
         const bool heads_inside = (heads == 1 || h >= head_dim) && (tokens == 1 || t >= (heads - 1) * h + head_dim);
         const bool tokens_inside = (tokens == 1 || t >= head_dim) && (heads == 1 || h >= (tokens - 1) * t + head_dim);

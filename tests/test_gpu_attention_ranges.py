@@ -1,11 +1,12 @@
-"""Attention where weights and values lie many powers of two apart."""
+"""Attention where weights and values lie many powers of two apart, and rows too far apart."""
 import math
 
 import pytest
 import torch
 
+import paper_1910_00178_amd as ng
 from attention_ref import check, quantise
-from test_gpu_attention import F16, BF16, ctx, decode, decode_wanted, filled_cache, gen, prompt, prompt_rows, prompt_wanted  # noqa: F401
+from test_gpu_attention import F16, BF16, ctx, decode, decode_wanted, filled_cache, gen, prompt, prompt_rows, prompt_wanted, refused  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -131,3 +132,22 @@ def test_prompt_parts_row_by_row_in_float16(ctx):  # noqa: F811
     assert bool((got[30:, 2:, 7] == math.inf).all())
     got[30:, 2:, 7], want[30:, 2:, 7] = 0, 0
     check(got, want, size, F16)
+
+
+def test_rows_too_far_apart(ctx):  # noqa: F811
+    """Strides whose products with the rows' number pass 63 bits are refused, whether rows are read or written, before anything is launched."""
+    D, H, far = 64, 8, 1 << 40
+    size = ng.ngemm_kv_cache_bytes(4, 16, H, D)
+    buf = torch.zeros(size, dtype=torch.uint8, device="cuda")
+    c = ng.ngemm_kv_cache_create(ctx, 4, 16, H, D, buf, size)
+    x = torch.zeros(16, H, D, dtype=BF16, device="cuda")
+    pages, off = torch.zeros(1, 1, dtype=torch.int32, device="cuda"), torch.tensor([0, 16], dtype=torch.int32, device="cuda")
+    for tokens in ((1 << 20) + 1, (1 << 23) + 1):          # 2^60 and some; 2^63: as 64 bits with a sign the heads seemed to lie behind each other
+        for head_stride in (0, D, far):
+            refused(ng.NGEMM_ERR_BAD_SHAPE, ng.ngemm_kv_read, ctx, c, ng.NGEMM_BF16, 1, tokens, x, far, head_stride, x, H * D, D, off, None, pages, 1)
+            refused(ng.NGEMM_ERR_BAD_SHAPE, ng.ngemm_kv_write, ctx, c, ng.NGEMM_BF16, 1, tokens, x, H * D, D, x, far, head_stride, off, None, pages, 1)
+            refused(ng.NGEMM_ERR_BAD_SHAPE, ng.ngemm_attention_prompt, ctx, ng.NGEMM_BF16, 1, H, H, D, tokens, x, H * D, D, tokens, x, far, head_stride, x, H * D, D,
+                    off, None, 1, 0.1, x, H * D, D)
+    torch.cuda.synchronize()
+    assert not buf.any() and not x.any()
+    ng.ngemm_kv_cache_free(c)
