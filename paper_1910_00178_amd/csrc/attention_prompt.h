@@ -71,11 +71,15 @@ __device__ __forceinline__ Buffer buffer_of(const void *from, int bytes)
     return (Buffer){(uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)at), (uint32_t)__builtin_amdgcn_readfirstlane((int)(uint32_t)(at >> 32)) & 0xffffu,
                     (uint32_t)__builtin_amdgcn_readfirstlane(bytes), 0x00020000u};
 }
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
 __device__ __forceinline__ void copy_to_lds(Buffer from, uint32_t lds_at, uint32_t offset)
 {
-    // (five wait states: what a vector instruction that wrote the descriptor's registers needs; M0 needs one)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane((int)lds_at)), "v"(offset), "s"(from) : "memory");
+    // (M0 is the compiler's as well, for what it makes itself of LDS copies and indexes: named, so that it keeps no value there.  It warns that the
+    // register is one of its reserved ones, which is the reason.  Five wait states: what a vector instruction that wrote the descriptor's registers needs; M0 needs one.)
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(__builtin_amdgcn_readfirstlane((int)lds_at)), "v"(offset), "s"(from) : "memory", "m0");
 }
+#pragma clang diagnostic pop
 __device__ __forceinline__ void copies_landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
 // Sums over a wavefront's lanes up to and with each.
