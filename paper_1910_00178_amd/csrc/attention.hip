@@ -5,6 +5,7 @@
 #include "attention_prompt.h"
 
 #include <algorithm>
+#include <atomic>
 #include <cmath>
 #include <new>
 
@@ -136,11 +137,17 @@ DecodeCut decode_cut(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t h
     return cut;
 }
 
-template <class E, int D, int NW>
-hipError_t allow_decode_lds()
+// LDS beyond 64 KiB is asked for once per kernel and device, before its first launch: programs that only multiply pay nothing for it.
+template <class KERNEL, int BYTES, class F>
+bool allow_lds(int device, F kernel)
 {
-    void (*const kernel)(DecodeArgs) = attention_decode_kernel<E, D, NW>;
-    return hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, NW * (32 + 16 * D) * 4);
+    if constexpr (BYTES <= 65536) return true;
+    static std::atomic<uint64_t> allowed{0};             // devices; others ask each time
+    const uint64_t mine = device < 64 ? 1ull << device : 0;
+    if (allowed.load(std::memory_order_acquire) & mine) return true;
+    if (hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, BYTES) != hipSuccess) return false;
+    allowed.fetch_or(mine, std::memory_order_release);
+    return true;
 }
 
 // f(Index<head_dim>{})
@@ -151,26 +158,34 @@ void with_head_dim(int64_t head_dim, F &&f)
     else if constexpr (D > 16) with_head_dim<D - 16>(head_dim, f);
 }
 
+template <class E, int D, int NW> struct DecodeForm {};
 template <class E, int D, int NW>
-void launch_decode_form(const DecodeArgs &a, hipStream_t st)
+bool launch_decode_form(const DecodeArgs &a, int device, hipStream_t st)
 {
     const int group = a.q_heads / a.cache.kv_heads;
     const unsigned grid = (unsigned)((int64_t)a.batch * a.cache.kv_heads * ((group + 15) / 16) * a.chunks);
-    const size_t lds = (size_t)NW * (32 + std::min(group, 16) * D) * 4;
-    hipLaunchKernelGGL((attention_decode_kernel<E, D, NW>), dim3(grid), dim3(NW * 64), lds, st, a);
+    const auto lds = [](int heads) constexpr { return NW * (32 + heads * D) * 4; };
+    if (!allow_lds<DecodeForm<E, D, NW>, lds(16)>(device, attention_decode_kernel<E, D, NW>)) return false;
+    hipLaunchKernelGGL((attention_decode_kernel<E, D, NW>), dim3(grid), dim3(NW * 64), (size_t)lds(std::min(group, 16)), st, a);
     if (a.chunks > 1) hipLaunchKernelGGL((attention_decode_join_kernel<E, D>), dim3((unsigned)(a.batch * a.q_heads)), dim3(kJoinThreads), 0, st, a);
+    return true;
 }
 
 template <class E>
-void launch_decode(const DecodeArgs &a, int64_t waves, hipStream_t st)
+bool launch_decode(const DecodeArgs &a, int64_t waves, int device, hipStream_t st)
 {
+    bool ok = false;
     with_head_dim(a.cache.head_dim, [&](auto dim) {
         constexpr int D = decltype(dim)::value;
         if constexpr (D <= kWideHeadDim) {
-            if (waves == 8) return launch_decode_form<E, D, 8>(a, st);
+            if (waves == 8) {
+                ok = launch_decode_form<E, D, 8>(a, device, st);
+                return;
+            }
         }
-        launch_decode_form<E, D, 4>(a, st);
+        ok = launch_decode_form<E, D, 4>(a, device, st);
     });
+    return ok;
 }
 
 // ---- prompts ----
@@ -186,19 +201,6 @@ void with_prompt_form(int64_t head_dim, F &&f)
     else if (head_dim <= 128) f(PromptCfg<128, 4, 1, 64, 2>{});
     else if (head_dim <= 192) f(PromptCfg<192, 4, 2, 64, 1>{});
     else f(PromptCfg<256, 4, 2, 64, 1>{});
-}
-
-template <class E, class C, bool VEC>
-hipError_t allow_prompt_lds()
-{
-    return hipFuncSetAttribute((const void *)attention_prompt_kernel<E, C, VEC>, hipFuncAttributeMaxDynamicSharedMemorySize, C::kLds);
-}
-
-template <class C>
-bool allow_prompt_form()
-{
-    return allow_prompt_lds<F16, C, true>() == hipSuccess && allow_prompt_lds<F16, C, false>() == hipSuccess &&
-           allow_prompt_lds<BF16, C, true>() == hipSuccess && allow_prompt_lds<BF16, C, false>() == hipSuccess;
 }
 
 // Copies of 16-byte pieces, a tile's offsets within 31 bits.
@@ -226,44 +228,34 @@ PromptCut prompt_cut(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t q
     return cut;
 }
 
-template <class E, class C>
-void launch_prompt_form(PromptArgs a, bool vec, void *workspace, hipStream_t st)
+template <class E, class C, bool VEC> struct PromptForm {};
+template <class E, class C, bool VEC>
+bool launch_prompt_form(const PromptArgs &a, const PromptCut &cut, int device, hipStream_t st)
 {
-    const PromptCut cut = prompt_cut<C>(a.batch, a.q_heads, a.kv_heads, a.q_tokens, a.k_tokens);
-    static_assert(C::BM == kPromptRows, "one height of tiles");
-    a.slots = (int32_t)cut.slots;
-    a.share = (float)cut.units / (float)a.kv_heads;
-    a.parts = (f4 *)workspace;
-    const dim3 grid((unsigned)(cut.slots * a.kv_heads)), block(C::NW * 64);
-    if (vec) hipLaunchKernelGGL((attention_prompt_kernel<E, C, true>), grid, block, C::kLds, st, a);
-    else hipLaunchKernelGGL((attention_prompt_kernel<E, C, false>), grid, block, C::kLds, st, a);
-    if (cut.units == 0) return;
-    const dim3 pieces((unsigned)(cut.tiles * a.kv_heads * (C::DP / 8))), threads(C::BM * 2);
-    if (vec) hipLaunchKernelGGL((attention_prompt_join_kernel<E, C, true>), pieces, threads, 0, st, a);
-    else hipLaunchKernelGGL((attention_prompt_join_kernel<E, C, false>), pieces, threads, 0, st, a);
+    if (!allow_lds<PromptForm<E, C, VEC>, C::kLds>(device, attention_prompt_kernel<E, C, VEC>)) return false;
+    hipLaunchKernelGGL((attention_prompt_kernel<E, C, VEC>), dim3((unsigned)(cut.slots * a.kv_heads)), dim3(C::NW * 64), C::kLds, st, a);
+    if (cut.units > 0)
+        hipLaunchKernelGGL((attention_prompt_join_kernel<E, C, VEC>), dim3((unsigned)(cut.tiles * a.kv_heads * (C::DP / 8))), dim3(C::BM * 2), 0, st, a);
+    return true;
 }
 
 template <class E>
-void launch_prompt(const PromptArgs &a, bool vec, void *workspace, hipStream_t st)
+bool launch_prompt(PromptArgs a, bool vec, void *workspace, int device, hipStream_t st)
 {
-    with_prompt_form(a.head_dim, [&](auto form) { launch_prompt_form<E, decltype(form)>(a, vec, workspace, st); });
+    bool ok = false;
+    with_prompt_form(a.head_dim, [&](auto form) {
+        typedef decltype(form) C;
+        static_assert(C::BM == kPromptRows, "one height of tiles");
+        const PromptCut cut = prompt_cut<C>(a.batch, a.q_heads, a.kv_heads, a.q_tokens, a.k_tokens);
+        a.slots = (int32_t)cut.slots;
+        a.share = (float)cut.units / (float)a.kv_heads;
+        a.parts = (f4 *)workspace;
+        ok = vec ? launch_prompt_form<E, C, true>(a, cut, device, st) : launch_prompt_form<E, C, false>(a, cut, device, st);
+    });
+    return ok;
 }
 
 }  // namespace
-
-bool ngemm::attention_setup()
-{
-    bool ok = true;
-    for (int64_t d = 16; d <= 256; d += 16)
-        with_head_dim(d, [&](auto dim) {
-            constexpr int D = decltype(dim)::value;
-            ok = ok && allow_decode_lds<F16, D, 4>() == hipSuccess && allow_decode_lds<BF16, D, 4>() == hipSuccess;
-            if constexpr (D <= kWideHeadDim) ok = ok && allow_decode_lds<F16, D, 8>() == hipSuccess && allow_decode_lds<BF16, D, 8>() == hipSuccess;
-        });
-    for (int64_t d : {64, 96, 128, 192, 256})
-        with_prompt_form(d, [&](auto form) { ok = ok && allow_prompt_form<decltype(form)>(); });
-    return ok;
-}
 
 extern "C" {
 
@@ -357,9 +349,8 @@ ngemm_status ngemm_attention_decode(ngemm_ctx *ctx, const ngemm_kv_cache *cache,
     const DecodeArgs a{view_of(cache, pages_dev, pages_stride), q, o, lengths_dev, (int32_t)batch, (int32_t)q_heads, (int32_t)max_length,
                        (int32_t)cut.chunk, (int32_t)cut.chunks, scale * 1.44269504f, (f4 *)workspace_dev, in_pieces(q, type), in_pieces(o, type)};
     hipStream_t st = (hipStream_t)hip_stream;
-    if (type == NGEMM_F16) launch_decode<F16>(a, cut.waves, st);
-    else launch_decode<BF16>(a, cut.waves, st);
-    return launched();
+    const bool ok = type == NGEMM_F16 ? launch_decode<F16>(a, cut.waves, ctx->device, st) : launch_decode<BF16>(a, cut.waves, ctx->device, st);
+    return ok ? launched() : NGEMM_ERR_DEVICE;
 }
 
 size_t ngemm_attention_prompt_workspace_bytes(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
@@ -410,9 +401,8 @@ ngemm_status ngemm_attention_prompt(ngemm_ctx *ctx, ngemm_type type, int64_t bat
                        (int32_t)head_dim, (int32_t)q_tokens, (int32_t)k_tokens, causal != 0, scale2, std::signbit(scale) ? 0x80008000u : 0u, 0, 0, nullptr};
     const bool vec = rows_in_pieces(q) && rows_in_pieces(k) && rows_in_pieces(v) && rows_in_pieces(o);
     hipStream_t st = (hipStream_t)hip_stream;
-    if (type == NGEMM_F16) launch_prompt<F16>(a, vec, workspace_dev, st);
-    else launch_prompt<BF16>(a, vec, workspace_dev, st);
-    return launched();
+    const bool ok = type == NGEMM_F16 ? launch_prompt<F16>(a, vec, workspace_dev, ctx->device, st) : launch_prompt<BF16>(a, vec, workspace_dev, ctx->device, st);
+    return ok ? launched() : NGEMM_ERR_DEVICE;
 }
 
 }  // extern "C"

@@ -1253,8 +1253,7 @@ ngemm_status ngemm_create(ngemm_ctx **out, int device_ordinal)
             allow_big_lds_wavek_far<WaveK12, 2, false>() != hipSuccess || allow_big_lds_wavek_far<WaveK12, 1, false>() != hipSuccess ||
             allow_big_lds_wavek_far<WaveK12, 1, true>() != hipSuccess || allow_big_lds_wavek_far<WaveK12, 1, false, true>() != hipSuccess ||
             allow_big_lds_mid<Mid256>() != hipSuccess || allow_big_lds_mid<Mid192>() != hipSuccess || allow_big_lds_mid<Mid128>() != hipSuccess ||
-            allow_big_lds_mid<Mid64x192>() != hipSuccess || allow_big_lds_mid<Mid64x128>() != hipSuccess ||
-            !attention_setup()) {
+            allow_big_lds_mid<Mid64x192>() != hipSuccess || allow_big_lds_mid<Mid64x128>() != hipSuccess) {
             delete c;
             return NGEMM_ERR_DEVICE;
         }

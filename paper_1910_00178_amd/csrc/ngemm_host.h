@@ -28,9 +28,6 @@ constexpr uint32_t kCtxMagic = 0x4e47454du;   // "NGEM"
 
 inline bool ctx_ok(const ngemm_ctx *c) { return c && c->magic == kCtxMagic; }
 
-// LDS sizes of the attention kernels, for the current device.
-bool attention_setup();
-
 struct DeviceGuard {
     int prev = -1;
     bool ok = false;
