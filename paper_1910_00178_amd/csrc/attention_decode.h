@@ -172,7 +172,7 @@ __global__ __launch_bounds__(NW * 64, decode_waves_per_simd(D)) void attention_d
 
     // Q as f16, relative to a power of two for a bf16 row: its 8 bits are exact there
     u4 q[2 * NJ];
-    float scale = a.scale;
+    float turned = 1.0f;                                 // the inverse of that power
     {
         int turn = 0;
 #pragma unroll
@@ -188,7 +188,7 @@ __global__ __launch_bounds__(NW * 64, decode_waves_per_simd(D)) void attention_d
                 for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(E::get(x[s][e])));
             most = max_of_rows(most);
             if (most > 0.0f && most < __builtin_inff()) turn = 15 - __builtin_amdgcn_frexp_expf(most);
-            scale = __builtin_amdgcn_ldexpf(scale, -turn);
+            turned = __builtin_amdgcn_ldexpf(1.0f, -turn);
 #pragma unroll
             for (int s = 0; s < 2 * NJ; ++s)
 #pragma unroll
@@ -204,7 +204,8 @@ __global__ __launch_bounds__(NW * 64, decode_waves_per_simd(D)) void attention_d
         __builtin_amdgcn_sched_barrier(0);
         // ---- scores ----
         const int there = v_place < 0 ? 0 : end - (first + 64 * tile + 16 * g);     // tokens of block g that count
-        float ks_now = h < there ? ks : 0.0f, vs_now = h < there ? vs : 0.0f;
+        // (with the call's scale first, then the row's power: a score's factor is of a size between theirs, whatever those of queries and keys)
+        float ks_now = h < there ? ks * a.scale : 0.0f, vs_now = h < there ? vs : 0.0f;
         // (here, so that the next tile's take the registers of this one's: moved at the loop's end, they would be waited for)
         asm volatile("" : "+v"(ks_now), "+v"(vs_now));
         f4 s[4];
@@ -229,7 +230,7 @@ __global__ __launch_bounds__(NW * 64, decode_waves_per_simd(D)) void attention_d
         }
         unrolled<16>([&](auto i) {
             constexpr int I = decltype(i)::value;
-            s[I / 4][I % 4] = s[I / 4][I % 4] * of_row<I>(ks_now) * scale;
+            s[I / 4][I % 4] = s[I / 4][I % 4] * (of_row<I>(ks_now) * turned);
         });
         const bool whole = __all(there >= 16);
         if (!whole) {

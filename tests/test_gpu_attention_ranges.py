@@ -151,3 +151,17 @@ def test_rows_too_far_apart(ctx):  # noqa: F811
     torch.cuda.synchronize()
     assert not buf.any() and not x.any()
     ng.ngemm_kv_cache_free(c)
+
+
+@pytest.mark.parametrize("power", [-115, -100, 100, 115])
+@pytest.mark.parametrize("form", FORMS)
+def test_decode_sizes_of_queries_and_keys(ctx, form, power):  # noqa: F811
+    """Keys of any size and bfloat16 queries of the inverse one: scores as ever."""
+    lengths, (Hq, H, D) = FORMS[form]
+    g = gen(power + 200)
+    cache, table = filled_cache(g, lengths, 32, H, D)
+    cache.views()[2].mul_(2.0 ** power)
+    q = (torch.randn(len(lengths), Hq, D, generator=g).double() * 2.0 ** -power).to(BF16)
+    scale = 1 / math.sqrt(D)
+    got = decode(ctx, cache, table, q, lengths, scale)
+    check(got, *decode_wanted(cache, table, q, lengths, scale), BF16, weights=F16)
