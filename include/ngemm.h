@@ -438,7 +438,7 @@ ngemm_status ngemm_kv_read(ngemm_ctx *ctx, const ngemm_kv_cache *cache, ngemm_ty
  *     O[b][h] = sum_t p_t V_t / sum_t p_t,  p_t = exp(scale <Q[b][h], K_t> - max),  t < lengths[b],
  * with the K and V of head h / (q_heads / kv_heads) (q_heads a multiple of the cache's kv_heads).  lengths_dev: int32
  * [batch], the tokens of each sequence in the cache, the new one included; at most max_length (up to 2^30) of them are read, which also
- * sizes the launch and the workspace: the longest of the lengths.  A
+ * sizes the launch and the workspace: the longest of the lengths (a larger number is right as well, and slower: sequences are cut by it).  A
  * sequence without tokens gives 0; tokens in a page that is not one of the cache's are left out.  Softmax
  * statistics and sums are float; the weights p_t times V's scales enter the second product as f16, relative
  * to the largest of these products (a token of no weight does not count, whatever its values): 11 bits of each that is at least 2^-38 of the
@@ -460,7 +460,8 @@ ngemm_status ngemm_attention_decode(ngemm_ctx *ctx, const ngemm_kv_cache *cache,
  * keys j <= i + m - n when `causal` is not 0, all of them when it is 0; a query that sees none gives 0, and what the K and V rows that
  * it does not see hold is without effect, infinities and NaN included.  q_heads a multiple of kv_heads, head_dim a multiple of 16 up to 256.
  * Softmax statistics and sums are float; the weights enter the second product in the rows' type (f16: 11 bits of each that is at least 2^-25 of the
- * row's largest; smaller ones are off by up to 2^-36 of it).
+ * row's largest; smaller ones are off by up to 2^-36 of it).  Rows of the usual strides and 16-byte alignment (token strides below 2^23) are copied in
+ * 16-byte pieces, others element by element, which takes two to four times as long.
  */
 size_t ngemm_attention_prompt_workspace_bytes(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
                                               int64_t q_tokens, int64_t k_tokens);

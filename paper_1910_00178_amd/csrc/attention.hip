@@ -114,11 +114,12 @@ ngemm_status move_rows(bool write, ngemm_ctx *ctx, const ngemm_kv_cache *cache, 
 // ---- one token per sequence ----
 
 // How a sequence is cut.  Whole, by eight wavefronts, where the sequences and heads give half of the units a workgroup and no wavefront takes more than
-// four tiles: the join, a launch more, costs what the split gains (32 sequences of up to 1000 tokens, 12 heads of 64: 8.7 us whole,
-// 10.8 in chunks of 512; 64 of 2000, 8 K/V heads of 64: 25 and 34; heads of more than 192 have no registers for it: 26.8 and 25.2).  Else in
-// chunks, by four wavefronts: as many as give every unit two workgroups, of 256 to 4096 tokens (8 sequences of 100000 to 131072 tokens: 362 us,
-// with half as long ones 377, with 512 tokens 413; 16 of 8192 with heads of 256: 62 us, with half as long ones 73; only 64 sequences of
-// very different lengths would rather have 1024 tokens: 73 us for 79).
+// four tiles: the join, a launch more, mostly costs more than the split gains (calls back to back: 32 sequences of up to 1000 tokens, 12 heads of 64: 10.0 us whole,
+// 12.2 in chunks; 16 of 2000, 8 K/V heads of 128: 16.7 and 18.2; 64 of 2000, 8 K/V heads of 64: 29.7 and 29.3; but 64 of 500, 8 of 128: 18.2 and 14.6; heads
+// of more than 192 have no registers for it).  Else in chunks, by four wavefronts: as many as give every unit two workgroups, of 256 to 4096 tokens (8
+// sequences of 100000 to 131072 tokens: 365 us, with half as long ones 375, with 1024 tokens 388, with 512 413; 16 of 8192 with heads of
+// 256: 60 us, with half as long ones 68; only 64 sequences of very different lengths would rather have 1024 tokens: 71 us for 77).  The cut follows max_length, not
+// the lengths, which the host does not know: one sequence of 4097 tokens takes 10.6 us where max_length says so and 24 where it says 131072.
 constexpr int64_t kUnits = 256;
 constexpr int kWideHeadDim = 192;
 
@@ -206,11 +207,12 @@ void with_prompt_form(int64_t head_dim, F &&f)
 // Copies of 16-byte pieces, a tile's offsets within 31 bits.
 bool rows_in_pieces(const Rows &r) { return in_pieces(r, NGEMM_BF16) && r.token_stride < (1 << 23); }
 
-// Tiles of query rows that any lengths of the sequences can need; and where these are few and the context is long enough for the join (a launch
+// Tiles of query rows that any lengths of the sequences can need; and where these are few and the mean context is long enough for the join (a launch
 // more) to pay, the units that share out the keys, with the workgroups that this takes: a tile has as many parts as its share of the units,
 // rounded down, but at least one.  Shares follow the lengths on the device: 8 rows behind 20000, 1500, 900, 500, 400 and 300 keys take 36 us, 88
 // with equal shares for all; sequences of equal lengths the same either way.  Two workgroups a unit write twice the parts: 16 heads on one K/V head,
-// 1144 rows, 40 us for 28; 8 rows behind 32768 keys 43 for 38; only 256 rows behind 8192 keys gain, 55 for 60.
+// 1144 rows, 40 us for 28; 8 rows behind 32768 keys 43 for 38; only 256 rows behind 8192 keys gain, 55 for 60.  Whether keys are split is
+// decided by the mean: 8 rows behind 10000 keys take 24 us alone and 199 in a batch with 15 others behind 200 (8 K/V heads of 128).
 struct PromptCut {
     int64_t tiles, slots, units;
     size_t bytes;

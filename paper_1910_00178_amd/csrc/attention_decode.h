@@ -77,11 +77,12 @@ __device__ __forceinline__ void put_row(const DecodeArgs &a, int b, int qh, int 
 // NW wavefronts of a workgroup take the chunk's tiles in turn, each with a running maximum and sum, merged through LDS at the end.
 //
 // Bound by reading the cache, 2 D + 8 bytes a token and K/V head, read once for all heads that share it, straight to registers: no two
-// wavefronts want the same bytes.  What counts is bytes on their way, so K of the next tile and V of this one are.  8 sequences of 100000
-// to 131072 tokens (8 K/V heads of 128, 32 heads, bf16): 345 us, 5.7 TB/s, where a large read reaches 6.15; 64 sequences of up to
-// 8192: 72 us, 3.9 TB/s, the units' loads unequal; 32 of up to 1000 (12 heads of 64): 8.8 us; one of 4097: 6.5 us, a chain of three
-// trips to memory (length, page, rows) and the tiles behind it.  A wavefront has work for 16 rows whatever the heads that share
-// a K/V head; with one to four of them the matrix instructions idle, which costs nothing here.
+// wavefronts want the same bytes.  What counts is bytes on their way, so K of the next tile and V of this one are (V asked for at the loop's
+// top and not where it ends: the compiler's waits then count K and V apart).  8 sequences of 100000 to 131072 tokens (8 K/V heads of 128, 32 heads,
+// bf16): the kernel alone 342 to 350 us, 5.7 to 5.8 TB/s, where a large read reaches 6.15; 64 sequences of up to 8192: 69 to 71 us, 3.9 to 4.0 TB/s, the
+// workgroups' loads unequal; 32 of up to 1000 (12 heads of 64): 8.5 to 9.4 us; one of 4097: 6.0 to 6.7 us, a chain of three trips to memory (length,
+// page, rows) and the tiles behind it.  A wavefront has work for 16 rows whatever the heads that share a K/V head; with one to four of them the matrix
+// instructions idle, which costs nothing here.
 template <class E, int D, int NW>
 __global__ __launch_bounds__(NW * 64, decode_waves_per_simd(D)) void attention_decode_kernel(const DecodeArgs a)
 {
@@ -361,7 +362,7 @@ __global__ __launch_bounds__(NW * 64, decode_waves_per_simd(D)) void attention_d
 
 // The chunks of a sequence and query head, joined in an order that depends on nothing but their number.  A workgroup per sequence and
 // head; groups of head_dim / 4 lanes take the chunks in turn, four at a time, and the groups' sums are added in their order.
-// 4 to 6 us: a launch and two trips to memory.  (Joined by the last workgroup of a sequence to arrive instead, with a counter and device scope
+// 3.6 to 6.3 us: a launch and two trips to memory.  (Joined by the last workgroup of a sequence to arrive instead, with a counter and device scope
 // stores, a call on 4097 tokens took 20.7 us and not 11.3: every unit waits for its stores.)
 constexpr int kJoinThreads = 512;
 

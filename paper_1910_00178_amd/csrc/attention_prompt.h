@@ -247,15 +247,17 @@ __device__ __forceinline__ void prompt_rows_one_by_one(const PromptArgs &a, cons
 // lane halves per tile, and P^T's operand is what the lane holds, rounded, with the keys in the order in which the transposing LDS
 // reads deliver V.
 //
-// Long prompts are bound by the matrix unit and the power it draws: 8192 tokens, causal, 32 heads on 8 K/V heads of 128 (bf16) 510 to 560 us from box
-// to box, 0.98 to 1.08 PFLOP/s, where a large library product of that type reaches 1.21; the matrix unit is busy for 52 % of the cycles,
-// the clock falls to 2.0 GHz, LDS reads have no bank conflict.  Heads of 64: 0.99 PFLOP/s, 96: 1.06, 192 and 256: 1.02.  Two
-// workgroups of four wavefronts share a unit so that one's softmax runs beside the other's products; heads of more than 128
-// have no registers for that, and there two wavefronts halve a tile's keys.  Neither four tiles in LDS nor the softmax of one tile
-// between the products of the next (535 us for 517) gained anything.
-// Few rows behind a long context are bound by a unit's path from beyond its L2, some 22 GB/s for each unit, and by what the parts write: 96 rows each behind
-// 3900 and 2100 keys (16 heads on 4 of 256, f16) 26.6 us and 10.3 for the join.  The smallest prompts are bound by the launch: 8 of 128
-// tokens (12 heads of 64) 5.6 us.
+// Long prompts are bound by the matrix unit and the power it draws: 8192 tokens, causal, 32 heads on 8 K/V heads of 128 (bf16) 510 to 590 us by the box
+// and what runs beside it (traced launches, alone between host work, are the slow ones), 0.93 to 1.08 PFLOP/s, where a large library product of that type
+// reaches 1.21; the matrix unit is busy for 51 % of the cycles, the clock falls to 2.0 GHz, LDS reads have no bank conflict.  Heads of 64: 0.99 PFLOP/s,
+// 96: 1.06, 192 and 256: 1.02.  Two workgroups of four wavefronts share a unit so that one's softmax runs beside the other's products; heads of more than 128
+// have no registers for that, and there two wavefronts halve a tile's keys (of more than 192 even so six registers do not fit, and one of the reloads, in tiles that are
+// masked, waits for the next tile's copies as well).  Neither four tiles in LDS nor the softmax of one tile between the products of the next (535 us for 517)
+// gained anything.
+// Few rows behind a long context are bound by memory, with what the parts write: 96 rows each behind 3900 and 2100 keys (16 heads on 4 of 256, f16) 26.4 us, in
+// which some 60 MB are read, K and V being 25 (three tiles of rows share a K/V head and mostly fetch its keys each for themselves), and 35 MB of parts written; 10.2
+// for the join, which reads them.  The smallest prompts are bound by the launch: 8 of 128 tokens (12 heads of 64) 5.4 to 6.2 us.
+// Rows that are not at 16-byte multiples go through registers element by element: 2048 tokens of the first heads 211 us for 53.
 template <class E, class C, bool VEC>
 __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_prompt_kernel(const PromptArgs a)
 {
@@ -538,7 +540,7 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_p
 }
 
 // The parts of a tile, joined in their order: a workgroup per tile and piece of 4 elements of a lane.  Bound by reading the parts: 34 MB
-// (252 of 128 rows of 256 elements) 10.3 us, 3.3 TB/s.
+// (252 of 128 rows of 256 elements) 10.2 us, 3.3 TB/s.
 template <class E, class C, bool VEC>
 __global__ __launch_bounds__(C::BM * 2) void attention_prompt_join_kernel(const PromptArgs a)
 {

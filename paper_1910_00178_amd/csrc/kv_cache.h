@@ -233,8 +233,8 @@ __device__ __forceinline__ u2 quantise(const Piece<E> &p, float most, bool finit
 // pass LDS so that a thread holds four tokens of four elements, whose bytes it transposes.
 //
 // Bound by memory: each row is read once, stays in registers while its maximum is found, and leaves as codes.  15800 tokens of 8 heads of 128
-// (bf16): 25 us, 3.9 TB/s read and written, where a large copy reaches 4.85; 64 sequences of a token each 4.7 us, a launch and four trips to
-// memory one behind the other (offsets, page, rows and the stores).
+// (bf16): 25 us, 3.9 TB/s read and written, where a large copy reaches 4.85 (f32 26 us; rows off 16-byte multiples 26 and 29); 64 sequences of a token each
+// 4.7 us, a launch and four trips to memory one behind the other (offsets, page, rows and the stores).
 template <class E, int LANES, int N, bool VEC>
 __global__ __launch_bounds__(16 * LANES) void kv_write_kernel(const MoveArgs a)
 {
@@ -325,7 +325,7 @@ __device__ __forceinline__ void values4(uint32_t codes, float scale, float *x)
 // K: LANES lanes a token, as above.  V: a thread takes four tokens of four elements and transposes their bytes.
 //
 // Bound by memory: 39700 tokens of 8 heads of 128 to bf16 53 us, 4.65 TB/s; 46000 of 16 heads of 64 in 64 us, 4.5 TB/s (82 with 16 lanes a token,
-// of which half had nothing); up to 4 x 1000 tokens 5.5 us.
+// of which half had nothing); up to 4 x 1000 tokens 5.4 us.  15800 of 8 heads of 128: 21 us, 27 to rows off 16-byte multiples; to f32 27 and 31.
 template <class E, int LANES, int N, bool VEC>
 __global__ __launch_bounds__(16 * LANES) void kv_read_kernel(const MoveArgs a)
 {
