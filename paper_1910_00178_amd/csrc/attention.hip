@@ -114,12 +114,12 @@ ngemm_status move_rows(bool write, ngemm_ctx *ctx, const ngemm_kv_cache *cache, 
 // ---- one token per sequence ----
 
 // How a sequence is cut.  Whole, by eight wavefronts, where the sequences and heads give half of the units a workgroup and no wavefront takes more than
-// four tiles: the join, a launch more, mostly costs more than the split gains (calls back to back: 32 sequences of up to 1000 tokens, 12 heads of 64: 10.0 us whole,
-// 12.2 in chunks; 16 of 2000, 8 K/V heads of 128: 16.7 and 18.2; 64 of 2000, 8 K/V heads of 64: 29.7 and 29.3; but 64 of 500, 8 of 128: 18.2 and 14.6; heads
+// four tiles: the join, a launch more, mostly costs more than the split gains (calls back to back: 32 sequences of up to 1000 tokens, 12 heads of 64: 9.5 us whole,
+// 12.0 in chunks; 16 of 2000, 8 K/V heads of 128: 16.7 and 17.7; 64 of 2000, 8 K/V heads of 64: 29.5 and 29.0; but 64 of 500, 8 of 128: 17.6 and 14.1; heads
 // of more than 192 have no registers for it).  Else in chunks, by four wavefronts: as many as give every unit two workgroups, of 256 to 4096 tokens (8
-// sequences of 100000 to 131072 tokens: 365 us, with half as long ones 375, with 1024 tokens 388, with 512 413; 16 of 8192 with heads of
-// 256: 60 us, with half as long ones 68; only 64 sequences of very different lengths would rather have 1024 tokens: 71 us for 77).  The cut follows max_length, not
-// the lengths, which the host does not know: one sequence of 4097 tokens takes 10.6 us where max_length says so and 24 where it says 131072.
+// sequences of 100000 to 131072 tokens: 365 us, with half as long ones 374, with 1024 tokens 387, with 512 409; 16 of 8192 with heads of
+// 256: 60 us, with half as long ones 66; only 64 sequences of very different lengths would rather have 1024 tokens: 71 us for 76).  The cut follows max_length, not
+// the lengths, which the host does not know: one sequence of 4097 tokens takes 9.9 us where max_length says so and 23 where it says 131072.
 constexpr int64_t kUnits = 256;
 constexpr int kWideHeadDim = 192;
 
@@ -349,7 +349,7 @@ ngemm_status ngemm_attention_decode(ngemm_ctx *ctx, const ngemm_kv_cache *cache,
     const DecodeCut cut = decode_cut(batch, q_heads, cache->kv_heads, cache->head_dim, max_length);
     if (batch * q_heads * cut.chunks > kMaxGroups) return NGEMM_ERR_BAD_SHAPE;
     const DecodeArgs a{view_of(cache, pages_dev, pages_stride), q, o, lengths_dev, (int32_t)batch, (int32_t)q_heads, (int32_t)max_length,
-                       (int32_t)cut.chunk, (int32_t)cut.chunks, scale * 1.44269504f, (f4 *)workspace_dev, in_pieces(q, type), in_pieces(o, type)};
+                       (int32_t)cut.chunk, (int32_t)cut.chunks, scale * 1.44269504f, (f4 *)workspace_dev, in_pieces(o, type)};
     hipStream_t st = (hipStream_t)hip_stream;
     const bool ok = type == NGEMM_F16 ? launch_decode<F16>(a, cut.waves, ctx->device, st) : launch_decode<BF16>(a, cut.waves, ctx->device, st);
     return ok ? launched() : NGEMM_ERR_DEVICE;

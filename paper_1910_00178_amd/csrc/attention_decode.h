@@ -12,7 +12,7 @@ struct DecodeArgs {
     int32_t chunk, chunks;   // tokens of a workgroup, workgroups along a sequence
     float scale;             // of the scores, times log2 e
     f4 *parts;               // chunks > 1: [batch][q_heads][chunks] times head_dim / 4 + 1: maximum and weight, sums
-    int32_t q_pieces, o_pieces;          // whether rows lie at 16-byte multiples
+    int32_t o_pieces;        // whether rows of O lie at 16-byte multiples
 };
 
 // (what the registers allow; told to the compiler, which otherwise takes some more for the rare branch of the tile loop)
@@ -79,8 +79,8 @@ __device__ __forceinline__ void put_row(const DecodeArgs &a, int b, int qh, int 
 // Bound by reading the cache, 2 D + 8 bytes a token and K/V head, read once for all heads that share it, straight to registers: no two
 // wavefronts want the same bytes.  What counts is bytes on their way, so K of the next tile and V of this one are (V asked for at the loop's
 // top and not where it ends: the compiler's waits then count K and V apart).  8 sequences of 100000 to 131072 tokens (8 K/V heads of 128, 32 heads,
-// bf16): the kernel alone 342 to 350 us, 5.7 to 5.8 TB/s, where a large read reaches 6.15; 64 sequences of up to 8192: 69 to 71 us, 3.9 to 4.0 TB/s, the
-// workgroups' loads unequal; 32 of up to 1000 (12 heads of 64): 8.5 to 9.4 us; one of 4097: 6.0 to 6.7 us, a chain of three trips to memory (length,
+// bf16): the kernel alone 344 to 348 us, 5.7 to 5.8 TB/s, where a large read reaches 6.15; 64 sequences of up to 8192: 69 to 71 us, 3.9 to 4.0 TB/s, the
+// workgroups' loads unequal; 32 of up to 1000 (12 heads of 64): 8.6 to 9.5 us; one of 4097: 5.7 to 5.9 us, a chain of three trips to memory (length,
 // page, rows) and the tiles behind it.  A wavefront has work for 16 rows whatever the heads that share a K/V head; with one to four of them the matrix
 // instructions idle, which costs nothing here.
 template <class E, int D, int NW>
@@ -132,18 +132,15 @@ __global__ __launch_bounds__(NW * 64, decode_waves_per_simd(D)) void attention_d
     const int tiles = end > first ? (end - first + 63) / 64 : 0;
     int places = tiles > wave ? look_up(wave) : -1;
     // the rows of Q, on their way before the cache's
-    typename E::T x[2 * NJ][8];
+    u4 q[2 * NJ];
     {
-        const int qh = q_head0 + min(h, heads - 1);
+        const int qh = q_head0 + min(h, heads - 1);      // (rows past the heads repeat the last one's and are not written)
         const T *row = (const T *)a.q.data + b * a.q.token_stride + qh * a.q.head_stride;
 #pragma unroll
         for (int s = 0; s < 2 * NJ; ++s) {
             const int d = 64 * (s / 2) + 16 * g + 8 * (s % 2);
             const T *from = row + (d < D ? d : 0);
-            if (a.q_pieces) __builtin_memcpy(x[s], __builtin_assume_aligned(from, 16), 16);
-            else
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[s][e] = from[e];
+            __builtin_memcpy(&q[s], from, 16);           // (one load, also where rows do not lie at 16-byte multiples)
         }
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -168,41 +165,36 @@ __global__ __launch_bounds__(NW * 64, decode_waves_per_simd(D)) void attention_d
 #pragma unroll
         for (int t = 0; t < DT; ++t) v[t] = *(const u4 *)(vb + (16 * t + h) * 16);
     };
-    if (wave < tiles) load_keys(0);
+    load_keys(0);                                        // (without a tile, the first block's: so that Q alone is waited for next, whatever the wavefront has)
     __builtin_amdgcn_sched_barrier(0);
 
     // Q as f16, relative to a power of two for a bf16 row: its 8 bits are exact there
-    u4 q[2 * NJ];
     float turned = 1.0f;                                 // the inverse of that power
-    {
-        int turn = 0;
-#pragma unroll
-        for (int s = 0; s < 2 * NJ; ++s)
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                if (64 * (s / 2) + 16 * g + 8 * (s % 2) >= D || h >= heads) x[s][e] = (T)0.0f;
-        if constexpr (!__is_same(T, _Float16)) {
-            float most = 0.0f;
-#pragma unroll
-            for (int s = 0; s < 2 * NJ; ++s)
-#pragma unroll
-                for (int e = 0; e < 8; ++e) most = fmaxf(most, fabsf(E::get(x[s][e])));
-            most = max_of_rows(most);
-            if (most > 0.0f && most < __builtin_inff()) turn = 15 - __builtin_amdgcn_frexp_expf(most);
-            turned = __builtin_amdgcn_ldexpf(1.0f, -turn);
-#pragma unroll
-            for (int s = 0; s < 2 * NJ; ++s)
-#pragma unroll
-                for (int e = 0; e < 8; e += 2)
-                    q[s][e / 2] = pack2<F16>(__builtin_amdgcn_ldexpf(E::get(x[s][e]), turn), __builtin_amdgcn_ldexpf(E::get(x[s][e + 1]), turn));
-        } else {
-#pragma unroll
-            for (int s = 0; s < 2 * NJ; ++s) __builtin_memcpy(&q[s], x[s], 16);
-        }
-    }
     for (int tile = wave, n = 0; tile < tiles; tile += NW) {
         load_values();
         __builtin_amdgcn_sched_barrier(0);
+        if (tile == wave) {                              // behind all requests of the first tile
+            if constexpr (D % 64 != 0) {
+#pragma unroll
+                for (int s = 2 * NJ - 2; s < 2 * NJ; ++s) q[s] = 64 * (NJ - 1) + 16 * g < D ? q[s] : (u4)(0u);
+            }
+            if constexpr (!__is_same(T, _Float16)) {
+                float most = 0.0f;
+#pragma unroll
+                for (int s = 0; s < 2 * NJ; ++s)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) most = fmaxf(fmaxf(most, fabsf(E::of_bits(q[s][e] & 0xffffu))), fabsf(E::of_bits(q[s][e] >> 16)));
+                most = max_of_rows(most);
+                int turn = 0;
+                if (most > 0.0f && most < __builtin_inff()) turn = 15 - __builtin_amdgcn_frexp_expf(most);
+                turned = __builtin_amdgcn_ldexpf(1.0f, -turn);
+#pragma unroll
+                for (int s = 0; s < 2 * NJ; ++s)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        q[s][e] = pack2<F16>(__builtin_amdgcn_ldexpf(E::of_bits(q[s][e] & 0xffffu), turn), __builtin_amdgcn_ldexpf(E::of_bits(q[s][e] >> 16), turn));
+            }
+        }
         // ---- scores ----
         const int there = v_place < 0 ? 0 : end - (first + 64 * tile + 16 * g);     // tokens of block g that count
         // (with the call's scale first, then the row's power: a score's factor is of a size between theirs, whatever those of queries and keys)
@@ -275,11 +267,13 @@ __global__ __launch_bounds__(NW * 64, decode_waves_per_simd(D)) void attention_d
                 }
                 f = next;
             }
-            if (!whole) {
+            if (!whole) {                                // without the tokens that do not count
+                const float gap = h < there ? 0.0f : __builtin_inff();
                 low = __builtin_inff();
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (i < there) low = fminf(low, s[i / 4][i % 4]);
+                unrolled<16>([&](auto i) {
+                    constexpr int I = decltype(i)::value;
+                    low = fminf(low, s[I / 4][I % 4] + of_row<I>(gap));
+                });
             }
             if (__any(low * f < 0x1p-14f)) {             // below float16's normal numbers: apart, times 2^12, and until then marked by the sign
 #pragma unroll
