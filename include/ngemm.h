@@ -401,8 +401,9 @@ typedef struct ngemm_kv_cache ngemm_kv_cache; /* opaque host descriptor of a cal
  *         K scales float   [16 tokens]
  *         V scales float   [16 tokens]
  * A row is code * scale: per token and head scale = amax / 127 (one division) and code = rint(127 x / amax), ties to
- * even, amax = max |x| over the row.  A row of zeros has scale 0; a row that holds an infinity or a NaN has scale
- * NaN and codes 0, so that it is NaN throughout when it is read.
+ * even, amax = max |x| over the row (f32 rows in float arithmetic: 127 x and the quotient are rounded, and near a tie a
+ * code can be the next one).  A row of zeros has scale 0; a row that holds an infinity or a NaN has scale NaN and codes
+ * 0, so that it is NaN throughout when it is read.
  *
  * ngemm_kv_cache_create describes a buffer (16-byte aligned; its content is left alone: a buffer's pages are written
  * before they are read); the descriptor is a host object owned by the caller until ngemm_kv_cache_free.
@@ -437,13 +438,15 @@ ngemm_status ngemm_kv_read(ngemm_ctx *ctx, const ngemm_kv_cache *cache, ngemm_ty
  * One new token per sequence attends to the cache (f16 or bf16):
  *     O[b][h] = sum_t p_t V_t / sum_t p_t,  p_t = exp(scale <Q[b][h], K_t> - max),  t < lengths[b],
  * with the K and V of head h / (q_heads / kv_heads) (q_heads a multiple of the cache's kv_heads).  lengths_dev: int32
- * [batch], the tokens of each sequence in the cache, the new one included; at most max_length (up to 2^30) of them are read, which also
- * sizes the launch and the workspace: the longest of the lengths (a larger number is right as well, and slower: sequences are cut by it).  A
- * sequence without tokens gives 0; tokens in a page that is not one of the cache's are left out.  Softmax
- * statistics and sums are float; the weights p_t times V's scales enter the second product as f16, relative
- * to the largest of these products (a token of no weight does not count, whatever its values): 11 bits of each that is at least 2^-38 of the
- * largest.  Scores are products of the 8-bit codes and the query as f16 (bf16 queries relative to a power of two per head).  Long sequences are split over workgroups; the parts meet in the workspace and are joined in their order, so that
- * equal calls give equal bits.  The workspace has to be 16-byte aligned and must not be in use by a call on another stream.
+ * [batch], the tokens of each sequence in the cache, the new one included; at most max_length (up to 2^30) of them are
+ * read, which also sizes the launch and the workspace: the longest of the lengths (a larger number is right as well, and
+ * slower: sequences are cut by it).  A sequence without tokens gives 0; tokens in a page that is not one of the cache's
+ * are left out.  Softmax statistics and sums are float; the weights p_t times V's scales enter the second product as
+ * f16, relative to the largest of these products (a token of no weight does not count, whatever its values): 11 bits of
+ * each that is at least 2^-38 of the largest.  Scores are products of the 8-bit codes and the query as f16 (bf16 queries
+ * relative to a power of two per head).  Long sequences are split over workgroups; the parts meet in the workspace and
+ * are joined in their order, so that equal calls give equal bits.  The workspace has to be 16-byte aligned and must not
+ * be in use by a call on another stream.
  */
 size_t ngemm_attention_decode_workspace_bytes(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t max_length);
 ngemm_status ngemm_attention_decode(ngemm_ctx *ctx, const ngemm_kv_cache *cache, ngemm_type type, int64_t batch, int64_t q_heads,
@@ -457,11 +460,12 @@ ngemm_status ngemm_attention_decode(ngemm_ctx *ctx, const ngemm_kv_cache *cache,
  * Whole prompts attend to themselves, or to a longer context that ends with them (f16 or bf16).  Packed sequences: b has
  * the query rows q_offsets[b] .. q_offsets[b + 1] - 1 and the K and V rows k_offsets[b] .. k_offsets[b + 1] - 1 (int32
  * [batch + 1] on the device; k_offsets_dev NULL: the same as the queries').  With n queries and m keys, query i sees the
- * keys j <= i + m - n when `causal` is not 0, all of them when it is 0; a query that sees none gives 0, and what the K and V rows that
- * it does not see hold is without effect, infinities and NaN included.  q_heads a multiple of kv_heads, head_dim a multiple of 16 up to 256.
- * Softmax statistics and sums are float; the weights enter the second product in the rows' type (f16: 11 bits of each that is at least 2^-25 of the
- * row's largest; smaller ones are off by up to 2^-36 of it).  Rows of the usual strides and 16-byte alignment (token strides below 2^23) are copied in
- * 16-byte pieces, others element by element, which takes two to four times as long.
+ * keys j <= i + m - n when `causal` is not 0, all of them when it is 0; a query that sees none gives 0, and what the K and
+ * V rows that it does not see hold is without effect, infinities and NaN included.  q_heads a multiple of kv_heads,
+ * head_dim a multiple of 16 up to 256.  Softmax statistics and sums are float; the weights enter the second product in
+ * the rows' type (f16: 11 bits of each that is at least 2^-25 of the row's largest; smaller ones are off by up to 2^-36
+ * of it).  Rows of the usual strides and 16-byte alignment (token strides below 2^23) are copied in 16-byte pieces, others
+ * element by element, which takes two to four times as long.
  */
 size_t ngemm_attention_prompt_workspace_bytes(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim,
                                               int64_t q_tokens, int64_t k_tokens);

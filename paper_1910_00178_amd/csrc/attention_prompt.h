@@ -247,7 +247,7 @@ __device__ __forceinline__ void prompt_rows_one_by_one(const PromptArgs &a, cons
 // lane halves per tile, and P^T's operand is what the lane holds, rounded, with the keys in the order in which the transposing LDS
 // reads deliver V.
 //
-// Long prompts are bound by the matrix unit and the power it draws: 8192 tokens, causal, 32 heads on 8 K/V heads of 128 (bf16) 510 to 590 us by the box
+// Long prompts are bound by the matrix unit and the power it draws: 8192 tokens, causal, 32 heads on 8 K/V heads of 128 (bf16) 510 to 590 us by the card
 // and what runs beside it (traced launches, alone between host work, are the slow ones), 0.93 to 1.08 PFLOP/s, where a large library product of that type
 // reaches 1.21; the matrix unit is busy for 51 % of the cycles, the clock falls to 2.0 GHz, LDS reads have no bank conflict.  Heads of 64: 0.99 PFLOP/s,
 // 96: 1.06, 192 and 256: 1.02.  Two workgroups of four wavefronts share a unit so that one's softmax runs beside the other's products; heads of more than 128
