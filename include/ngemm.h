@@ -385,7 +385,7 @@ ngemm_status ngemm_run_batched_u8s8s32(ngemm_ctx *ctx, int count, const ngemm_pr
  * element to the last.  Sizes that would take more than 2^23 workgroups are refused as NGEMM_ERR_BAD_SHAPE like others that are out of range.
  */
 typedef enum {
-    NGEMM_F32 = 0,               /* kv_write and kv_read only */
+    NGEMM_F32 = 0,               /* norms, rotations, writes and reads; not attention */
     NGEMM_F16 = 1,
     NGEMM_BF16 = 2
 } ngemm_type;
@@ -435,6 +435,57 @@ ngemm_status ngemm_kv_read(ngemm_ctx *ctx, const ngemm_kv_cache *cache, ngemm_ty
                            const int32_t *pages_dev, int64_t pages_stride, void *hip_stream);
 
 /*
+ * Rotations of rows by their positions, and norms of rows per head, between the projections and the cache or the attention.
+ *
+ * A rotation is a table of angles in device memory, float [positions][dim]: for each position the cosines and behind them the sines of the
+ * dim / 2 pairs of a row (for angles position * base^(-2 i / dim) a few lines fill it, in 64 bits; scaled or interpolated ones are as good).
+ * It turns the first dim elements of a row (a multiple of 16 up to head_dim, at most 256) and leaves the others: pair i is elements i and i + dim / 2
+ * (halves) or 2 i and 2 i + 1 (neighbours), and (a, b) becomes (a cos - b sin, b cos + a sin).  ngemm_rotation_create describes a table
+ * (16-byte aligned, ngemm_rotation_bytes bytes, 0 for sizes that are not allowed; up to 2^30 positions); the descriptor is a host object owned by the
+ * caller until ngemm_rotation_free, and the table has to stay while it is used.
+ */
+typedef enum {
+    NGEMM_PAIRS_HALVES = 0,
+    NGEMM_PAIRS_NEIGHBOURS = 1
+} ngemm_pairs;
+
+typedef struct ngemm_rotation ngemm_rotation; /* opaque host descriptor of a caller-owned device buffer */
+
+size_t ngemm_rotation_bytes(int64_t positions, int64_t dim);
+ngemm_status ngemm_rotation_create(ngemm_ctx *ctx, int64_t positions, int64_t dim, ngemm_pairs pairs, const float *table_dev, size_t table_bytes,
+                                   ngemm_rotation **out);
+ngemm_status ngemm_rotation_free(ngemm_rotation *rotation);
+
+/*
+ * Norm and rotation of Q's and K's rows (f32, f16 or bf16) in one pass:
+ *     y = x / sqrt(mean(x^2) + eps) * weight          (weight_dev: float [head_dim] for all heads, or NULL: rows are not normalised)
+ *     then the rotation by positions[token]           (rotation NULL: none; positions_dev: int32 [tokens])
+ * in float arithmetic, rounded to the type once.  head_dim a multiple of 16 up to 256.  Rows of any magnitude: squares that leave the floats' range are
+ * formed relative to a power of two.  A row of zeros stays zero under the norm, with eps 0 too.  A position that the table does not have makes the
+ * token's rows NaN.  k_heads 0 (or q_heads 0) leaves that side's arguments unused.  Outputs may stand in their own inputs' places (same
+ * address and strides); else no output overlaps an input or the other output.
+ * Rows of the usual strides and 16-byte alignment move in 16-byte pieces, others element by element.
+ */
+ngemm_status ngemm_qk_norm_rotate(ngemm_ctx *ctx, ngemm_type type, int64_t head_dim, int64_t tokens,
+                                  int64_t q_heads, const void *Q_dev, int64_t q_token_stride, int64_t q_head_stride, const float *q_weight_dev,
+                                  int64_t k_heads, const void *K_dev, int64_t k_token_stride, int64_t k_head_stride, const float *k_weight_dev,
+                                  float eps, const ngemm_rotation *rotation, const int32_t *positions_dev,
+                                  void *QO_dev, int64_t qo_token_stride, int64_t qo_head_stride,
+                                  void *KO_dev, int64_t ko_token_stride, int64_t ko_head_stride, void *hip_stream);
+
+/*
+ * ngemm_kv_write with K's rows normalised (k_weight_dev NULL: not) and rotated (rotation NULL: not) on the way, by the positions at which they stand in
+ * their sequences.  The rows are quantised as the floats that come out, not rounded to the type in between; near a tie a code can be the next
+ * one, as with f32 rows.  A position that the rotation's table does not have is written as a row of NaN (K only).
+ */
+ngemm_status ngemm_kv_write_rotated(ngemm_ctx *ctx, const ngemm_kv_cache *cache, ngemm_type type, int64_t batch, int64_t tokens,
+                                    const void *K_dev, int64_t k_token_stride, int64_t k_head_stride,
+                                    const void *V_dev, int64_t v_token_stride, int64_t v_head_stride,
+                                    const float *k_weight_dev, float eps, const ngemm_rotation *rotation,
+                                    const int32_t *offsets_dev, const int32_t *starts_dev,
+                                    const int32_t *pages_dev, int64_t pages_stride, void *hip_stream);
+
+/*
  * One new token per sequence attends to the cache (f16 or bf16):
  *     O[b][h] = sum_t p_t V_t / sum_t p_t,  p_t = exp(scale <Q[b][h], K_t> - max),  t < lengths[b],
  * with the K and V of head h / (q_heads / kv_heads) (q_heads a multiple of the cache's kv_heads).  lengths_dev: int32
@@ -455,6 +506,30 @@ ngemm_status ngemm_attention_decode(ngemm_ctx *ctx, const ngemm_kv_cache *cache,
                                     const int32_t *pages_dev, int64_t pages_stride, float scale,
                                     void *O_dev, int64_t o_token_stride, int64_t o_head_stride,
                                     void *workspace_dev, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * New tokens attend to their sequences in the cache, the new ones included (f16 or bf16): a token of generation each, tokens that are proposed and checked
+ * together, a piece of a prompt, a whole one, or a batch of all of these.  Q and O hold packed rows as ngemm_kv_write takes K and V: sequence b has
+ * the rows offsets[b] .. offsets[b + 1] - 1 (offsets_dev: int32 [batch + 1], not falling, from 0 to tokens; rows behind the last sequence's are left
+ * alone), at the positions starts[b], starts[b] + 1, ... (starts_dev: int32 [batch], or NULL for 0).  The row at position p sees the tokens t <= p, with
+ * a window (not 0) only t > p - window and the first `sinks` ones:
+ *     O = sum_t w_t V_t / sum_t w_t,  w_t = exp(scale <Q, K_t> - max)
+ * with the K and V of head h / (q_heads / kv_heads) (q_heads a multiple of the cache's kv_heads).  A row that sees nothing gives 0; what a row does not
+ * see is without effect on it, NaN included; tokens in a page that is not one of the cache's are left out.  max_new: the most new tokens of a
+ * sequence, max_length: the most tokens of one with them (up to 2^30); larger numbers are right as well, and slower, since the launches and the workspace are
+ * sized by them.  With smaller ones a sequence's rows past the first max_new are left alone, and tokens from max_length on are not read.  window and
+ * sinks up to 2^30.  Softmax statistics and sums are float; scores are products of the 8-bit codes and the queries as they are; the weights w_t
+ * times V's scales enter the second product as bf16 (bf16 rows of sequences with more than 32 rows, new tokens times q_heads / kv_heads) or as the sum of
+ * two bf16 numbers, 16 bits, so that they have the floats' range.  Workspace, order of sums and streams as for ngemm_attention_decode.
+ */
+size_t ngemm_attention_chunk_workspace_bytes(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t tokens, int64_t max_new,
+                                             int64_t max_length, int64_t window, int64_t sinks);
+ngemm_status ngemm_attention_chunk(ngemm_ctx *ctx, const ngemm_kv_cache *cache, ngemm_type type, int64_t batch, int64_t q_heads, int64_t tokens,
+                                   const void *Q_dev, int64_t q_token_stride, int64_t q_head_stride,
+                                   const int32_t *offsets_dev, const int32_t *starts_dev, int64_t max_new, int64_t max_length,
+                                   const int32_t *pages_dev, int64_t pages_stride, int64_t window, int64_t sinks, float scale,
+                                   void *O_dev, int64_t o_token_stride, int64_t o_head_stride,
+                                   void *workspace_dev, size_t workspace_bytes, void *hip_stream);
 
 /*
  * Whole prompts attend to themselves, or to a longer context that ends with them (f16 or bf16).  Packed sequences: b has

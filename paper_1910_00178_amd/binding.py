@@ -35,6 +35,9 @@ NGEMM_F32 = 0
 NGEMM_F16 = 1
 NGEMM_BF16 = 2
 
+NGEMM_PAIRS_HALVES = 0
+NGEMM_PAIRS_NEIGHBOURS = 1
+
 EXPORTS = (
     "ngemm_status_string", "ngemm_create", "ngemm_destroy", "ngemm_set_kernel", "ngemm_tune_u8s8s32", "ngemm_tuned_kernel", "ngemm_set_max_workgroups",
     "ngemm_packed_b_bytes", "ngemm_pack_b", "ngemm_pack_b_u8", "ngemm_packed_b_free", "ngemm_packed_b_shape",
@@ -43,6 +46,8 @@ EXPORTS = (
     "ngemm_batched_workspace_bytes", "ngemm_run_batched_u8s8s32",
     "ngemm_kv_cache_bytes", "ngemm_kv_cache_create", "ngemm_kv_cache_free", "ngemm_kv_write", "ngemm_kv_read",
     "ngemm_attention_decode_workspace_bytes", "ngemm_attention_decode", "ngemm_attention_prompt_workspace_bytes", "ngemm_attention_prompt",
+    "ngemm_rotation_bytes", "ngemm_rotation_create", "ngemm_rotation_free", "ngemm_qk_norm_rotate", "ngemm_kv_write_rotated",
+    "ngemm_attention_chunk_workspace_bytes", "ngemm_attention_chunk",
 )
 
 
@@ -121,8 +126,20 @@ _lib.ngemm_attention_prompt_workspace_bytes.restype = _sz
 _lib.ngemm_attention_prompt_workspace_bytes.argtypes = [_i64, _i64, _i64, _i64, _i64, _i64]
 _lib.ngemm_attention_prompt.argtypes = [_p, _int, _i64, _i64, _i64, _i64, _i64, _p, _i64, _i64, _i64, _p, _i64, _i64, _p, _i64, _i64, _p, _p, _int,
                                         _f32, _p, _i64, _i64, _p, _sz, _p]
+_lib.ngemm_rotation_bytes.restype = _sz
+_lib.ngemm_rotation_bytes.argtypes = [_i64, _i64]
+_lib.ngemm_rotation_create.argtypes = [_p, _i64, _i64, _int, _p, _sz, ctypes.POINTER(_p)]
+_lib.ngemm_rotation_free.argtypes = [_p]
+_lib.ngemm_qk_norm_rotate.argtypes = [_p, _int, _i64, _i64, _i64, _p, _i64, _i64, _p, _i64, _p, _i64, _i64, _p, _f32, _p, _p, _p, _i64, _i64,
+                                      _p, _i64, _i64, _p]
+_lib.ngemm_kv_write_rotated.argtypes = [_p, _p, _int, _i64, _i64, _p, _i64, _i64, _p, _i64, _i64, _p, _f32, _p, _p, _p, _p, _i64, _p]
+_lib.ngemm_attention_chunk_workspace_bytes.restype = _sz
+_lib.ngemm_attention_chunk_workspace_bytes.argtypes = [_i64] * 9
+_lib.ngemm_attention_chunk.argtypes = [_p, _p, _int, _i64, _i64, _i64, _p, _i64, _i64, _p, _p, _i64, _i64, _p, _i64, _i64, _i64, _f32, _p, _i64, _i64,
+                                       _p, _sz, _p]
 for _name in ("ngemm_kv_cache_create", "ngemm_kv_cache_free", "ngemm_kv_write", "ngemm_kv_read", "ngemm_attention_decode",
-              "ngemm_attention_prompt"):
+              "ngemm_attention_prompt", "ngemm_rotation_create", "ngemm_rotation_free", "ngemm_qk_norm_rotate", "ngemm_kv_write_rotated",
+              "ngemm_attention_chunk"):
     getattr(_lib, _name).restype = _int
 for _name in ("ngemm_create", "ngemm_destroy", "ngemm_set_kernel", "ngemm_set_max_workgroups", "ngemm_pack_b", "ngemm_packed_b_free",
               "ngemm_packed_b_shape", "ngemm_run_u8s8s32", "ngemm_run_u8s8u8_requant",
@@ -410,13 +427,61 @@ def ngemm_attention_prompt(ctx, type, batch, q_heads, kv_heads, head_dim, q_toke
            "ngemm_attention_prompt")
 
 
+def ngemm_rotation_bytes(positions, dim):
+    return int(_lib.ngemm_rotation_bytes(int(positions), int(dim)))
+
+
+def ngemm_rotation_create(ctx, positions, dim, pairs, table_dev, table_bytes):
+    h = _p()
+    _check(_lib.ngemm_rotation_create(ctx, int(positions), int(dim), int(pairs), _dev(table_dev), int(table_bytes), ctypes.byref(h)),
+           "ngemm_rotation_create")
+    return h
+
+
+def ngemm_rotation_free(rotation):
+    _check(_lib.ngemm_rotation_free(rotation), "ngemm_rotation_free")
+
+
+def ngemm_qk_norm_rotate(ctx, type, head_dim, tokens, q_heads, Q_dev, q_token_stride, q_head_stride, q_weight_dev, k_heads, K_dev, k_token_stride,
+                         k_head_stride, k_weight_dev, eps, rotation, positions_dev, QO_dev, qo_token_stride, qo_head_stride, KO_dev,
+                         ko_token_stride, ko_head_stride, hip_stream=None):
+    _check(_lib.ngemm_qk_norm_rotate(ctx, int(type), int(head_dim), int(tokens), int(q_heads), _dev(Q_dev), int(q_token_stride), int(q_head_stride),
+                                     _dev(q_weight_dev), int(k_heads), _dev(K_dev), int(k_token_stride), int(k_head_stride), _dev(k_weight_dev),
+                                     float(eps), rotation, _dev(positions_dev), _dev(QO_dev), int(qo_token_stride), int(qo_head_stride),
+                                     _dev(KO_dev), int(ko_token_stride), int(ko_head_stride), _stream(hip_stream)), "ngemm_qk_norm_rotate")
+
+
+def ngemm_kv_write_rotated(ctx, cache, type, batch, tokens, K_dev, k_token_stride, k_head_stride, V_dev, v_token_stride, v_head_stride,
+                           k_weight_dev, eps, rotation, offsets_dev, starts_dev, pages_dev, pages_stride, hip_stream=None):
+    _check(_lib.ngemm_kv_write_rotated(ctx, cache, int(type), int(batch), int(tokens), _dev(K_dev), int(k_token_stride), int(k_head_stride),
+                                       _dev(V_dev), int(v_token_stride), int(v_head_stride), _dev(k_weight_dev), float(eps), rotation,
+                                       _dev(offsets_dev), _dev(starts_dev), _dev(pages_dev), int(pages_stride), _stream(hip_stream)),
+           "ngemm_kv_write_rotated")
+
+
+def ngemm_attention_chunk_workspace_bytes(batch, q_heads, kv_heads, head_dim, tokens, max_new, max_length, window, sinks):
+    return int(_lib.ngemm_attention_chunk_workspace_bytes(int(batch), int(q_heads), int(kv_heads), int(head_dim), int(tokens), int(max_new),
+                                                          int(max_length), int(window), int(sinks)))
+
+
+def ngemm_attention_chunk(ctx, cache, type, batch, q_heads, tokens, Q_dev, q_token_stride, q_head_stride, offsets_dev, starts_dev, max_new,
+                          max_length, pages_dev, pages_stride, window, sinks, scale, O_dev, o_token_stride, o_head_stride, workspace_dev=None,
+                          workspace_bytes=0, hip_stream=None):
+    _check(_lib.ngemm_attention_chunk(ctx, cache, int(type), int(batch), int(q_heads), int(tokens), _dev(Q_dev), int(q_token_stride),
+                                      int(q_head_stride), _dev(offsets_dev), _dev(starts_dev), int(max_new), int(max_length), _dev(pages_dev),
+                                      int(pages_stride), int(window), int(sinks), float(scale), _dev(O_dev), int(o_token_stride),
+                                      int(o_head_stride), _dev(workspace_dev), int(workspace_bytes), _stream(hip_stream)),
+           "ngemm_attention_chunk")
+
+
 # The calls above that a program makes per product, weight, batch or step: natively where all arguments are of the usual types,
 # else as above.
 _kinds = {"ngemm_run_u8s8s32": "run", "ngemm_run_s8s8s32": "run", "ngemm_run_u8u8s32": "run", "ngemm_run_s16s16s32": "run",
           "ngemm_run_u8s8s32_static": "static", "ngemm_run_u8s8u8_requant": "requant", "ngemm_run_u8s8u8_requant_channel": "channel",
           "ngemm_run_u8s8s32_unpacked": "unpacked", "ngemm_run_batched_u8s8s32": "batched", "ngemm_pack_b": "pack", "ngemm_pack_b_u8": "pack",
           "ngemm_pack_b_s16": "pack", "ngemm_packed_b_free": "free", "ngemm_kv_write": "move", "ngemm_kv_read": "move",
-          "ngemm_attention_decode": "decode", "ngemm_attention_prompt": "prompt"}
+          "ngemm_attention_decode": "decode", "ngemm_attention_prompt": "prompt", "ngemm_qk_norm_rotate": "turn",
+          "ngemm_kv_write_rotated": "move_turned", "ngemm_attention_chunk": "chunk"}
 _native = hasattr(_calls, "Call")
 if _native:
     for _name in _kinds:

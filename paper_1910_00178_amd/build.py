@@ -8,7 +8,7 @@ from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
-SOURCES = [os.path.join(HERE, "csrc", name) for name in ("ngemm.hip", "attention.hip")]
+SOURCES = [os.path.join(HERE, "csrc", name) for name in ("ngemm.hip", "attention.hip", "attention_chunk.hip", "rotation.hip")]
 LIB = os.path.join(HERE, "libngemm.so")
 CALLS_SRC = os.path.join(HERE, "csrc", "calls.c")
 CALLS = os.path.join(HERE, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))

@@ -18,44 +18,11 @@ struct DecodeArgs {
 // (what the registers allow; told to the compiler, which otherwise takes some more for the rare branch of the tile loop)
 constexpr int decode_waves_per_simd(int D) { return D <= 64 ? 4 : D <= 96 ? 3 : D <= 192 ? 2 : 1; }
 
-// 16 codes as 16-bit floats, in order.  A code with its sign bit turned, as the low byte under 0x64, is the float 1024 + 128 + code.
-constexpr uint32_t kCodeSigns = 0x80808080u;
-__device__ __forceinline__ void codes_to_f16(u4 x, u4 (&out)[2], uint32_t signs = kCodeSigns)
-{
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-        const uint32_t y = x[e] ^ signs;
-        const h2 base = {(_Float16)-1152.0f, (_Float16)-1152.0f};
-        const h2 lo = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, y, 0x04010400u)) + base;
-        const h2 hi = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, y, 0x04030402u)) + base;
-        out[e / 2][2 * (e % 2)] = __builtin_bit_cast(uint32_t, lo);
-        out[e / 2][2 * (e % 2) + 1] = __builtin_bit_cast(uint32_t, hi);
-    }
-}
-
 // Of two 16-bit floats those without a sign, else 0.
 __device__ __forceinline__ uint32_t positive_halves(uint32_t x)
 {
     typedef int16_t V2 __attribute__((ext_vector_type(2)));
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(V2, x), (V2)(int16_t)0));
-}
-
-// Lane 16 r + K's value in all lanes 16 r .. 16 r + 15.
-template <int K>
-__device__ __forceinline__ float of_row(float x)
-{
-    return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x150 + K, 0xf, 0xf, true));
-}
-
-// f(Index<0>) .. f(Index<N - 1>)
-template <int I> struct Index { static constexpr int value = I; };
-template <int N, int I = 0, class F>
-__device__ __forceinline__ void unrolled(F &&f)
-{
-    if constexpr (I < N) {
-        f(Index<I>{});
-        unrolled<N, I + 1>(f);
-    }
 }
 
 // Elements d .. d + 3 of an output row (0 where nothing was seen).

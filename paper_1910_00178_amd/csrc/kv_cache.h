@@ -173,17 +173,27 @@ __device__ __forceinline__ void store(typename E::T *to, const float (&x)[N])
     }
 }
 
-// Over aligned groups of 16 or 8 lanes.
-template <int LANES, class T>
-__device__ __forceinline__ T max_of_lanes(T x)
+// f over aligned groups of 16, 8 or 4 lanes, the same in all of them.
+template <int LANES, class T, class F>
+__device__ __forceinline__ T over_lanes(T x, F &&f)
 {
-#define NGEMM_WITH(dpp) x = max(x, __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), dpp, 0xf, 0xf, true)))
+#define NGEMM_WITH(dpp) x = f(x, __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), dpp, 0xf, 0xf, true)))
     if constexpr (LANES == 16) NGEMM_WITH(0x140);        // lane 15 - i's
-    NGEMM_WITH(0x141);                                   // of 8 lanes, lane 7 - i's
+    if constexpr (LANES >= 8) NGEMM_WITH(0x141);         // of 8 lanes, lane 7 - i's
     NGEMM_WITH(0x1b);                                    // of 4, lane 3 - i's
     NGEMM_WITH(0xb1);                                    // of 2, the other's
 #undef NGEMM_WITH
     return x;
+}
+template <int LANES, class T>
+__device__ __forceinline__ T max_of_lanes(T x)
+{
+    return over_lanes<LANES>(x, [](T a, T b) { return max(a, b); });
+}
+template <int LANES>
+__device__ __forceinline__ float sum_of_lanes(float x)
+{
+    return over_lanes<LANES>(x, [](float a, float b) { return a + b; });
 }
 
 // The four dwords' bytes as a 4 x 4 matrix, transposed.
