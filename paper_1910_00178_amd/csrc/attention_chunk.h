@@ -61,17 +61,40 @@ struct ChunkTiles {
     __device__ __forceinline__ int at(int i) const { return i < sink_tiles ? i : i - sink_tiles + lo_tile; }
 };
 
-// 16 codes as 16-bit floats, in order.
-__device__ __forceinline__ void codes_to(F16, u4 x, u4 (&out)[2]) { codes_to_f16(x, out); }
-__device__ __forceinline__ void codes_to(BF16, u4 x, u4 (&out)[2])
+// The number of the block that holds positions 16 * index .. of sequence b and a head, or -1 where there is none.  Without branches (a table without
+// entries has been taken as one without tokens), so that loops around it have uniform ones only: sums in registers stay where they are.
+__device__ __forceinline__ int chunk_place(const ChunkArgs &a, int b, int head, int index)
+{
+    const int page = index / a.cache.page_blocks;
+    const bool there = page < a.cache.pages_stride;
+    const int id = a.cache.pages[b * a.cache.pages_stride + (there ? page : 0)];
+    return there && id >= 0 && id < a.cache.num_pages ? (id * a.cache.kv_heads + head) * a.cache.page_blocks + (index - page * a.cache.page_blocks) : -1;
+}
+
+// Four codes as 16-bit floats, in order.
+__device__ __forceinline__ u2 codes4_to(F16, uint32_t x)
+{
+    const uint32_t y = x ^ kCodeSigns;
+    const h2 base = {(_Float16)-1152.0f, (_Float16)-1152.0f};
+    return (u2){__builtin_bit_cast(uint32_t, __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, y, 0x04010400u)) + base),
+                __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, y, 0x04030402u)) + base)};
+}
+__device__ __forceinline__ u2 codes4_to(BF16, uint32_t x)
+{
+    float f[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = (float)(int8_t)(x >> (8 * i));            // (whole numbers of 8 bits: the upper half is all of it)
+    return (u2){__builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302u),
+                __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302u)};
+}
+template <class E>
+__device__ __forceinline__ void codes_to(E, u4 x, u4 (&out)[2])
 {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        float f[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) f[i] = (float)(int8_t)(x[e] >> (8 * i));
-        out[e / 2][2 * (e % 2)] = __builtin_amdgcn_perm(__float_as_uint(f[1]), __float_as_uint(f[0]), 0x07060302u);
-        out[e / 2][2 * (e % 2) + 1] = __builtin_amdgcn_perm(__float_as_uint(f[3]), __float_as_uint(f[2]), 0x07060302u);
+        const u2 y = codes4_to(E{}, x[e]);
+        out[e / 2][2 * (e % 2)] = y[0];
+        out[e / 2][2 * (e % 2) + 1] = y[1];
     }
 }
 
@@ -132,15 +155,8 @@ __global__ __launch_bounds__(kFewWaves * 64) void attention_chunk_few_kernel(con
 
     // the wavefront's blocks, 16 tiles ahead: lane l looks up block l % 4 of its tile l / 4
     constexpr int block_bytes = 32 * D + 128;
-    const int blocks_per_page = a.cache.page_blocks;
     auto look_up = [&](int i) {
-        const int index = 4 * list.at(min(i + NW * (lane >> 2), max(list.count - 1, 0))) + (lane & 3), page = index / blocks_per_page;
-        int where = -1;
-        if (page < a.cache.pages_stride) {
-            const int id = a.cache.pages[b * a.cache.pages_stride + page];
-            if (id >= 0 && id < a.cache.num_pages) where = (id * kv_heads + head) * blocks_per_page + (index - page * blocks_per_page);
-        }
-        return where;
+        return chunk_place(a, b, head, 4 * list.at(min(i + NW * (lane >> 2), list.count - 1)) + (lane & 3));
     };
     int places = first + wave < end ? look_up(first + wave) : -1;
 
@@ -364,14 +380,14 @@ __global__ __launch_bounds__(kFewJoinThreads) void attention_chunk_few_join_kern
 
 // ---- many rows ----
 
-// DP: head_dim rounded up.
-template <int DP_, int PER_CU_>
+// DP: head_dim rounded up; R: groups of 32 rows of a wavefront; PER_CU workgroups to a unit.
+template <int DP_, int R_, int PER_CU_>
 struct ChunkCfg {
-    static constexpr int DP = DP_, PER_CU = PER_CU_, NW = 4, BM = 32 * NW, BN = kChunkKeys;
+    static constexpr int DP = DP_, R = R_, PER_CU = PER_CU_, NW = 4, BM = 32 * R * NW, BN = kChunkKeys;
     static constexpr int CH = DP / 8;                            // 16-byte pieces of a row of K
-    static constexpr int kTile = BN * DP * 2, kScales = 2 * kTile, kStage = 2 * kTile + 2 * BN * 4, kLds = 2 * kStage;
+    static constexpr int kTile = BN * DP * 2, kScales = 4 * kTile, kScaleBytes = 2 * BN * 4, kLds = kScales + 3 * kScaleBytes;     // two of K, two of V, three of scales
     static constexpr int PIECES = 4 * DP / (NW * 64) + (4 * DP % (NW * 64) != 0);        // of 16 codes of K (and of V) per thread
-    static constexpr int kPart = BM * 2 * (DP / 8 + 1);          // 16-byte pieces of a part: sums, maximum and weight
+    static constexpr int kPart = NW * 64 * R * (DP / 8 + 1);     // 16-byte pieces of a part: sums, maximum and weight
     static __device__ __forceinline__ int k_swizzle(int j) { return CH % 16 == 0 ? j & 15 : CH % 8 == 0 ? (j >> 1) & 7 : (j >> 2) & 3; }
     static __device__ __forceinline__ int v_swizzle(int d) { return (d >> 1) & 7; }
 };
@@ -402,7 +418,7 @@ template <class E, class C, bool VEC>
 __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_chunk_kernel(const ChunkArgs a)
 {
     extern __shared__ __align__(1024) uint8_t lds[];
-    constexpr int DP = C::DP, BN = C::BN, PIECES = C::PIECES;
+    constexpr int DP = C::DP, BN = C::BN, R = C::R, PIECES = C::PIECES;
     constexpr bool SPLIT = __is_same(typename E::T, _Float16);   // two bf16 numbers per weight
     typedef typename E::T T;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, col = lane & 31;
@@ -414,234 +430,343 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_c
     const ChunkTiles list = tile.keys(a);
     const int parts = max(1, min(a.parts, (list.count + a.run - 1) / a.run));
     if (part >= parts) return;
-    const int first = (int)((int64_t)list.count * part / parts), end = (int)((int64_t)list.count * (part + 1) / parts);
+    const int first = (int)((int64_t)list.count * part / parts), count = (int)((int64_t)list.count * (part + 1) / parts) - first;
 
-    const int row = tile.row0 + 32 * wave + col;
-    const bool row_there = row < rows;
-    const int query = min(row, rows - 1) / group, qhead = head * group + min(row, rows - 1) % group;
-    const ChunkRow range = tile.row(a, row), wave_first = tile.row(a, tile.row0 + 32 * wave), wave_last = tile.row(a, tile.row0 + 32 * wave + 31);
-    const bool wave_there = tile.row0 + 32 * wave < rows;
+    const int row0 = tile.row0 + 32 * R * wave;                  // the wavefront's
+    const ChunkRow row_first = tile.row(a, row0), row_last = tile.row(a, row0 + 32 * R - 1);
+    ChunkRow range[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) range[r] = tile.row(a, row0 + 32 * r + col);
 
     // ---- the blocks of 16 tiles: lane l looks up block l % 4 of tile l / 4 ----
-    const int blocks_per_page = a.cache.page_blocks, block_bytes = 32 * D + 128;
+    const int block_bytes = 32 * D + 128;
     auto look_up = [&](int i) {
-        const int index = 4 * list.at(min(i + (lane >> 2), max(list.count - 1, 0))) + (lane & 3), page = index / blocks_per_page;
-        int where = -1;
-        if (page < a.cache.pages_stride) {
-            const int id = a.cache.pages[tile.b * a.cache.pages_stride + page];
-            if (id >= 0 && id < a.cache.num_pages) where = (id * kv_heads + head) * blocks_per_page + (index - page * blocks_per_page);
-        }
-        return where;
+        const int index = 4 * list.at(min(first + i + (lane >> 2), list.count - 1)) + (lane & 3);
+        return chunk_place(a, tile.b, head, index);
     };
     // ---- a tile's codes, and where they go as 16-bit floats ----
-    int piece_block[PIECES], piece_at[PIECES], k_to[PIECES][2], v_to[PIECES][2];
-    bool piece_there[PIECES];
+    // (all threads store: those past the last piece others' again, those past head_dim something finite where it meets Q's zeros or becomes no output)
+    int piece_block[PIECES], piece_at[PIECES], k_to[PIECES], v_to[PIECES];
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-        const int p = i * C::NW * 64 + tid, q = p % DP, per = D / 16, token = q / per, c = 2 * (q % per);
+        const int p = (i * C::NW * 64 + tid) % (4 * DP), q = p % DP, per = D / 16, token = q < D ? q / per : 0, c = 2 * (q < D ? q % per : per);
         piece_block[i] = p / DP;
-        piece_there[i] = p < 4 * DP && q < D;
-        piece_at[i] = 16 * q;
+        piece_at[i] = q < D ? 16 * q : 0;
         const int j = 16 * piece_block[i] + token;
-#pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            k_to[i][e] = j * DP * 2 + ((c + e) ^ C::k_swizzle(j)) * 16;
-            v_to[i][e] = C::kTile + q * BN * 2 + ((2 * piece_block[i] + e) ^ C::v_swizzle(q)) * 16;
-        }
+        k_to[i] = j * DP * 2 + (c ^ C::k_swizzle(j)) * 16;       // (the second half of its 32 bytes: where bit 4 is turned)
+        v_to[i] = 2 * C::kTile + q * BN * 2 + (2 * piece_block[i] ^ C::v_swizzle(q)) * 16;
     }
     u4 k_codes[PIECES], v_codes[PIECES];
-    float a_scale = 0.0f;                                        // threads 0 .. 63: K's of key tid, 64 .. 127: V's
-    auto load_codes = [&](int places, int n) {
+    float a_scale = 0.0f;                                        // even wavefronts: K's of key `lane`, odd ones: V's
+    auto load_k = [&](int places, int n) {
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-            if (!piece_there[i]) continue;
-            const uint8_t *block = a.cache.data + (int64_t)max(__shfl(places, 4 * n + piece_block[i]), 0) * block_bytes;
-            k_codes[i] = *(const u4 *)(block + piece_at[i]);
-            v_codes[i] = *(const u4 *)(block + 16 * D + piece_at[i]);
-        }
+        for (int i = 0; i < PIECES; ++i)
+            k_codes[i] = *(const u4 *)(a.cache.data + (int64_t)max(__shfl(places, 4 * n + piece_block[i]), 0) * block_bytes + piece_at[i]);
         const uint8_t *block = a.cache.data + (int64_t)max(__shfl(places, 4 * n + (lane >> 4)), 0) * block_bytes + 32 * D;
-        if (wave < 2) a_scale = *(const float *)(block + 64 * wave + 4 * (lane & 15));
+        a_scale = *(const float *)(block + 64 * (wave & 1) + 4 * (lane & 15));
     };
-    auto store_codes = [&](uint8_t *at) {
+    auto load_v = [&](int places, int n) {
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i) {
-            if (!piece_there[i]) continue;
-            u4 x[2];
-            codes_to(E{}, k_codes[i], x);
-            *(u4 *)(at + k_to[i][0]) = x[0];
-            *(u4 *)(at + k_to[i][1]) = x[1];
-            codes_to(BF16{}, v_codes[i], x);
-            *(u4 *)(at + v_to[i][0]) = x[0];
-            *(u4 *)(at + v_to[i][1]) = x[1];
-        }
-        if (wave < 2) ((float *)(at + C::kScales))[tid] = wave == 0 ? a_scale * a.scale : a_scale;
+        for (int i = 0; i < PIECES; ++i)
+            v_codes[i] = *(const u4 *)(a.cache.data + (int64_t)max(__shfl(places, 4 * n + piece_block[i]), 0) * block_bytes + 16 * D + piece_at[i]);
     };
-    if (D < DP) {                                                // elements past head_dim are 0 throughout
-        for (int i = tid; i < C::kLds / 16; i += C::NW * 64) ((u4 *)lds)[i] = (u4)(0u);
-        __syncthreads();
-    }
-    int places = first < end ? look_up(first) : -1;
-    if (first < end) load_codes(places, 0);
+    // dword x % 4 of piece x / 4, stored with the piece's last
+    u4 out[2];
+    auto store_step = [&](auto which, auto x, uint8_t *at) {
+        constexpr int X = decltype(x)::value, I = X / 4, W = X % 4;
+        constexpr bool V = decltype(which)::value;
+        const uint32_t codes = V ? v_codes[I][W] : k_codes[I][W];
+        u2 y;
+        if constexpr (V) y = codes4_to(BF16{}, codes);
+        else y = codes4_to(E{}, codes);
+        out[W / 2][2 * (W % 2)] = y[0];
+        out[W / 2][2 * (W % 2) + 1] = y[1];
+        if constexpr (W % 2 == 1) *(u4 *)(at + ((V ? v_to[I] : k_to[I]) ^ (W / 2 * 16))) = out[W / 2];
+    };
+    auto store_scales = [&](int tile_number) {
+        ((float *)(lds + C::kScales + tile_number % 3 * C::kScaleBytes))[tid & 127] = a_scale * (wave & 1 ? 1.0f : a.scale);
+    };
+    // elements past head_dim, and what stands for the values before the first block's, are 0
+    for (int i = tid; i < (D < DP ? 4 * C::kTile : C::kTile) / 16; i += C::NW * 64) ((u4 *)(lds + (D < DP ? 0 : 3 * C::kTile)))[i] = (u4)(0u);
+    if (D < DP) __syncthreads();
+    int places = count > 0 ? look_up(0) : -1;
+    load_k(places, 0);
+    load_v(places, 0);
 
     // ---- Q^T's operand: 8 elements of the lane's row per step ----
-    u4 q[DP / 16];
-    {
-        const T *from = (const T *)a.q.data + (tile.seq.first + query) * a.q.token_stride + qhead * a.q.head_stride;
+    u4 q[R][DP / 16];
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const int row = min(row0 + 32 * r + col, rows - 1);
+        const T *from = (const T *)a.q.data + (tile.seq.first + row / group) * a.q.token_stride + (head * group + row % group) * a.q.head_stride;
 #pragma unroll
         for (int s = 0; s < DP / 16; ++s) {
             const int d = 16 * s + 8 * half;
             const T *at = from + (d < D ? d : 0);
-            if constexpr (VEC) q[s] = *(const u4 *)at;
-            else __builtin_memcpy(&q[s], at, 16);
-            if (d >= D) q[s] = (u4)(0u);
+            if constexpr (VEC) q[r][s] = *(const u4 *)at;
+            else __builtin_memcpy(&q[r][s], at, 16);
+            if (d >= D) q[r][s] = (u4)(0u);
+            asm volatile("" : "+a"(q[r][s]));            // (only the matrix unit reads it: beside the sums, out of the vector unit's registers)
         }
     }
     // the key whose scores are row `col` of the first product: so that a lane holds 8 consecutive keys' of each 16
     const int key = 16 * (col >> 4) + 8 * (col >> 2 & 1) + 4 * (col >> 3 & 1) + (col & 3);
-    const int k_row = key * DP * 2, k_chunk = (half ^ C::k_swizzle(key)) * 16;
-    const int v_row = C::kTile + col * BN * 2, v_chunk = (half ^ C::v_swizzle(col)) * 16;
+    const int k_row = key * DP * 2, v_row = 2 * C::kTile + col * BN * 2;
+    int k_chunk = (half ^ C::k_swizzle(key)) * 16, v_chunk = (half ^ C::v_swizzle(col)) * 16;
 
-    f16v o[DP / 32];
+    f16v o[R][DP / 32], s[2][R];
+    u4 p[2][R][2], rest[2][R][2];
+    float m[R], l[R];
 #pragma unroll
-    for (int t = 0; t < DP / 32; ++t) o[t] = (f16v)(0.0f);
-    float m = -3.0e38f, l = 0.0f;
-    for (int i = first; i < end; ++i) {
-        uint8_t *const at = lds + (i - first & 1) * C::kStage;
-        const int n = i - first & 15;
-        const uint32_t lost = (uint32_t)(__ballot(places < 0) >> (4 * n)) & 15u;         // blocks that are not there
-        store_codes(at);
-        if (i + 1 < end) {
-            if (n == 15) places = look_up(i + 1);
-            load_codes(places, n + 1 & 15);
-        }
-        __syncthreads();
-        const int key0 = BN * list.at(i);
-        if (!wave_there || key0 > wave_last.hi || (key0 + BN - 1 < wave_first.lo && key0 >= a.sinks)) continue;
-        f16v s[2];
+    for (int r = 0; r < R; ++r) {
+        m[r] = -3.0e38f;
+        l[r] = 0.0f;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-            s[t] = (f16v)(0.0f);
+        for (int t = 0; t < DP / 32; ++t) o[r][t] = (f16v)(0.0f);
 #pragma unroll
-            for (int u = 0; u < DP / 16; ++u) s[t] = mfma32(E{}, *(const u4 *)(at + k_row + (k_chunk ^ 32 * u) + t * 32 * DP * 2), q[u], s[t]);
-        }
-        const bool masked = lost || !wave_first.sees_all(key0, a.sinks) || !wave_last.sees_all(key0, a.sinks);
-        // bit 32 t + 16 (e / 8) + e % 8: whether the row sees s[t][e]'s key
-        uint64_t seen = ~(uint64_t)0;
-        if (masked) {
-            seen = range.seen(key0, a.sinks);
+        for (int u = 0; u < 2; ++u) p[1][r][u] = rest[1][r][u] = (u4)(0u);
+    }
+    auto k_operand = [&](const uint8_t *at, int u) { return *(const u4 *)(at + k_row + (k_chunk ^ 32 * u)); };
+    auto v_operand = [&](const uint8_t *at, int block, int u, int t) { return *(const u4 *)(at + v_row + (v_chunk ^ (64 * block + 32 * u)) + t * 32 * BN * 2); };
+
+    // Block j of 32 keys (B: its parity): the scores of block j become weights while the matrix unit makes those of block j + 1 and takes the weights of
+    // block j - 1 to the values, and codes of the next tile (of K where B is 0, of V where it is 1) become floats: 16 steps, with a score of each row group
+    // and a share of everything else in each.
+    constexpr float kMostSum = 0x1p12f;
+    auto block = [&](auto parity, auto masked, int i, uint32_t lost) {
+        constexpr int B = decltype(parity)::value;
+        constexpr bool MASKED = decltype(masked)::value;
+        // (not known to stay the same: one instruction per read is cheaper than the registers of all places)
+        asm volatile("" : "+v"(k_chunk), "+v"(v_chunk));
+        const uint8_t *const k_at = lds + (B == 0 ? i & 1 : ~i & 1) * C::kTile + (B == 0 ? 32 * DP * 2 : 0);     // block j + 1's
+        const uint8_t *const v_at = lds + (B == 0 ? ~i & 1 : i & 1) * C::kTile;                                   // block j - 1's
+        uint8_t *const to = lds + (~i & 1) * C::kTile;
+        const float *const scales = (const float *)(lds + C::kScales + i % 3 * C::kScaleBytes) + 32 * B + 8 * half;
+        uint32_t seen[R];
+        if constexpr (MASKED) {
+            const int key0 = BN * list.at(first + i);
 #pragma unroll
-            for (int g = 0; g < 4; ++g)
-                if (lost >> g & 1) seen &= ~((uint64_t)0xffff << (16 * g));
-            seen >>= 8 * half;
-        }
-        const float *const scales = (const float *)(at + C::kScales) + 8 * half;
-        float most = m;
+            for (int r = 0; r < R; ++r) {
+                uint64_t bits = range[r].seen(key0, a.sinks);
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-                const f4 by = *(const f4 *)(scales + 32 * t + 16 * (e / 8) + e % 8);
-#pragma unroll
-                for (int x = 0; x < 4; ++x) s[t][e + x] *= by[x];
+                for (int g = 0; g < 4; ++g)
+                    if (lost >> g & 1) bits &= ~((uint64_t)0xffff << (16 * g));
+                seen[r] = (uint32_t)(bits >> (32 * B)) >> (8 * half);
             }
-        if (masked)
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int e = 0; e < 16; ++e) s[t][e] = where_bit((uint32_t)(seen >> (32 * t)), 16 * (e / 8) + e % 8, s[t][e], -__builtin_inff());
-#pragma unroll
-        for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int e = 0; e < 16; ++e) most = fmaxf(most, s[t][e]);
-        most = max_of_halves(most);
-        if (__any(most > m)) {                           // weights are 1 at most, and 2^-8 or more for the largest
-            const float next = most > m ? most + 8.0f : m, fall = __builtin_amdgcn_exp2f(m - next);
-            l *= fall;
-            m = next;
-#pragma unroll
-            for (int t = 0; t < DP / 32; ++t) o[t] *= fall;
         }
-        u4 p[4], rest[4];
+        constexpr int STEPS = DP / 16, DT = DP / 32, QK = R * STEPS, PV = R * 2 * DT;
+        u4 k_ahead[2], v_ahead[2];
+        f4 ks[2], vs[2];
+        k_ahead[0] = k_operand(k_at, 0);
+        v_ahead[0] = v_operand(v_at, 1 - B, 0, 0);
+        ks[0] = *(const f4 *)scales;
+        vs[0] = *(const f4 *)(scales + BN);
+        float sum[R], w[R][2];
+        uint32_t pinned[R];
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int r = 0; r < R; ++r) sum[r] = 0.0f;
+        __builtin_amdgcn_sched_barrier(0);
+        unrolled<16>([&](auto step) {
+            constexpr int N = decltype(step)::value;
+            // the matrix unit's share
+            unrolled<(N + 1) * QK / 16 - N * QK / 16>([&](auto x) {
+                constexpr int M = N * QK / 16 + decltype(x)::value, U = M / R, r = M % R;
+                if constexpr (r == 0 && U + 1 < STEPS) k_ahead[(U + 1) & 1] = k_operand(k_at, U + 1);
+                s[1 - B][r] = mfma32(E{}, k_ahead[U & 1], q[r][U], U == 0 ? (f16v)(0.0f) : s[1 - B][r]);
+            });
+            unrolled<(N + 1) * PV / 16 - N * PV / 16>([&](auto x) {
+                constexpr int M = N * PV / 16 + decltype(x)::value, V = M / R, r = M % R, U = V / DT, t = V % DT;
+                if constexpr (r == 0 && V + 1 < 2 * DT) v_ahead[(V + 1) & 1] = v_operand(v_at, 1 - B, (V + 1) / DT, (V + 1) % DT);
+                if constexpr (SPLIT) o[r][t] = mfma32(BF16{}, v_ahead[V & 1], rest[1 - B][r][U], o[r][t]);
+                o[r][t] = mfma32(BF16{}, v_ahead[V & 1], p[1 - B][r][U], o[r][t]);
+            });
+            // the weights: keys 16 (N / 8) + 8 half + N % 8 of the block
+            if constexpr (N % 4 == 0 && N + 4 < 16) {
+                constexpr int G = N / 4 + 1;
+                ks[G & 1] = *(const f4 *)(scales + 16 * (G / 2) + 4 * (G % 2));
+                vs[G & 1] = *(const f4 *)(scales + BN + 16 * (G / 2) + 4 * (G % 2));
+            }
 #pragma unroll
-            for (int e = 0; e < 16; e += 4) {
-                const f4 by = *(const f4 *)(scales + BN + 32 * t + 16 * (e / 8) + e % 8);
-                float w[4];
-#pragma unroll
-                for (int x = 0; x < 4; ++x) {
-                    w[x] = __builtin_amdgcn_exp2f(s[t][e + x] - m);
-                    l += w[x];
-                    w[x] *= by[x];
-                }
-                if (masked)                              // (a hidden key's scale may be NaN)
-#pragma unroll
-                    for (int x = 0; x < 4; ++x) w[x] = where_bit((uint32_t)(seen >> (32 * t)), 16 * (e / 8) + e % 8 + x, w[x], 0.0f);
-#pragma unroll
-                for (int x = 0; x < 4; x += 2) {
-                    const int u = 2 * t + e / 8, to = (e % 8 + x) / 2;
+            for (int r = 0; r < R; ++r) {
+                float x = __builtin_fmaf(s[B][r][N], ks[N / 4 & 1][N % 4], -m[r]);
+                if constexpr (MASKED) x = where_bit(seen[r], 16 * (N / 8) + N % 8, x, -__builtin_inff());
+                x = __builtin_amdgcn_exp2f(x);
+                sum[r] += x;
+                x *= vs[N / 4 & 1][N % 4];
+                if constexpr (MASKED) x = where_bit(seen[r], 16 * (N / 8) + N % 8, x, 0.0f);     // (a hidden key's scale may be NaN)
+                w[r][N % 2] = x;
+                if constexpr (N % 2 == 1) {
                     if constexpr (SPLIT) {
-                        const u2 both = split2(w[x], w[x + 1]);
-                        p[u][to] = both[0];
-                        rest[u][to] = both[1];
+                        const u2 both = split2(w[r][0], w[r][1]);
+                        p[B][r][N / 8][N % 8 / 2] = both[0];
+                        rest[B][r][N / 8][N % 8 / 2] = both[1];
                     } else {
-                        p[u][to] = pack2<BF16>(w[x], w[x + 1]);
+                        p[B][r][N / 8][N % 8 / 2] = pack2<BF16>(w[r][0], w[r][1]);
+                    }
+                    pinned[r] = p[B][r][N / 8][N % 8 / 2];
+                    asm volatile("" : "+v"(pinned[r]));          // (formed here, beside the matrix unit's work, and not where it is wanted)
+                    p[B][r][N / 8][N % 8 / 2] = pinned[r];
+                }
+            }
+            // the next tile's codes
+            unrolled<(N + 1) * 4 * PIECES / 16 - N * 4 * PIECES / 16>([&](auto x) {
+                store_step(Index<B>{}, Index<N * 4 * PIECES / 16 + decltype(x)::value>{}, to);
+            });
+            __builtin_amdgcn_sched_barrier(0);
+        });
+        // Weights stay relative to what was the largest score once, as long as their sums are moderate (bf16 and float lose nothing by that).
+        bool more = false;
+#pragma unroll
+        for (int r = 0; r < R; ++r) more = more || sum[r] > kMostSum;
+        if (__any(more)) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                float most = m[r];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    float x = s[B][r][e] * scales[16 * (e / 8) + e % 8];
+                    if constexpr (MASKED) x = where_bit(seen[r], 16 * (e / 8) + e % 8, x, -__builtin_inff());
+                    most = fmaxf(most, x);
+                }
+                most = max_of_halves(most);
+                const float fall = __builtin_amdgcn_exp2f(m[r] - most);
+                m[r] = most;
+                l[r] *= fall;
+                sum[r] = 0.0f;
+#pragma unroll
+                for (int t = 0; t < DT; ++t) {           // (one after the other, and not before the branch: or the registers would not do)
+                    asm volatile("" : "+a"(o[r][t]));
+                    o[r][t] *= fall;
+                    asm volatile("" : "+a"(o[r][t]));
+                }
+#pragma unroll
+                for (int e = 0; e < 16; e += 2) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        const int of = 16 * (e / 8) + e % 8 + h;
+                        float x = __builtin_fmaf(s[B][r][e + h], scales[of], -m[r]);
+                        if constexpr (MASKED) x = where_bit(seen[r], of, x, -__builtin_inff());
+                        x = __builtin_amdgcn_exp2f(x);
+                        sum[r] += x;
+                        x *= scales[BN + of];
+                        if constexpr (MASKED) x = where_bit(seen[r], of, x, 0.0f);
+                        w[r][h] = x;
+                    }
+                    if constexpr (SPLIT) {
+                        const u2 both = split2(w[r][0], w[r][1]);
+                        p[B][r][e / 8][e % 8 / 2] = both[0];
+                        rest[B][r][e / 8][e % 8 / 2] = both[1];
+                    } else {
+                        p[B][r][e / 8][e % 8 / 2] = pack2<BF16>(w[r][0], w[r][1]);
                     }
                 }
             }
+        }
 #pragma unroll
-        for (int u = 0; u < 4; ++u)
+        for (int r = 0; r < R; ++r) l[r] += sum[r];
+    };
+    if (count > 0) {
+        unrolled<4 * PIECES>([&](auto x) { store_step(Index<0>{}, x, lds); });
+        unrolled<4 * PIECES>([&](auto x) { store_step(Index<1>{}, x, lds); });
+        store_scales(0);
+        uint32_t lost = (uint32_t)__ballot(places < 0) & 15u;    // blocks of the tile that are not there
+        auto next = [&](int i) {                                 // (past the end: the last tile again)
+            if (i < count && (i & 15) == 0) places = look_up(i);
+            return min(i, count - 1) & 15;
+        };
+        int n = next(1);
+        uint32_t lost_next = (uint32_t)(__ballot(places < 0) >> (4 * n)) & 15u;
+        load_k(places, n);
+        load_v(places, n);
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < DP / 16; ++u)
+#pragma unroll
+            for (int r = 0; r < R; ++r) s[0][r] = mfma32(E{}, k_operand(lds, u), q[r][u], u == 0 ? (f16v)(0.0f) : s[0][r]);
+        int i = 0;
+        auto whole = [&]() {                                     // (the same in all lanes, which the compiler has to see)
+            const int key0 = BN * list.at(first + i);
+            return __builtin_amdgcn_readfirstlane(!lost && row_first.sees_all(key0, a.sinks) && row_last.sees_all(key0, a.sinks)) != 0;
+        };
+        auto step = [&](auto masked) {
+            store_scales(i + 1);
+            block(Index<0>{}, masked, i, lost);
+            n = next(i + 2);
+            load_k(places, n);
+            __syncthreads();
+            block(Index<1>{}, masked, i, lost);
+            load_v(places, n);
+            lost = lost_next;
+            lost_next = (uint32_t)(__ballot(places < 0) >> (4 * n)) & 15u;
+            ++i;
+        };
+        while (i < count) {                                      // (two loops, not a choice in one: that would keep the sums twice)
+            while (i < count && whole()) step(Index<0>{});
+            while (i < count && !whole()) step(Index<1>{});
+        }
+        const uint8_t *const v_at = lds + (count - 1 & 1) * C::kTile;
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int t = 0; t < DP / 32; ++t) {
-                const u4 x = *(const u4 *)(at + v_row + (v_chunk ^ 32 * u) + t * 32 * BN * 2);
-                if constexpr (SPLIT) o[t] = mfma32(BF16{}, x, rest[u], o[t]);
-                o[t] = mfma32(BF16{}, x, p[u], o[t]);
+                const u4 x = v_operand(v_at, 1, u, t);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    if constexpr (SPLIT) o[r][t] = mfma32(BF16{}, x, rest[1][r][u], o[r][t]);
+                    o[r][t] = mfma32(BF16{}, x, p[1][r][u], o[r][t]);
+                }
             }
     }
-    l = sum_of_halves(l);
-    if (parts > 1) {
-        f4 *mine = a.part_data + (int64_t)blockIdx.x * C::kPart + tid;
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        const float weight = sum_of_halves(l[r]);
+        const int row = min(row0 + 32 * r + col, rows - 1);
+        if (parts > 1) {
+            f4 *mine = a.part_data + (int64_t)blockIdx.x * C::kPart + r * C::NW * 64 + tid;
+#pragma unroll
+            for (int t = 0; t < DP / 32; ++t)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    mine[(4 * t + i) * R * C::NW * 64] = (f4){o[r][t][4 * i], o[r][t][4 * i + 1], o[r][t][4 * i + 2], o[r][t][4 * i + 3]};
+            mine[DP / 8 * R * C::NW * 64] = (f4){m[r], weight, 0.0f, 0.0f};
+            continue;
+        }
+        // ---- O = O^T / l: 4 consecutive elements per lane and quarter, exchanged between lane halves to 8 ----
+        T *to = (T *)a.o.data + (tile.seq.first + row / group) * a.o.token_stride + (head * group + row % group) * a.o.head_stride;
+        const float by = 1.0f / weight;
 #pragma unroll
         for (int t = 0; t < DP / 32; ++t)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) mine[(4 * t + i) * C::BM * 2] = (f4){o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
-        mine[DP / 8 * C::BM * 2] = (f4){m, l, 0.0f, 0.0f};
-        return;
-    }
-    // ---- O = O^T / l: 4 consecutive elements per lane and quarter, exchanged between lane halves to 8 ----
-    T *out = (T *)a.o.data + (tile.seq.first + query) * a.o.token_stride + qhead * a.o.head_stride;
+            for (int i = 0; i < 16; i += 8) {
+                float x[8];
 #pragma unroll
-    for (int t = 0; t < DP / 32; ++t)
+                for (int e = 0; e < 8; ++e) x[e] = weight == 0.0f ? 0.0f : o[r][t][i + e] * by;
+                const u2 s0 = __builtin_amdgcn_permlane32_swap(pack2<E>(x[0], x[1]), pack2<E>(x[4], x[5]), false, false);
+                const u2 s1 = __builtin_amdgcn_permlane32_swap(pack2<E>(x[2], x[3]), pack2<E>(x[6], x[7]), false, false);
+                const u4 y = {s0[0], s1[0], s0[1], s1[1]};
+                const int d = 32 * t + 2 * i + 8 * half;
+                if (row0 + 32 * r + col < rows && d < D) {
+                    if constexpr (VEC) {
+                        *(u4 *)(to + d) = y;
+                    } else {
+                        T e8[8];
+                        __builtin_memcpy(e8, &y, 16);
 #pragma unroll
-        for (int i = 0; i < 16; i += 8) {
-            float x[8];
-#pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = l == 0.0f ? 0.0f : o[t][i + e] / l;
-            const u2 s0 = __builtin_amdgcn_permlane32_swap(pack2<E>(x[0], x[1]), pack2<E>(x[4], x[5]), false, false);
-            const u2 s1 = __builtin_amdgcn_permlane32_swap(pack2<E>(x[2], x[3]), pack2<E>(x[6], x[7]), false, false);
-            const u4 y = {s0[0], s1[0], s0[1], s1[1]};
-            const int d = 32 * t + 2 * i + 8 * half;
-            if (row_there && d < D) {
-                if constexpr (VEC) {
-                    *(u4 *)(out + d) = y;
-                } else {
-                    T e8[8];
-                    __builtin_memcpy(e8, &y, 16);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) out[d + e] = e8[e];
+                        for (int e = 0; e < 8; ++e) to[d + e] = e8[e];
+                    }
                 }
             }
-        }
+    }
 }
 
 // The parts of a tile, joined in their order: a workgroup per tile and piece of 4 elements of a lane.
-template <class E, class C, bool VEC>
-__global__ __launch_bounds__(C::BM * 2) void attention_chunk_join_kernel(const ChunkArgs a)
+template <class E, class C>
+__global__ __launch_bounds__(C::NW * 64 * C::R) void attention_chunk_join_kernel(const ChunkArgs a)
 {
-    constexpr int THREADS = C::BM * 2, PIECES = C::DP / 8;
+    constexpr int THREADS = C::NW * 64 * C::R, PIECES = C::DP / 8;
     const int piece = blockIdx.x % PIECES, kv_heads = a.cache.kv_heads, head = blockIdx.x / PIECES % kv_heads, number = blockIdx.x / PIECES / kv_heads;
     const ChunkTile<C> tile = ChunkTile<C>::find(a, a.slots - 1 - number);
-    const int tid = threadIdx.x, lane = tid & 63, row = tile.row0 + 32 * (tid >> 6) + (lane & 31);
+    const int tid = threadIdx.x, lane = tid & 63, row = tile.row0 + 32 * (C::R * (tid >> 6 & 3) + (tid >> 8)) + (lane & 31);
     const int d = 8 * piece + 4 * (lane >> 5);                   // 32 (piece / 4) + 8 (piece % 4) + ..
     if (!tile.there || row >= tile.rows || d >= a.cache.head_dim) return;
     const int parts = max(1, min(a.parts, (tile.keys(a).count + a.run - 1) / a.run));

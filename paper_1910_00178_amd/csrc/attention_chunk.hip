@@ -12,18 +12,18 @@ namespace {
 constexpr int64_t kUnits = 256;
 // Rows of a sequence that attention_chunk_few_kernel takes at most: heads of more than 128 leave no registers for two tiles of 16.
 constexpr int64_t few_rows_of(int64_t head_dim) { return head_dim <= 128 ? 32 : 16; }
-constexpr int64_t kManyRows = 128;
 
-// f(ChunkCfg<...>{}) for the smallest DP that holds head_dim.
+// f(ChunkCfg<...>{}) for the smallest DP that holds head_dim.  `wide`: 256 rows a workgroup where there are registers for it.
 template <class F>
-void with_chunk_form(int64_t head_dim, F &&f)
+void with_chunk_form(int64_t head_dim, bool wide, F &&f)
 {
-    if (head_dim <= 64) f(ChunkCfg<64, 2>{});
-    else if (head_dim <= 96) f(ChunkCfg<96, 2>{});
-    else if (head_dim <= 128) f(ChunkCfg<128, 2>{});
-    else if (head_dim <= 192) f(ChunkCfg<192, 1>{});
-    else f(ChunkCfg<256, 1>{});
+    if (head_dim <= 64) wide ? f(ChunkCfg<64, 2, 1>{}) : f(ChunkCfg<64, 1, 2>{});
+    else if (head_dim <= 96) wide ? f(ChunkCfg<96, 2, 1>{}) : f(ChunkCfg<96, 1, 2>{});
+    else if (head_dim <= 128) wide ? f(ChunkCfg<128, 2, 1>{}) : f(ChunkCfg<128, 1, 2>{});
+    else if (head_dim <= 192) f(ChunkCfg<192, 1, 1>{});
+    else f(ChunkCfg<256, 1, 1>{});
 }
+int64_t tile_rows(int64_t head_dim, bool wide) { return wide && head_dim <= 128 ? 256 : 128; }
 
 // Tiles of keys that `queries` consecutive tokens of a sequence see at most.
 int64_t most_tiles(int64_t queries, int64_t max_length, int64_t window, int64_t sinks)
@@ -36,6 +36,7 @@ int64_t most_tiles(int64_t queries, int64_t max_length, int64_t window, int64_t 
 struct ChunkCut {
     int64_t few_rows = 0;                                        // 0: no sequence can have so few
     int64_t few_run = 1, few_parts = 1, slots = 0, run = 1, parts = 1;           // slots 0: no sequence can have more
+    bool wide = false;
     size_t few_bytes = 0, bytes = 0;
 };
 ChunkCut chunk_cut(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t tokens, int64_t max_new, int64_t max_length,
@@ -52,14 +53,16 @@ ChunkCut chunk_cut(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t hea
         if (cut.few_parts > 1) cut.few_bytes = (size_t)(grid * cut.few_parts * cut.few_rows * (head_dim / 4 + 1) * 16);
     }
     if (most_new * group > cut.few_rows) {
-        cut.slots = tokens * group / kManyRows + batch;
-        const int64_t tiles = std::max<int64_t>(1, most_tiles(std::min(most_new, kManyRows / group + 2), max_length, window, sinks));
-        const int64_t grid = std::max(batch, (tokens * group + kManyRows - 1) / kManyRows) * kv_heads;
-        cut.run = std::max<int64_t>((tiles * grid + 2 * kUnits - 1) / (2 * kUnits), 4);
-        cut.parts = grid >= 2 * kUnits ? 1 : (tiles + cut.run - 1) / cut.run;
+        cut.wide = tokens * group / batch >= 256;
+        const int64_t height = tile_rows(head_dim, cut.wide), places = cut.wide || head_dim > 128 ? kUnits : 2 * kUnits;
+        cut.slots = tokens * group / height + batch;
+        const int64_t tiles = std::max<int64_t>(1, most_tiles(std::min(most_new, height / group + 2), max_length, window, sinks));
+        const int64_t grid = std::max(batch, (tokens * group + height - 1) / height) * kv_heads;
+        cut.run = std::max<int64_t>((tiles * grid + places - 1) / places, 4);
+        cut.parts = grid >= places ? 1 : (tiles + cut.run - 1) / cut.run;
         if (cut.parts == 1) cut.run = tiles;
         else
-            with_chunk_form(head_dim, [&](auto form) { cut.bytes = (size_t)(cut.slots * kv_heads * cut.parts) * decltype(form)::kPart * 16; });
+            with_chunk_form(head_dim, cut.wide, [&](auto form) { cut.bytes = (size_t)(cut.slots * kv_heads * cut.parts) * decltype(form)::kPart * 16; });
     }
     return cut;
 }
@@ -68,7 +71,7 @@ bool sizes_ok(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim
               int64_t sinks)
 {
     return batch >= 0 && batch <= kMaxCount && q_heads >= 1 && q_heads <= 65536 && kv_heads >= 1 && q_heads % kv_heads == 0 && head_dim_ok(head_dim) &&
-           tokens >= 0 && tokens <= kMaxCount && (tokens + kManyRows * batch) * q_heads <= kMaxCount && max_new >= 0 && max_new <= kMaxCount && max_length >= 0 &&
+           tokens >= 0 && tokens <= kMaxCount && (tokens + 256 * batch) * q_heads <= kMaxCount && max_new >= 0 && max_new <= kMaxCount && max_length >= 0 &&
            max_length <= kMaxLength && window >= 0 && window <= kMaxLength && sinks >= 0 && sinks <= kMaxLength;
 }
 
@@ -92,7 +95,7 @@ bool launch_many(const ChunkArgs &a, int device, hipStream_t st)
     if (!allow_lds<ManyForm<E, C, VEC>, C::kLds>(device, attention_chunk_kernel<E, C, VEC>)) return false;
     const unsigned units = (unsigned)(a.slots * a.cache.kv_heads);
     hipLaunchKernelGGL((attention_chunk_kernel<E, C, VEC>), dim3(units * a.parts), dim3(C::NW * 64), C::kLds, st, a);
-    if (a.parts > 1) hipLaunchKernelGGL((attention_chunk_join_kernel<E, C, VEC>), dim3(units * (C::DP / 8)), dim3(C::BM * 2), 0, st, a);
+    if (a.parts > 1) hipLaunchKernelGGL((attention_chunk_join_kernel<E, C>), dim3(units * (C::DP / 8)), dim3(C::NW * 64 * C::R), 0, st, a);
     return true;
 }
 
@@ -103,9 +106,8 @@ bool launch_chunk(ChunkArgs a, const ChunkCut &cut, bool vec, uint8_t *workspace
     a.few_rows = (int32_t)cut.few_rows;
     if (cut.slots > 0) {
         a.run = (int32_t)cut.run, a.parts = (int32_t)cut.parts, a.slots = (int32_t)cut.slots, a.part_data = (f4 *)workspace;
-        with_chunk_form(a.cache.head_dim, [&](auto form) {
+        with_chunk_form(a.cache.head_dim, cut.wide, [&](auto form) {
             typedef decltype(form) C;
-            static_assert(C::BM == kManyRows, "one height of tiles");
             ok = vec ? launch_many<E, C, true>(a, device, st) : launch_many<E, C, false>(a, device, st);
         });
     }
@@ -165,7 +167,7 @@ ngemm_status ngemm_attention_chunk(ngemm_ctx *ctx, const ngemm_kv_cache *cache, 
     DeviceGuard g(ctx->device);
     if (!g.ok) return NGEMM_ERR_DEVICE;
     const ChunkArgs a{view_of(cache, pages_dev, pages_stride), q, o, offsets_dev, starts_dev, (int32_t)batch, (int32_t)q_heads, (int32_t)tokens, (int32_t)max_new,
-                      (int32_t)max_length, (int32_t)window, (int32_t)sinks, scale * 1.44269504f, 0, 1, 1, 0, nullptr, in_pieces(o, type)};
+                      pages_stride > 0 ? (int32_t)max_length : 0, (int32_t)window, (int32_t)sinks, scale * 1.44269504f, 0, 1, 1, 0, nullptr, in_pieces(o, type)};
     const bool vec = in_pieces(q, type) && in_pieces(o, type);
     hipStream_t st = (hipStream_t)hip_stream;
     const bool ok = type == NGEMM_F16 ? launch_chunk<F16>(a, cut, vec, (uint8_t *)workspace_dev, ctx->device, st)

@@ -137,7 +137,7 @@ def test_workspace_stays_small(ctx):
         for new in (1, 2, 16, 100, 3000, 70000):
             for heads, kv, dim in ((32, 8, 128), (12, 12, 64), (64, 1, 256), (16, 1, 16)):
                 tokens = batch * new
-                if (tokens + 128 * batch) * heads < 1 << 31:
+                if (tokens + 256 * batch) * heads < 1 << 31:
                     for longest in (new, new + 1000, 1 << 20, 1 << 30):
                         most = max(most, ng.ngemm_attention_chunk_workspace_bytes(batch, heads, kv, dim, tokens, new, longest, 0, 0))
     assert 0 < most < 1 << 30
