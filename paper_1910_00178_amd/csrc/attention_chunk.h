@@ -380,16 +380,17 @@ __global__ __launch_bounds__(kFewJoinThreads) void attention_chunk_few_join_kern
 
 // ---- many rows ----
 
-// DP: head_dim rounded up; R: groups of 32 rows of a wavefront; PER_CU workgroups to a unit.
-template <int DP_, int R_, int PER_CU_>
+// DP: head_dim rounded up; NW wavefronts of 32 rows, PER_SIMD of which share a SIMD's registers.
+template <int DP_, int NW_, int PER_SIMD_>
 struct ChunkCfg {
-    static constexpr int DP = DP_, R = R_, PER_CU = PER_CU_, NW = 4, BM = 32 * R * NW, BN = kChunkKeys;
-    static constexpr int CH = DP / 8;                            // 16-byte pieces of a row of K
-    static constexpr int kTile = BN * DP * 2, kScales = 4 * kTile, kScaleBytes = 2 * BN * 4, kLds = kScales + 3 * kScaleBytes;     // two of K, two of V, three of scales
-    static constexpr int PIECES = 4 * DP / (NW * 64) + (4 * DP % (NW * 64) != 0);        // of 16 codes of K (and of V) per thread
-    static constexpr int kPart = NW * 64 * R * (DP / 8 + 1);     // 16-byte pieces of a part: sums, maximum and weight
-    static __device__ __forceinline__ int k_swizzle(int j) { return CH % 16 == 0 ? j & 15 : CH % 8 == 0 ? (j >> 1) & 7 : (j >> 2) & 3; }
-    static __device__ __forceinline__ int v_swizzle(int d) { return (d >> 1) & 7; }
+    static constexpr int DP = DP_, NW = NW_, PER_SIMD = PER_SIMD_, BM = 32 * NW, BN = kChunkKeys;
+    // rows in LDS: of K (a key's elements) and of V (an element's keys), 16 bytes apart more than they are long, so that 16 consecutive ones' equal pieces
+    // fall on different banks (64 of 4 bytes) without a turn of addresses
+    static constexpr int kKeyRow = 2 * DP + 16, kValueRow = 2 * BN + 16;
+    static constexpr int kKeys = BN * kKeyRow, kValues = DP * kValueRow, kValuesAt = 2 * kKeys, kScalesAt = kValuesAt + 2 * kValues, kScales = 2 * BN * 4;
+    static constexpr int kLds = kScalesAt + 3 * kScales;         // two tiles of K, two of V, three of scales
+    static constexpr int PIECES = (4 * DP + NW * 64 - 1) / (NW * 64);                    // of 16 codes of K (and of V) per thread
+    static constexpr int kPart = BM * 2 * (DP / 8 + 1);          // 16-byte pieces of a part: sums, maximum and weight
 };
 
 // A tile of a sequence's rows, heads fastest, and its share of the keys.
@@ -415,10 +416,10 @@ struct ChunkTile {
 };
 
 template <class E, class C, bool VEC>
-__global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_chunk_kernel(const ChunkArgs a)
+__global__ __launch_bounds__(C::NW * 64, C::PER_SIMD) void attention_chunk_kernel(const ChunkArgs a)
 {
     extern __shared__ __align__(1024) uint8_t lds[];
-    constexpr int DP = C::DP, BN = C::BN, R = C::R, PIECES = C::PIECES;
+    constexpr int DP = C::DP, BN = C::BN, NW = C::NW, PIECES = C::PIECES, STEPS = DP / 16, DT = DP / 32;
     constexpr bool SPLIT = __is_same(typename E::T, _Float16);   // two bf16 numbers per weight
     typedef typename E::T T;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, col = lane & 31;
@@ -432,242 +433,221 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_c
     if (part >= parts) return;
     const int first = (int)((int64_t)list.count * part / parts), count = (int)((int64_t)list.count * (part + 1) / parts) - first;
 
-    const int row0 = tile.row0 + 32 * R * wave;                  // the wavefront's
-    const ChunkRow row_first = tile.row(a, row0), row_last = tile.row(a, row0 + 32 * R - 1);
-    ChunkRow range[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) range[r] = tile.row(a, row0 + 32 * r + col);
+    const int row0 = tile.row0 + 32 * wave, row = min(row0 + col, rows - 1);             // the wavefront's first, the lane's
+    const ChunkRow range = tile.row(a, row), row_first = tile.row(a, row0), row_last = tile.row(a, row0 + 31);
 
     // ---- the blocks of 16 tiles: lane l looks up block l % 4 of tile l / 4 ----
     const int block_bytes = 32 * D + 128;
-    auto look_up = [&](int i) {
-        const int index = 4 * list.at(min(first + i + (lane >> 2), list.count - 1)) + (lane & 3);
-        return chunk_place(a, tile.b, head, index);
-    };
+    auto look_up = [&](int i) { return chunk_place(a, tile.b, head, 4 * list.at(min(first + i + (lane >> 2), list.count - 1)) + (lane & 3)); };
     // ---- a tile's codes, and where they go as 16-bit floats ----
     // (all threads store: those past the last piece others' again, those past head_dim something finite where it meets Q's zeros or becomes no output)
     int piece_block[PIECES], piece_at[PIECES], k_to[PIECES], v_to[PIECES];
 #pragma unroll
     for (int i = 0; i < PIECES; ++i) {
-        const int p = (i * C::NW * 64 + tid) % (4 * DP), q = p % DP, per = D / 16, token = q < D ? q / per : 0, c = 2 * (q < D ? q % per : per);
+        const int p = (i * NW * 64 + tid) % (4 * DP), q = p % DP, per = D / 16, token = q < D ? q / per : 0, c = 2 * (q < D ? q % per : per);
         piece_block[i] = p / DP;
         piece_at[i] = q < D ? 16 * q : 0;
-        const int j = 16 * piece_block[i] + token;
-        k_to[i] = j * DP * 2 + (c ^ C::k_swizzle(j)) * 16;       // (the second half of its 32 bytes: where bit 4 is turned)
-        v_to[i] = 2 * C::kTile + q * BN * 2 + (2 * piece_block[i] ^ C::v_swizzle(q)) * 16;
+        k_to[i] = (16 * piece_block[i] + token) * C::kKeyRow + c * 16;
+        v_to[i] = C::kValuesAt + q * C::kValueRow + piece_block[i] * 32;
     }
     u4 k_codes[PIECES], v_codes[PIECES];
-    float a_scale = 0.0f;                                        // even wavefronts: K's of key `lane`, odd ones: V's
+    float a_scale = 0.0f;                                        // of block `wave` % 4: lanes 0 .. 15 K's, 16 .. 31 V's
+    // block b of tile n of those looked up; the pieces of a wavefront are of one block mostly, which the scalar unit finds
+    auto block_of = [&](int places, int b) { return a.cache.data + (int64_t)max(__builtin_amdgcn_readlane(places, b), 0) * block_bytes; };
+    auto block_of_piece = [&](int places, int n, int i) {
+        if constexpr (DP % 64 == 0) return block_of(places, 4 * n + (i * NW + wave) * 64 / DP % 4);
+        else return a.cache.data + (int64_t)max(__shfl(places, 4 * n + piece_block[i]), 0) * block_bytes;
+    };
     auto load_k = [&](int places, int n) {
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i)
-            k_codes[i] = *(const u4 *)(a.cache.data + (int64_t)max(__shfl(places, 4 * n + piece_block[i]), 0) * block_bytes + piece_at[i]);
-        const uint8_t *block = a.cache.data + (int64_t)max(__shfl(places, 4 * n + (lane >> 4)), 0) * block_bytes + 32 * D;
-        a_scale = *(const float *)(block + 64 * (wave & 1) + 4 * (lane & 15));
+        for (int i = 0; i < PIECES; ++i) k_codes[i] = *(const u4 *)(block_of_piece(places, n, i) + (uint32_t)piece_at[i]);
+        a_scale = *(const float *)(block_of(places, 4 * n + wave % 4) + (uint32_t)(32 * D + 4 * (lane & 31)));
     };
     auto load_v = [&](int places, int n) {
 #pragma unroll
-        for (int i = 0; i < PIECES; ++i)
-            v_codes[i] = *(const u4 *)(a.cache.data + (int64_t)max(__shfl(places, 4 * n + piece_block[i]), 0) * block_bytes + 16 * D + piece_at[i]);
+        for (int i = 0; i < PIECES; ++i) v_codes[i] = *(const u4 *)(block_of_piece(places, n, i) + (uint32_t)(16 * D + piece_at[i]));
     };
-    // dword x % 4 of piece x / 4, stored with the piece's last
-    u4 out[2];
-    auto store_step = [&](auto which, auto x, uint8_t *at) {
+    // dword x % 4 of piece x / 4, stored with the second and the fourth
+    u4 out;
+    auto store_step = [&](auto which, auto x, int buffer) {
         constexpr int X = decltype(x)::value, I = X / 4, W = X % 4;
         constexpr bool V = decltype(which)::value;
-        const uint32_t codes = V ? v_codes[I][W] : k_codes[I][W];
         u2 y;
-        if constexpr (V) y = codes4_to(BF16{}, codes);
-        else y = codes4_to(E{}, codes);
-        out[W / 2][2 * (W % 2)] = y[0];
-        out[W / 2][2 * (W % 2) + 1] = y[1];
-        if constexpr (W % 2 == 1) *(u4 *)(at + ((V ? v_to[I] : k_to[I]) ^ (W / 2 * 16))) = out[W / 2];
+        if constexpr (V) y = codes4_to(BF16{}, v_codes[I][W]);
+        else y = codes4_to(E{}, k_codes[I][W]);
+        out[2 * (W % 2)] = y[0];
+        out[2 * (W % 2) + 1] = y[1];
+        if constexpr (W % 2 == 1) *(u4 *)(lds + buffer * (V ? C::kValues : C::kKeys) + (V ? v_to[I] : k_to[I]) + W / 2 * 16) = out;
     };
     auto store_scales = [&](int tile_number) {
-        ((float *)(lds + C::kScales + tile_number % 3 * C::kScaleBytes))[tid & 127] = a_scale * (wave & 1 ? 1.0f : a.scale);
+        ((float *)(lds + C::kScalesAt + tile_number % 3 * C::kScales))[(lane >> 4 & 1) * BN + 16 * (wave % 4) + (lane & 15)] = a_scale * (lane & 16 ? 1.0f : a.scale);
     };
     // elements past head_dim, and what stands for the values before the first block's, are 0
-    for (int i = tid; i < (D < DP ? 4 * C::kTile : C::kTile) / 16; i += C::NW * 64) ((u4 *)(lds + (D < DP ? 0 : 3 * C::kTile)))[i] = (u4)(0u);
+    for (int i = (D < DP ? 0 : C::kValuesAt + C::kValues) / 16 + tid; i < C::kScalesAt / 16; i += NW * 64) ((u4 *)lds)[i] = (u4)(0u);
     if (D < DP) __syncthreads();
     int places = count > 0 ? look_up(0) : -1;
     load_k(places, 0);
     load_v(places, 0);
 
     // ---- Q^T's operand: 8 elements of the lane's row per step ----
-    u4 q[R][DP / 16];
+    u4 q[STEPS];
+    const int qhead = head * group + row % group, token = tile.seq.first + row / group;
+    {
+        const T *from = (const T *)a.q.data + token * a.q.token_stride + qhead * a.q.head_stride;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const int row = min(row0 + 32 * r + col, rows - 1);
-        const T *from = (const T *)a.q.data + (tile.seq.first + row / group) * a.q.token_stride + (head * group + row % group) * a.q.head_stride;
-#pragma unroll
-        for (int s = 0; s < DP / 16; ++s) {
+        for (int s = 0; s < STEPS; ++s) {
             const int d = 16 * s + 8 * half;
             const T *at = from + (d < D ? d : 0);
-            if constexpr (VEC) q[r][s] = *(const u4 *)at;
-            else __builtin_memcpy(&q[r][s], at, 16);
-            if (d >= D) q[r][s] = (u4)(0u);
-            asm volatile("" : "+a"(q[r][s]));            // (only the matrix unit reads it: beside the sums, out of the vector unit's registers)
+            if constexpr (VEC) q[s] = *(const u4 *)at;
+            else __builtin_memcpy(&q[s], at, 16);
+            if (d >= D) q[s] = (u4)(0u);
+            asm volatile("" : "+a"(q[s]));               // (only the matrix unit reads it: beside the sums, out of the vector unit's registers)
         }
     }
     // the key whose scores are row `col` of the first product: so that a lane holds 8 consecutive keys' of each 16
     const int key = 16 * (col >> 4) + 8 * (col >> 2 & 1) + 4 * (col >> 3 & 1) + (col & 3);
-    const int k_row = key * DP * 2, v_row = 2 * C::kTile + col * BN * 2;
-    int k_chunk = (half ^ C::k_swizzle(key)) * 16, v_chunk = (half ^ C::v_swizzle(col)) * 16;
+    const uint8_t *const k_from = lds + key * C::kKeyRow + 16 * half, *const v_from = lds + C::kValuesAt + col * C::kValueRow + 16 * half;
+    const float *const ks_from = (const float *)(lds + C::kScalesAt) + 8 * half;
+    const float *const vs_from = (const float *)(lds + C::kScalesAt) + BN + 16 * (lane >> 3 & 1) + 8 * half + (lane & 7);    // lane x of 16: score x's
 
-    f16v o[R][DP / 32], s[2][R];
-    u4 p[2][R][2], rest[2][R][2];
-    float m[R], l[R];
+    f16v o[DT], s[2];
+    u4 p[2][2], rest[2][2];
+    f4 ks[2];                                                    // scales of K of the next four keys, and of V of the block's 16
+    float vs;
+    float m = -3.0e38f, l = 0.0f;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        m[r] = -3.0e38f;
-        l[r] = 0.0f;
+    for (int t = 0; t < DT; ++t) o[t] = (f16v)(0.0f);
 #pragma unroll
-        for (int t = 0; t < DP / 32; ++t) o[r][t] = (f16v)(0.0f);
-#pragma unroll
-        for (int u = 0; u < 2; ++u) p[1][r][u] = rest[1][r][u] = (u4)(0u);
-    }
-    auto k_operand = [&](const uint8_t *at, int u) { return *(const u4 *)(at + k_row + (k_chunk ^ 32 * u)); };
-    auto v_operand = [&](const uint8_t *at, int block, int u, int t) { return *(const u4 *)(at + v_row + (v_chunk ^ (64 * block + 32 * u)) + t * 32 * BN * 2); };
+    for (int u = 0; u < 2; ++u) p[1][u] = rest[1][u] = (u4)(0u);
+    auto k_operand = [&](const uint8_t *at, int u) { return *(const u4 *)(at + 32 * u); };
+    auto v_operand = [&](const uint8_t *at, int u, int t) { return *(const u4 *)(at + t * 32 * C::kValueRow + 32 * u); };
 
     // Block j of 32 keys (B: its parity): the scores of block j become weights while the matrix unit makes those of block j + 1 and takes the weights of
-    // block j - 1 to the values, and codes of the next tile (of K where B is 0, of V where it is 1) become floats: 16 steps, with a score of each row group
-    // and a share of everything else in each.
+    // block j - 1 to the values, and codes of the next tile (of K where B is 0, of V where it is 1) become floats: 16 steps, with one of the lane's scores and a
+    // share of everything else in each.
     constexpr float kMostSum = 0x1p12f;
     auto block = [&](auto parity, auto masked, int i, uint32_t lost) {
         constexpr int B = decltype(parity)::value;
         constexpr bool MASKED = decltype(masked)::value;
-        // (not known to stay the same: one instruction per read is cheaper than the registers of all places)
-        asm volatile("" : "+v"(k_chunk), "+v"(v_chunk));
-        const uint8_t *const k_at = lds + (B == 0 ? i & 1 : ~i & 1) * C::kTile + (B == 0 ? 32 * DP * 2 : 0);     // block j + 1's
-        const uint8_t *const v_at = lds + (B == 0 ? ~i & 1 : i & 1) * C::kTile;                                   // block j - 1's
-        uint8_t *const to = lds + (~i & 1) * C::kTile;
-        const float *const scales = (const float *)(lds + C::kScales + i % 3 * C::kScaleBytes) + 32 * B + 8 * half;
-        uint32_t seen[R];
+        const int odd = i & 1, next = i % 3 == 2 ? 0 : i % 3 + 1;
+        const uint8_t *const k_at = k_from + (B == 0 ? odd : 1 - odd) * C::kKeys + (B == 0 ? 32 * C::kKeyRow : 0);           // block j + 1's
+        const uint8_t *const v_at = v_from + (B == 0 ? 1 - odd : odd) * C::kValues + (B == 0 ? 64 : 0);                      // block j - 1's
+        const float *const scales = ks_from + i % 3 * (C::kScales / 4) + 32 * B;
+        uint32_t seen = 0;
         if constexpr (MASKED) {
-            const int key0 = BN * list.at(first + i);
+            uint64_t bits = range.seen(BN * list.at(first + i), a.sinks);
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                uint64_t bits = range[r].seen(key0, a.sinks);
-#pragma unroll
-                for (int g = 0; g < 4; ++g)
-                    if (lost >> g & 1) bits &= ~((uint64_t)0xffff << (16 * g));
-                seen[r] = (uint32_t)(bits >> (32 * B)) >> (8 * half);
-            }
+            for (int g = 0; g < 4; ++g)
+                if (lost >> g & 1) bits &= ~((uint64_t)0xffff << (16 * g));
+            seen = (uint32_t)(bits >> (32 * B)) >> (8 * half);
         }
-        constexpr int STEPS = DP / 16, DT = DP / 32, QK = R * STEPS, PV = R * 2 * DT;
-        u4 k_ahead[2], v_ahead[2];
-        f4 ks[2], vs[2];
-        k_ahead[0] = k_operand(k_at, 0);
-        v_ahead[0] = v_operand(v_at, 1 - B, 0, 0);
-        ks[0] = *(const f4 *)scales;
-        vs[0] = *(const f4 *)(scales + BN);
-        float sum[R], w[R][2];
-        uint32_t pinned[R];
+        // MFMAS matrix instructions over all steps but the first (their operands are on their way), scores and values in turn, operands read AHEAD
+        constexpr int MFMAS = 2 * STEPS, AHEAD = 1, RING = AHEAD + 1;
+        u4 k_ahead[RING], v_ahead[RING];
 #pragma unroll
-        for (int r = 0; r < R; ++r) sum[r] = 0.0f;
+        for (int u = 0; u < AHEAD; ++u) {
+            k_ahead[u] = k_operand(k_at, u);
+            v_ahead[u] = v_operand(v_at, u / DT, u % DT);
+        }
+        float sum = 0.0f, w[2];
+        float vs_next = 0.0f;
+        uint32_t pinned;
         __builtin_amdgcn_sched_barrier(0);
         unrolled<16>([&](auto step) {
             constexpr int N = decltype(step)::value;
-            // the matrix unit's share
-            unrolled<(N + 1) * QK / 16 - N * QK / 16>([&](auto x) {
-                constexpr int M = N * QK / 16 + decltype(x)::value, U = M / R, r = M % R;
-                if constexpr (r == 0 && U + 1 < STEPS) k_ahead[(U + 1) & 1] = k_operand(k_at, U + 1);
-                s[1 - B][r] = mfma32(E{}, k_ahead[U & 1], q[r][U], U == 0 ? (f16v)(0.0f) : s[1 - B][r]);
-            });
-            unrolled<(N + 1) * PV / 16 - N * PV / 16>([&](auto x) {
-                constexpr int M = N * PV / 16 + decltype(x)::value, V = M / R, r = M % R, U = V / DT, t = V % DT;
-                if constexpr (r == 0 && V + 1 < 2 * DT) v_ahead[(V + 1) & 1] = v_operand(v_at, 1 - B, (V + 1) / DT, (V + 1) % DT);
-                if constexpr (SPLIT) o[r][t] = mfma32(BF16{}, v_ahead[V & 1], rest[1 - B][r][U], o[r][t]);
-                o[r][t] = mfma32(BF16{}, v_ahead[V & 1], p[1 - B][r][U], o[r][t]);
-            });
             // the weights: keys 16 (N / 8) + 8 half + N % 8 of the block
-            if constexpr (N % 4 == 0 && N + 4 < 16) {
+            if constexpr (N % 4 == 0) {                  // four keys' scales ahead, the next block's first at last
                 constexpr int G = N / 4 + 1;
-                ks[G & 1] = *(const f4 *)(scales + 16 * (G / 2) + 4 * (G % 2));
-                vs[G & 1] = *(const f4 *)(scales + BN + 16 * (G / 2) + 4 * (G % 2));
+                const float *from = scales + 16 * (G / 2) + 4 * (G % 2);
+                if constexpr (G == 4) from = B == 0 ? scales + 32 : ks_from + next * (C::kScales / 4);
+                ks[G & 1] = *(const f4 *)from;
+                if constexpr (G == 4) vs_next = B == 0 ? vs_from[i % 3 * (C::kScales / 4) + 32] : vs_from[next * (C::kScales / 4)];
             }
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-                float x = __builtin_fmaf(s[B][r][N], ks[N / 4 & 1][N % 4], -m[r]);
-                if constexpr (MASKED) x = where_bit(seen[r], 16 * (N / 8) + N % 8, x, -__builtin_inff());
-                x = __builtin_amdgcn_exp2f(x);
-                sum[r] += x;
-                x *= vs[N / 4 & 1][N % 4];
-                if constexpr (MASKED) x = where_bit(seen[r], 16 * (N / 8) + N % 8, x, 0.0f);     // (a hidden key's scale may be NaN)
-                w[r][N % 2] = x;
-                if constexpr (N % 2 == 1) {
-                    if constexpr (SPLIT) {
-                        const u2 both = split2(w[r][0], w[r][1]);
-                        p[B][r][N / 8][N % 8 / 2] = both[0];
-                        rest[B][r][N / 8][N % 8 / 2] = both[1];
-                    } else {
-                        p[B][r][N / 8][N % 8 / 2] = pack2<BF16>(w[r][0], w[r][1]);
-                    }
-                    pinned[r] = p[B][r][N / 8][N % 8 / 2];
-                    asm volatile("" : "+v"(pinned[r]));          // (formed here, beside the matrix unit's work, and not where it is wanted)
-                    p[B][r][N / 8][N % 8 / 2] = pinned[r];
+            float x = __builtin_fmaf(s[B][N], ks[N / 4 & 1][N % 4], -m);
+            if constexpr (MASKED) x = where_bit(seen, 16 * (N / 8) + N % 8, x, -__builtin_inff());
+            x = __builtin_amdgcn_exp2f(x);
+            sum += x;
+            x *= of_row<N>(vs);
+            if constexpr (MASKED) x = where_bit(seen, 16 * (N / 8) + N % 8, x, 0.0f);            // (a hidden key's scale may be NaN)
+            w[N % 2] = x;
+            if constexpr (N % 2 == 1) {
+                if constexpr (SPLIT) {
+                    const u2 both = split2(w[0], w[1]);
+                    pinned = both[0];
+                    rest[B][N / 8][N % 8 / 2] = both[1];
+                } else {
+                    pinned = pack2<BF16>(w[0], w[1]);
                 }
+                asm volatile("" : "+v"(pinned));         // (formed here, beside the matrix unit's work, and not where it is wanted)
+                p[B][N / 8][N % 8 / 2] = pinned;
             }
+            // the matrix unit's share
+            constexpr int M0 = N < 1 ? 0 : (N - 1) * MFMAS / 15, M1 = N * MFMAS / 15;
+            unrolled<M1 - M0>([&](auto x) {
+                constexpr int M = M0 + decltype(x)::value, U = M / 2;
+                if constexpr (M % 2 == 0) {
+                    if constexpr (U + AHEAD < STEPS) k_ahead[(U + AHEAD) % RING] = k_operand(k_at, U + AHEAD);
+                    s[1 - B] = mfma32(E{}, k_ahead[U % RING], q[U], U == 0 ? (f16v)(0.0f) : s[1 - B]);
+                } else {
+                    if constexpr (U + AHEAD < STEPS) v_ahead[(U + AHEAD) % RING] = v_operand(v_at, (U + AHEAD) / DT, (U + AHEAD) % DT);
+                    if constexpr (SPLIT) o[U % DT] = mfma32(BF16{}, v_ahead[U % RING], rest[1 - B][U / DT], o[U % DT]);
+                    o[U % DT] = mfma32(BF16{}, v_ahead[U % RING], p[1 - B][U / DT], o[U % DT]);
+                }
+            });
             // the next tile's codes
             unrolled<(N + 1) * 4 * PIECES / 16 - N * 4 * PIECES / 16>([&](auto x) {
-                store_step(Index<B>{}, Index<N * 4 * PIECES / 16 + decltype(x)::value>{}, to);
+                store_step(Index<B>{}, Index<N * 4 * PIECES / 16 + decltype(x)::value>{}, 1 - odd);
             });
             __builtin_amdgcn_sched_barrier(0);
         });
         // Weights stay relative to what was the largest score once, as long as their sums are moderate (bf16 and float lose nothing by that).
-        bool more = false;
+        if (__any(sum > kMostSum)) {
+            float most = m;
 #pragma unroll
-        for (int r = 0; r < R; ++r) more = more || sum[r] > kMostSum;
-        if (__any(more)) {
+            for (int e = 0; e < 16; ++e) {
+                float x = s[B][e] * scales[16 * (e / 8) + e % 8];
+                if constexpr (MASKED) x = where_bit(seen, 16 * (e / 8) + e % 8, x, -__builtin_inff());
+                most = fmaxf(most, x);
+            }
+            most = max_of_halves(most);
+            const float fall = __builtin_amdgcn_exp2f(m - most);
+            m = most;
+            l *= fall;
+            sum = 0.0f;
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                float most = m[r];
+            for (int t = 0; t < DT; ++t) {               // (one after the other, and not before the branch: or the registers would not do)
+                asm volatile("" : "+a"(o[t]));
+                o[t] *= fall;
+                asm volatile("" : "+a"(o[t]));
+            }
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    float x = s[B][r][e] * scales[16 * (e / 8) + e % 8];
-                    if constexpr (MASKED) x = where_bit(seen[r], 16 * (e / 8) + e % 8, x, -__builtin_inff());
-                    most = fmaxf(most, x);
+            for (int e = 0; e < 16; e += 2) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const int of = 16 * (e / 8) + e % 8 + h;
+                    float x = __builtin_fmaf(s[B][e + h], scales[of], -m);
+                    if constexpr (MASKED) x = where_bit(seen, of, x, -__builtin_inff());
+                    x = __builtin_amdgcn_exp2f(x);
+                    sum += x;
+                    x *= scales[BN + of];
+                    if constexpr (MASKED) x = where_bit(seen, of, x, 0.0f);
+                    w[h] = x;
                 }
-                most = max_of_halves(most);
-                const float fall = __builtin_amdgcn_exp2f(m[r] - most);
-                m[r] = most;
-                l[r] *= fall;
-                sum[r] = 0.0f;
-#pragma unroll
-                for (int t = 0; t < DT; ++t) {           // (one after the other, and not before the branch: or the registers would not do)
-                    asm volatile("" : "+a"(o[r][t]));
-                    o[r][t] *= fall;
-                    asm volatile("" : "+a"(o[r][t]));
-                }
-#pragma unroll
-                for (int e = 0; e < 16; e += 2) {
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const int of = 16 * (e / 8) + e % 8 + h;
-                        float x = __builtin_fmaf(s[B][r][e + h], scales[of], -m[r]);
-                        if constexpr (MASKED) x = where_bit(seen[r], of, x, -__builtin_inff());
-                        x = __builtin_amdgcn_exp2f(x);
-                        sum[r] += x;
-                        x *= scales[BN + of];
-                        if constexpr (MASKED) x = where_bit(seen[r], of, x, 0.0f);
-                        w[r][h] = x;
-                    }
-                    if constexpr (SPLIT) {
-                        const u2 both = split2(w[r][0], w[r][1]);
-                        p[B][r][e / 8][e % 8 / 2] = both[0];
-                        rest[B][r][e / 8][e % 8 / 2] = both[1];
-                    } else {
-                        p[B][r][e / 8][e % 8 / 2] = pack2<BF16>(w[r][0], w[r][1]);
-                    }
+                if constexpr (SPLIT) {
+                    const u2 both = split2(w[0], w[1]);
+                    p[B][e / 8][e % 8 / 2] = both[0];
+                    rest[B][e / 8][e % 8 / 2] = both[1];
+                } else {
+                    p[B][e / 8][e % 8 / 2] = pack2<BF16>(w[0], w[1]);
                 }
             }
         }
-#pragma unroll
-        for (int r = 0; r < R; ++r) l[r] += sum[r];
+        vs = vs_next;
+        l += sum;
     };
     if (count > 0) {
-        unrolled<4 * PIECES>([&](auto x) { store_step(Index<0>{}, x, lds); });
-        unrolled<4 * PIECES>([&](auto x) { store_step(Index<1>{}, x, lds); });
+        unrolled<4 * PIECES>([&](auto x) { store_step(Index<0>{}, x, 0); });
+        unrolled<4 * PIECES>([&](auto x) { store_step(Index<1>{}, x, 0); });
         store_scales(0);
         uint32_t lost = (uint32_t)__ballot(places < 0) & 15u;    // blocks of the tile that are not there
         auto next = [&](int i) {                                 // (past the end: the last tile again)
@@ -679,10 +659,10 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_c
         load_k(places, n);
         load_v(places, n);
         __syncthreads();
+        ks[0] = *(const f4 *)ks_from;
+        vs = vs_from[0];
 #pragma unroll
-        for (int u = 0; u < DP / 16; ++u)
-#pragma unroll
-            for (int r = 0; r < R; ++r) s[0][r] = mfma32(E{}, k_operand(lds, u), q[r][u], u == 0 ? (f16v)(0.0f) : s[0][r]);
+        for (int u = 0; u < STEPS; ++u) s[0] = mfma32(E{}, k_operand(k_from, u), q[u], u == 0 ? (f16v)(0.0f) : s[0]);
         int i = 0;
         auto whole = [&]() {                                     // (the same in all lanes, which the compiler has to see)
             const int key0 = BN * list.at(first + i);
@@ -704,69 +684,61 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_CU * C::NW / 4) void attention_c
             while (i < count && whole()) step(Index<0>{});
             while (i < count && !whole()) step(Index<1>{});
         }
-        const uint8_t *const v_at = lds + (count - 1 & 1) * C::kTile;
+        const uint8_t *const v_at = v_from + (count - 1 & 1) * C::kValues + 64;
 #pragma unroll
         for (int u = 0; u < 2; ++u)
 #pragma unroll
-            for (int t = 0; t < DP / 32; ++t) {
-                const u4 x = v_operand(v_at, 1, u, t);
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    if constexpr (SPLIT) o[r][t] = mfma32(BF16{}, x, rest[1][r][u], o[r][t]);
-                    o[r][t] = mfma32(BF16{}, x, p[1][r][u], o[r][t]);
-                }
+            for (int t = 0; t < DT; ++t) {
+                const u4 x = v_operand(v_at, u, t);
+                if constexpr (SPLIT) o[t] = mfma32(BF16{}, x, rest[1][u], o[t]);
+                o[t] = mfma32(BF16{}, x, p[1][u], o[t]);
             }
     }
+    const float weight = sum_of_halves(l);
+    if (parts > 1) {
+        f4 *mine = a.part_data + (int64_t)blockIdx.x * C::kPart + tid;
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-        const float weight = sum_of_halves(l[r]);
-        const int row = min(row0 + 32 * r + col, rows - 1);
-        if (parts > 1) {
-            f4 *mine = a.part_data + (int64_t)blockIdx.x * C::kPart + r * C::NW * 64 + tid;
+        for (int t = 0; t < DT; ++t)
 #pragma unroll
-            for (int t = 0; t < DP / 32; ++t)
+            for (int i = 0; i < 4; ++i) mine[(4 * t + i) * NW * 64] = (f4){o[t][4 * i], o[t][4 * i + 1], o[t][4 * i + 2], o[t][4 * i + 3]};
+        mine[DP / 8 * NW * 64] = (f4){m, weight, 0.0f, 0.0f};
+        return;
+    }
+    // ---- O = O^T / l: 4 consecutive elements per lane and quarter, exchanged between lane halves to 8 ----
+    T *to = (T *)a.o.data + token * a.o.token_stride + qhead * a.o.head_stride;
+    const float by = 1.0f / weight;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    mine[(4 * t + i) * R * C::NW * 64] = (f4){o[r][t][4 * i], o[r][t][4 * i + 1], o[r][t][4 * i + 2], o[r][t][4 * i + 3]};
-            mine[DP / 8 * R * C::NW * 64] = (f4){m[r], weight, 0.0f, 0.0f};
-            continue;
+    for (int t = 0; t < DT; ++t)
+#pragma unroll
+        for (int i = 0; i < 16; i += 8) {
+            float x[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[e] = weight == 0.0f ? 0.0f : o[t][i + e] * by;
+            const u2 s0 = __builtin_amdgcn_permlane32_swap(pack2<E>(x[0], x[1]), pack2<E>(x[4], x[5]), false, false);
+            const u2 s1 = __builtin_amdgcn_permlane32_swap(pack2<E>(x[2], x[3]), pack2<E>(x[6], x[7]), false, false);
+            const u4 y = {s0[0], s1[0], s0[1], s1[1]};
+            const int d = 32 * t + 2 * i + 8 * half;
+            if (row0 + col < rows && d < D) {
+                if constexpr (VEC) {
+                    *(u4 *)(to + d) = y;
+                } else {
+                    T e8[8];
+                    __builtin_memcpy(e8, &y, 16);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) to[d + e] = e8[e];
+                }
+            }
         }
-        // ---- O = O^T / l: 4 consecutive elements per lane and quarter, exchanged between lane halves to 8 ----
-        T *to = (T *)a.o.data + (tile.seq.first + row / group) * a.o.token_stride + (head * group + row % group) * a.o.head_stride;
-        const float by = 1.0f / weight;
-#pragma unroll
-        for (int t = 0; t < DP / 32; ++t)
-#pragma unroll
-            for (int i = 0; i < 16; i += 8) {
-                float x[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = weight == 0.0f ? 0.0f : o[r][t][i + e] * by;
-                const u2 s0 = __builtin_amdgcn_permlane32_swap(pack2<E>(x[0], x[1]), pack2<E>(x[4], x[5]), false, false);
-                const u2 s1 = __builtin_amdgcn_permlane32_swap(pack2<E>(x[2], x[3]), pack2<E>(x[6], x[7]), false, false);
-                const u4 y = {s0[0], s1[0], s0[1], s1[1]};
-                const int d = 32 * t + 2 * i + 8 * half;
-                if (row0 + 32 * r + col < rows && d < D) {
-                    if constexpr (VEC) {
-                        *(u4 *)(to + d) = y;
-                    } else {
-                        T e8[8];
-                        __builtin_memcpy(e8, &y, 16);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) to[d + e] = e8[e];
-                    }
-                }
-            }
-    }
 }
 
 // The parts of a tile, joined in their order: a workgroup per tile and piece of 4 elements of a lane.
 template <class E, class C>
-__global__ __launch_bounds__(C::NW * 64 * C::R) void attention_chunk_join_kernel(const ChunkArgs a)
+__global__ __launch_bounds__(C::NW * 64) void attention_chunk_join_kernel(const ChunkArgs a)
 {
-    constexpr int THREADS = C::NW * 64 * C::R, PIECES = C::DP / 8;
+    constexpr int THREADS = C::NW * 64, PIECES = C::DP / 8;
     const int piece = blockIdx.x % PIECES, kv_heads = a.cache.kv_heads, head = blockIdx.x / PIECES % kv_heads, number = blockIdx.x / PIECES / kv_heads;
     const ChunkTile<C> tile = ChunkTile<C>::find(a, a.slots - 1 - number);
-    const int tid = threadIdx.x, lane = tid & 63, row = tile.row0 + 32 * (C::R * (tid >> 6 & 3) + (tid >> 8)) + (lane & 31);
+    const int tid = threadIdx.x, lane = tid & 63, row = tile.row0 + 32 * (tid >> 6) + (lane & 31);
     const int d = 8 * piece + 4 * (lane >> 5);                   // 32 (piece / 4) + 8 (piece % 4) + ..
     if (!tile.there || row >= tile.rows || d >= a.cache.head_dim) return;
     const int parts = max(1, min(a.parts, (tile.keys(a).count + a.run - 1) / a.run));

@@ -17,11 +17,11 @@ constexpr int64_t few_rows_of(int64_t head_dim) { return head_dim <= 128 ? 32 : 
 template <class F>
 void with_chunk_form(int64_t head_dim, bool wide, F &&f)
 {
-    if (head_dim <= 64) wide ? f(ChunkCfg<64, 2, 1>{}) : f(ChunkCfg<64, 1, 2>{});
-    else if (head_dim <= 96) wide ? f(ChunkCfg<96, 2, 1>{}) : f(ChunkCfg<96, 1, 2>{});
-    else if (head_dim <= 128) wide ? f(ChunkCfg<128, 2, 1>{}) : f(ChunkCfg<128, 1, 2>{});
-    else if (head_dim <= 192) f(ChunkCfg<192, 1, 1>{});
-    else f(ChunkCfg<256, 1, 1>{});
+    if (head_dim <= 64) wide ? f(ChunkCfg<64, 8, 2>{}) : f(ChunkCfg<64, 4, 2>{});
+    else if (head_dim <= 96) wide ? f(ChunkCfg<96, 8, 2>{}) : f(ChunkCfg<96, 4, 2>{});
+    else if (head_dim <= 128) wide ? f(ChunkCfg<128, 8, 2>{}) : f(ChunkCfg<128, 4, 2>{});
+    else if (head_dim <= 192) f(ChunkCfg<192, 4, 1>{});
+    else f(ChunkCfg<256, 4, 1>{});
 }
 int64_t tile_rows(int64_t head_dim, bool wide) { return wide && head_dim <= 128 ? 256 : 128; }
 
@@ -95,7 +95,7 @@ bool launch_many(const ChunkArgs &a, int device, hipStream_t st)
     if (!allow_lds<ManyForm<E, C, VEC>, C::kLds>(device, attention_chunk_kernel<E, C, VEC>)) return false;
     const unsigned units = (unsigned)(a.slots * a.cache.kv_heads);
     hipLaunchKernelGGL((attention_chunk_kernel<E, C, VEC>), dim3(units * a.parts), dim3(C::NW * 64), C::kLds, st, a);
-    if (a.parts > 1) hipLaunchKernelGGL((attention_chunk_join_kernel<E, C>), dim3(units * (C::DP / 8)), dim3(C::NW * 64 * C::R), 0, st, a);
+    if (a.parts > 1) hipLaunchKernelGGL((attention_chunk_join_kernel<E, C>), dim3(units * (C::DP / 8)), dim3(C::NW * 64), 0, st, a);
     return true;
 }
 
