@@ -5,6 +5,8 @@
 namespace ngemm {
 
 constexpr int kChunkKeys = 64;                                   // of a tile
+constexpr int kLeastTiles = 4;                                   // of keys, of a workgroup where a tile's are shared out
+constexpr int kMostShared = 128;                                 // sequences of a call that are
 
 struct ChunkArgs {
     CacheView cache;
@@ -14,9 +16,9 @@ struct ChunkArgs {
     int32_t window, sinks;   // window 0: none
     float scale;             // of the scores, times log2 e
     int32_t few_rows;        // sequences of up to so many rows (new tokens times heads that share a K/V head) are attention_chunk_few_kernel's
-    int32_t run, parts;      // tiles of keys of a workgroup at most, workgroups along a sequence
-    int32_t slots;           // tiles of rows (attention_chunk_kernel)
-    f4 *part_data;           // parts > 1: sums, maxima and weights of the parts
+    int32_t slots;           // workgroups of a K/V head
+    float share;             // of the device's places, where the keys are shared out: a K/V head's; else 0
+    f4 *part_data;           // keys shared out: [slots][kv_heads] parts: sums, maxima and weights
     int32_t o_pieces;        // whether rows of O lie at 16-byte multiples
 };
 
@@ -71,6 +73,101 @@ __device__ __forceinline__ int chunk_place(const ChunkArgs &a, int b, int head, 
     return there && id >= 0 && id < a.cache.num_pages ? (id * a.cache.kv_heads + head) * a.cache.page_blocks + (index - page * a.cache.page_blocks) : -1;
 }
 
+// A tile of a sequence's rows (new tokens times the heads that share a K/V head, heads fastest) and a workgroup's share of its keys.  FEW: the sequences of
+// up to few_rows rows, a tile each; else the others, in tiles of BM.
+template <bool FEW, int BM>
+struct ChunkUnit {
+    int b, first_row, queries, rows, row0, group;                // first_row: of the packed rows of tokens
+    int64_t start;
+    int part, parts, part0;                                      // `parts` workgroups share out the keys; of them this one, and the first one's number
+    bool there;
+
+    __device__ __forceinline__ void take(const ChunkArgs &a, int begin, int end, int at)
+    {
+        const ChunkSequence seq(a, begin, end, at);
+        first_row = seq.first, queries = seq.queries, start = seq.start, rows = queries * group;
+    }
+    __device__ __forceinline__ ChunkRow row(const ChunkArgs &a, int r) const
+    {
+        return ChunkRow(a, (int)min(max(start + min(r, rows - 1) / group, (int64_t)-1), (int64_t)0x7ffffffe));
+    }
+    __device__ __forceinline__ ChunkTiles keys(const ChunkArgs &a) const { return ChunkTiles(a, row(a, row0), row(a, row0 + BM - 1)); }
+    __device__ __forceinline__ bool mine(const ChunkArgs &a) const { return FEW ? rows > 0 && rows <= min(a.few_rows, BM) : rows > a.few_rows; }
+
+    // Workgroup `number` of a head (JOIN: tile `number`).
+    template <int JOIN>
+    __device__ __forceinline__ ChunkUnit(const ChunkArgs &a, int number, Index<JOIN>) : row0(0), group(a.q_heads / a.cache.kv_heads), part(0), parts(1), part0(0)
+    {
+        if (a.share == 0.0f) {                                   // a workgroup takes all keys of its tile
+            int of[3];
+            if constexpr (FEW) {
+                b = number;
+                of[0] = a.offsets[b], of[1] = a.offsets[b + 1], of[2] = a.starts ? a.starts[b] : 0;
+            } else {                                             // sequence b has the slots floor(rows before it / BM) + b .. : as many as its rows need or one more
+                const int group = this->group;
+                b = find_sequence(a.batch, number, {a.offsets, a.offsets + 1, a.starts}, of, [group](int offset, int x) { return offset * group / BM + x; });
+                row0 = (number - (of[0] * group / BM + b)) * BM;
+            }
+            take(a, of[0], of[1], of[2]);
+            there = mine(a) && row0 >= 0 && row0 < rows;
+            return;
+        }
+        // Up to kMostShared sequences, a lane each.  If each tile took what its sequence's last one does, all places of the device would have the same; tiles that see less
+        // are cut into as many parts.
+        constexpr int TURNS = kMostShared / 64;
+        const int lane = threadIdx.x & 63;
+        int of[TURNS][3] = {}, tiles[TURNS] = {}, most[TURNS] = {};
+        float work = 0.0f;
+#pragma unroll
+        for (int i = 0; i < TURNS; ++i) {
+            if (64 * i >= a.batch) break;
+            const int at = min(64 * i + lane, a.batch - 1);
+            of[i][0] = a.offsets[at], of[i][1] = a.offsets[at + 1], of[i][2] = a.starts ? a.starts[at] : 0;
+            take(a, of[i][0], of[i][1], of[i][2]);
+            tiles[i] = 64 * i + lane < a.batch && mine(a) ? (rows + BM - 1) / BM : 0;
+            row0 = max(tiles[i] - 1, 0) * BM;
+            most[i] = tiles[i] > 0 ? keys(a).count : 0;
+            work += (float)tiles[i] * (float)most[i];
+        }
+        work = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sums_up_to(work)), 63));
+        const float share = a.share / fmaxf(work, 1.0f);
+        int tile = 0, each = 1, tiles_before = 0, parts_before = 0;
+        there = false;
+        b = 0;
+#pragma unroll
+        for (int i = 0; i < TURNS; ++i) {
+            if (64 * i >= a.batch) break;
+            // (a whole number of parts may come out as a little less)
+            const int cut = max(1, min((int)((float)most[i] * share + 0x1p-8f), most[i] / kLeastTiles)), all = tiles[i] * cut;
+            const int tiles_to = tiles_before + sums_up_to(tiles[i]), parts_to = parts_before + sums_up_to(all);
+            const int begin = JOIN ? tiles_to - tiles[i] : parts_to - all, end = JOIN ? tiles_to : parts_to;
+            const uint64_t here = __ballot(begin <= number && number < end);
+            if (here) {
+                const int l = __builtin_ctzll(here);
+                take(a, __builtin_amdgcn_readlane(of[i][0], l), __builtin_amdgcn_readlane(of[i][1], l), __builtin_amdgcn_readlane(of[i][2], l));
+                b = 64 * i + l;
+                each = __builtin_amdgcn_readlane(cut, l);
+                const int at = number - __builtin_amdgcn_readlane(begin, l);
+                tile = JOIN ? at : at / each;
+                part = JOIN ? 0 : at % each;
+                part0 = __builtin_amdgcn_readlane(parts_to - all, l) + tile * each;
+                tile = __builtin_amdgcn_readlane(tiles[i], l) - 1 - tile;          // the longest first
+                there = true;
+            }
+            tiles_before = __builtin_amdgcn_readlane(tiles_to, 63);
+            parts_before = __builtin_amdgcn_readlane(parts_to, 63);
+        }
+        if (!there) return;
+        row0 = tile * BM;
+        parts = max(1, min(each, keys(a).count / kLeastTiles));
+        there = part < parts && part0 >= 0 && part0 + parts <= a.slots;          // (places past the end: offsets that fall)
+        // (the same in all lanes, which the compiler does not see)
+        for (int *const x : {&b, &first_row, &queries, &rows, &row0, &part, &parts, &part0}) *x = __builtin_amdgcn_readfirstlane(*x);
+        start = (int64_t)__builtin_amdgcn_readfirstlane((int)start);
+        there = __builtin_amdgcn_readfirstlane(there);
+    }
+};
+
 // Four codes as 16-bit floats, in order.
 __device__ __forceinline__ u2 codes4_to(F16, uint32_t x)
 {
@@ -124,34 +221,28 @@ __device__ __forceinline__ void put_chunk_row(const ChunkArgs &a, int token, int
 }
 
 constexpr int kFewWaves = 4;
+constexpr int few_waves_per_simd(int D, int R) { return D * R <= 128 ? 2 : 1; }
 
 // Sequences of few rows: those of up to R tiles of 16 (new tokens times the heads that share a K/V head, heads fastest).  A wavefront takes
 // tiles of 64 keys = 4 blocks: S^T = K Q^T and O^T = V^T P^T on 16 x 16 x 32 matrix instructions.  Row r of the first product's tile t is
 // token 4 t + r % 4 of block r / 4, so that lane 16 g + h holds row h's scores of block g's tokens, which is what the second product wants of it.
 // The weights times V's scales enter the second product as two bf16 numbers each.
 template <class E, int D, int R>
-__global__ __launch_bounds__(kFewWaves * 64) void attention_chunk_few_kernel(const ChunkArgs a)
+__global__ __launch_bounds__(kFewWaves * 64, few_waves_per_simd(D, R)) void attention_chunk_few_kernel(const ChunkArgs a)
 {
     extern __shared__ __align__(16) float shared[];
     constexpr int NW = kFewWaves, NJ = (D + 63) / 64, DT = D / 16, ROWS = 16 * R;
     typedef typename E::T T;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = lane & 15, g = lane >> 4;
-    const int kv_heads = a.cache.kv_heads, group = a.q_heads / kv_heads;
-    int id = blockIdx.x;
-    const int head = id % kv_heads;
-    id /= kv_heads;
-    const int b = id % a.batch, part = id / a.batch;
-
-    const ChunkSequence seq(a, a.offsets[b], a.offsets[b + 1], a.starts ? a.starts[b] : 0);
-    const int rows = seq.queries * group;
-    if (rows == 0 || rows > min(a.few_rows, ROWS)) return;
-    const ChunkTiles list(a, ChunkRow(a, seq.position(0)), ChunkRow(a, seq.position(seq.queries - 1)));
-    // parts of whole turns of the wavefronts; an empty list's first workgroup writes its zeros
-    const int parts = max(1, min(a.parts, (list.count + a.run - 1) / a.run));
+    const int kv_heads = a.cache.kv_heads, head = blockIdx.x % kv_heads;
+    const ChunkUnit<true, ROWS> unit(a, blockIdx.x / kv_heads, Index<0>{});
+    if (!unit.there) return;
+    const int group = unit.group, rows = unit.rows, parts = unit.parts, b = unit.b;
+    const ChunkTiles list = unit.keys(a);
+    // parts of whole turns of the wavefronts (the last of them may be empty)
     const int each = ((list.count + parts - 1) / parts + NW - 1) / NW * NW;
-    const int first = part * each, end = min(list.count, first + each);
-    if (part > 0 && first >= end) return;
+    const int first = min(list.count, unit.part * each), end = min(list.count, first + each);
 
     // the wavefront's blocks, 16 tiles ahead: lane l looks up block l % 4 of its tile l / 4
     constexpr int block_bytes = 32 * D + 128;
@@ -165,13 +256,14 @@ __global__ __launch_bounds__(kFewWaves * 64) void attention_chunk_few_kernel(con
 #pragma unroll
     for (int r = 0; r < R; ++r) {                        // (rows past the last repeat it and are not written)
         const int row = min(16 * r + h, rows - 1), query = row / group;
-        range[r] = ChunkRow(a, seq.position(query));
-        const T *from = (const T *)a.q.data + (seq.first + query) * a.q.token_stride + (head * group + row % group) * a.q.head_stride;
+        range[r] = unit.row(a, row);
+        const T *from = (const T *)a.q.data + (unit.first_row + query) * a.q.token_stride + (head * group + row % group) * a.q.head_stride;
 #pragma unroll
         for (int s = 0; s < 2 * NJ; ++s) {
             const int d = 64 * (s / 2) + 16 * g + 8 * (s % 2);
             __builtin_memcpy(&q[r][s], from + (d < D ? d : 0), 16);
             if (d >= D) q[r][s] = (u4)(0u);
+            if constexpr (few_waves_per_simd(D, R) == 1) asm volatile("" : "+a"(q[r][s]));       // (out of the vector unit's registers, which are short)
         }
     }
 
@@ -217,12 +309,14 @@ __global__ __launch_bounds__(kFewWaves * 64) void attention_chunk_few_kernel(con
 #pragma unroll
             for (int j = 0; j < NJ; ++j) {
                 u4 x[2];
+                asm volatile("" : "+v"(k[t][j]));        // (converted here and not before, and 16 codes at a time: all floats at once would be too many registers)
                 codes_to(E{}, k[t][j], x);
 #pragma unroll
                 for (int r = 0; r < R; ++r) {
                     s[r][t] = mfma16(E{}, x[0], q[r][2 * j], s[r][t]);
                     s[r][t] = mfma16(E{}, x[1], q[r][2 * j + 1], s[r][t]);
                 }
+                __builtin_amdgcn_sched_barrier(0);
             }
         }
         if (i + NW < end) {
@@ -255,7 +349,11 @@ __global__ __launch_bounds__(kFewWaves * 64) void attention_chunk_few_kernel(con
                 l[r] *= fall;
                 m[r] = next;
 #pragma unroll
-                for (int t = 0; t < DT; ++t) o[r][t] *= fall;
+                for (int t = 0; t < DT; ++t) {
+                    if constexpr (few_waves_per_simd(D, R) == 1) asm volatile("" : "+a"(o[r][t]));
+                    o[r][t] *= fall;
+                    if constexpr (few_waves_per_simd(D, R) == 1) asm volatile("" : "+a"(o[r][t]));
+                }
             }
             unrolled<16>([&](auto at) {
                 constexpr int I = decltype(at)::value;
@@ -276,6 +374,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void attention_chunk_few_kernel(con
 #pragma unroll
         for (int t = 0; t < DT; ++t) {
             u4 x[2];
+            asm volatile("" : "+v"(v[t]));
             codes_to(BF16{}, v[t], x);
 #pragma unroll
             for (int r = 0; r < R; ++r) {
@@ -284,6 +383,7 @@ __global__ __launch_bounds__(kFewWaves * 64) void attention_chunk_few_kernel(con
                 o[r][t] = mfma16(BF16{}, x[0], p[r][0], o[r][t]);
                 o[r][t] = mfma16(BF16{}, x[1], p[r][1], o[r][t]);
             }
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
 
@@ -322,60 +422,65 @@ __global__ __launch_bounds__(kFewWaves * 64) void attention_chunk_few_kernel(con
             ref = fmaxf(ref, ms[ROWS * w + row]);
         }
         if (parts > 1) {
-            f4 *to = a.part_data + ((((int64_t)b * kv_heads + head) * a.parts + part) * ROWS + row) * (PIECES + 1);
+            f4 *to = a.part_data + ((int64_t)blockIdx.x * ROWS + row) * (PIECES + 1);
             to[1 + piece] = sum;
             if (piece == 0) to[0] = (f4){ref, weight, 0.0f, 0.0f};
         } else {
-            put_chunk_row<E>(a, seq.first + row / group, head * group + row % group, 4 * piece, sum, weight);
+            put_chunk_row<E>(a, unit.first_row + row / group, head * group + row % group, 4 * piece, sum, weight);
         }
     }
 }
 
-// The parts of a row, joined in an order that depends on nothing but their number.  A workgroup per row; groups of D / 4 lanes take the parts
-// in turn, and the groups' sums are added in their order.
+// The parts of a sequence's rows, joined in an order that depends on nothing but their number.  Lanes take D / 4 pieces of a row; with few parts a workgroup has as
+// many rows as lanes allow, with many (rows_each 1) groups of lanes take the parts in turn, and the groups' sums are added in their order.
 constexpr int kFewJoinThreads = 256;
 
 template <class E, int D, int R>
-__global__ __launch_bounds__(kFewJoinThreads) void attention_chunk_few_join_kernel(const ChunkArgs a)
+__global__ __launch_bounds__(kFewJoinThreads) void attention_chunk_few_join_kernel(const ChunkArgs a, int rows_each, int blocks)
 {
-    constexpr int PIECES = D / 4, ROWS = 16 * R, GROUPS = kFewJoinThreads / PIECES;
-    __shared__ f4 sums[GROUPS * PIECES];
-    __shared__ float weights[GROUPS];
-    const int kv_heads = a.cache.kv_heads, group = a.q_heads / kv_heads, tid = threadIdx.x;
-    const int row = blockIdx.x % ROWS, unit = blockIdx.x / ROWS, head = unit % kv_heads, b = unit / kv_heads;
-    const ChunkSequence seq(a, a.offsets[b], a.offsets[b + 1], a.starts ? a.starts[b] : 0);
-    const int rows = seq.queries * group;
-    if (row >= rows || rows > min(a.few_rows, ROWS)) return;
-    const ChunkTiles list(a, ChunkRow(a, seq.position(0)), ChunkRow(a, seq.position(seq.queries - 1)));
-    const int parts = max(1, min(a.parts, (list.count + a.run - 1) / a.run));
-    if (parts == 1) return;
-    const int each = ((list.count + parts - 1) / parts + kFewWaves - 1) / kFewWaves * kFewWaves, full = (list.count + each - 1) / each;
-    const f4 *from = a.part_data + ((int64_t)unit * a.parts * ROWS + row) * (PIECES + 1);
-    constexpr int STEP = ROWS * (PIECES + 1);
-    float top = -3.0e38f;
-    for (int c = tid & 63; c < full; c += 64) top = fmaxf(top, from[(int64_t)c * STEP][0]);
-    top = max_of_rows(max_of_lanes<16>(top));
-    const int g = tid / PIECES, piece = tid % PIECES;
+    constexpr int PIECES = D / 4, ROWS = 16 * R, SLOTS = kFewJoinThreads / PIECES;
+    __shared__ f4 sums[SLOTS * PIECES];
+    __shared__ float weights[SLOTS], refs[SLOTS];
+    const int kv_heads = a.cache.kv_heads, tid = threadIdx.x, id = blockIdx.x / blocks, row0 = (int)blockIdx.x % blocks * rows_each;
+    const int head = id % kv_heads, number = id / kv_heads;
+    const ChunkUnit<true, ROWS> unit(a, number, Index<1>{});
+    const int groups = SLOTS / rows_each, slot = tid / PIECES, piece = tid % PIECES;
+    const int row = row0 + slot / groups, g = slot % groups;
+    if (!unit.there || unit.parts == 1 || row0 >= unit.rows) return;
+    const f4 *from = a.part_data + (((int64_t)unit.part0 * kv_heads + head) * ROWS + min(row, unit.rows - 1)) * (PIECES + 1);
+    const int64_t step = (int64_t)kv_heads * ROWS * (PIECES + 1);
+    float top = -3.0e38f, weight = 0.0f;
     f4 sum = (f4)(0.0f);
-    float weight = 0.0f;
-    if (g < GROUPS) {
-        for (int c = g; c < full; c += GROUPS) {
-            const f4 *part = from + (int64_t)c * STEP;
-            const f4 stats = part[0], x = part[1 + piece];
-            const float fall = __builtin_amdgcn_exp2f(stats[0] - top);
-            weight += stats[1] * fall;
-            sum += x * fall;
+    if (slot < groups * rows_each) {
+        for (int c = g; c < unit.parts; c += 4 * groups) {       // four on their way together
+            f4 stats[4], x[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const f4 *part = from + min(c + i * groups, unit.parts - 1) * step;
+                stats[i] = part[0];
+                x[i] = part[1 + piece];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                if (c + i * groups >= unit.parts) break;
+                const float now = fmaxf(top, stats[i][0]), fall = __builtin_amdgcn_exp2f(top - now), by = __builtin_amdgcn_exp2f(stats[i][0] - now);
+                weight = weight * fall + stats[i][1] * by;
+                sum = sum * fall + x[i] * by;
+                top = now;
+            }
         }
         sums[tid] = sum;
-        if (piece == 0) weights[g] = weight;
+        if (piece == 0) weights[slot] = weight, refs[slot] = top;
     }
     __syncthreads();
-    if (g > 0) return;
-    for (int x = 1; x < min(GROUPS, full); ++x) {
-        sum += sums[x * PIECES + piece];
-        weight += weights[x];
+    if (g > 0 || slot >= groups * rows_each || row >= unit.rows) return;
+    for (int x = 1; x < min(groups, unit.parts); ++x) {
+        const float now = fmaxf(top, refs[slot + x]), fall = __builtin_amdgcn_exp2f(top - now), by = __builtin_amdgcn_exp2f(refs[slot + x] - now);
+        weight = weight * fall + weights[slot + x] * by;
+        sum = sum * fall + sums[tid + x * PIECES] * by;
+        top = now;
     }
-    put_chunk_row<E>(a, seq.first + row / group, head * group + row % group, 4 * piece, sum, weight);
+    put_chunk_row<E>(a, unit.first_row + row / unit.group, head * unit.group + row % unit.group, 4 * piece, sum, weight);
 }
 
 // ---- many rows ----
@@ -393,28 +498,6 @@ struct ChunkCfg {
     static constexpr int kPart = BM * 2 * (DP / 8 + 1);          // 16-byte pieces of a part: sums, maximum and weight
 };
 
-// A tile of a sequence's rows, heads fastest, and its share of the keys.
-template <class C>
-struct ChunkTile {
-    ChunkSequence seq;
-    int group, row0, rows;
-    bool there;
-    // Sequence b has the slots floor(rows before it / BM) + b .. : as many as its rows need or one more.
-    __device__ __forceinline__ static ChunkTile find(const ChunkArgs &a, int slot)
-    {
-        const int group = a.q_heads / a.cache.kv_heads;
-        int of[3];
-        const int b = find_sequence(a.batch, slot, {a.offsets, a.offsets + 1, a.starts}, of, [&](int offset, int x) { return offset * group / C::BM + x; });
-        ChunkTile t{ChunkSequence(a, of[0], of[1], of[2]), group, (slot - (of[0] * group / C::BM + b)) * C::BM, 0, false, b};
-        t.rows = t.seq.queries * group;
-        t.there = t.row0 >= 0 && t.row0 < t.rows && t.rows > a.few_rows;
-        return t;
-    }
-    int b;
-    __device__ __forceinline__ ChunkRow row(const ChunkArgs &a, int r) const { return ChunkRow(a, seq.position(min(r, rows - 1) / group)); }
-    __device__ __forceinline__ ChunkTiles keys(const ChunkArgs &a) const { return ChunkTiles(a, row(a, row0), row(a, row0 + C::BM - 1)); }
-};
-
 template <class E, class C, bool VEC>
 __global__ __launch_bounds__(C::NW * 64, C::PER_SIMD) void attention_chunk_kernel(const ChunkArgs a)
 {
@@ -424,14 +507,12 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_SIMD) void attention_chunk_kerne
     typedef typename E::T T;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, col = lane & 31;
     const int kv_heads = a.cache.kv_heads, D = a.cache.head_dim;
-    const int head = blockIdx.x % kv_heads, part = blockIdx.x / kv_heads % a.parts;
-    const ChunkTile<C> tile = ChunkTile<C>::find(a, a.slots - 1 - blockIdx.x / kv_heads / a.parts);
+    const int head = blockIdx.x % kv_heads, number = blockIdx.x / kv_heads;
+    const ChunkUnit<false, C::BM> tile(a, a.share > 0.0f ? number : a.slots - 1 - number, Index<0>{});
     if (!tile.there) return;
-    const int group = tile.group, rows = tile.rows;
+    const int group = tile.group, rows = tile.rows, parts = tile.parts;
     const ChunkTiles list = tile.keys(a);
-    const int parts = max(1, min(a.parts, (list.count + a.run - 1) / a.run));
-    if (part >= parts) return;
-    const int first = (int)((int64_t)list.count * part / parts), count = (int)((int64_t)list.count * (part + 1) / parts) - first;
+    const int first = (int)((int64_t)list.count * tile.part / parts), count = (int)((int64_t)list.count * (tile.part + 1) / parts) - first;
 
     const int row0 = tile.row0 + 32 * wave, row = min(row0 + col, rows - 1);             // the wavefront's first, the lane's
     const ChunkRow range = tile.row(a, row), row_first = tile.row(a, row0), row_last = tile.row(a, row0 + 31);
@@ -491,7 +572,7 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_SIMD) void attention_chunk_kerne
 
     // ---- Q^T's operand: 8 elements of the lane's row per step ----
     u4 q[STEPS];
-    const int qhead = head * group + row % group, token = tile.seq.first + row / group;
+    const int qhead = head * group + row % group, token = tile.first_row + row / group;
     {
         const T *from = (const T *)a.q.data + token * a.q.token_stride + qhead * a.q.head_stride;
 #pragma unroll
@@ -598,7 +679,7 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_SIMD) void attention_chunk_kerne
             unrolled<(N + 1) * 4 * PIECES / 16 - N * 4 * PIECES / 16>([&](auto x) {
                 store_step(Index<B>{}, Index<N * 4 * PIECES / 16 + decltype(x)::value>{}, 1 - odd);
             });
-            __builtin_amdgcn_sched_barrier(0);
+            if constexpr (N % 2 == 1) __builtin_amdgcn_sched_barrier(0);
         });
         // Weights stay relative to what was the largest score once, as long as their sums are moderate (bf16 and float lose nothing by that).
         if (__any(sum > kMostSum)) {
@@ -737,13 +818,11 @@ __global__ __launch_bounds__(C::NW * 64) void attention_chunk_join_kernel(const 
 {
     constexpr int THREADS = C::NW * 64, PIECES = C::DP / 8;
     const int piece = blockIdx.x % PIECES, kv_heads = a.cache.kv_heads, head = blockIdx.x / PIECES % kv_heads, number = blockIdx.x / PIECES / kv_heads;
-    const ChunkTile<C> tile = ChunkTile<C>::find(a, a.slots - 1 - number);
-    const int tid = threadIdx.x, lane = tid & 63, row = tile.row0 + 32 * (tid >> 6) + (lane & 31);
+    const ChunkUnit<false, C::BM> tile(a, number, Index<1>{});
+    const int tid = threadIdx.x, lane = tid & 63, row = tile.row0 + 32 * (tid >> 6) + (lane & 31), parts = tile.parts;
     const int d = 8 * piece + 4 * (lane >> 5);                   // 32 (piece / 4) + 8 (piece % 4) + ..
-    if (!tile.there || row >= tile.rows || d >= a.cache.head_dim) return;
-    const int parts = max(1, min(a.parts, (tile.keys(a).count + a.run - 1) / a.run));
-    if (parts == 1) return;
-    const f4 *from = a.part_data + ((int64_t)number * a.parts * kv_heads + head) * C::kPart + tid;
+    if (!tile.there || parts == 1 || row >= tile.rows || d >= a.cache.head_dim) return;
+    const f4 *from = a.part_data + ((int64_t)tile.part0 * kv_heads + head) * C::kPart + tid;
     float top = -3.0e38f, l = 0.0f;
     f4 o = (f4)(0.0f);
     for (int p0 = 0; p0 < parts; p0 += 4) {                      // four on their way together
@@ -769,7 +848,7 @@ __global__ __launch_bounds__(C::NW * 64) void attention_chunk_join_kernel(const 
             o += x[i] * by;
         }
     }
-    put_chunk_row<E>(a, tile.seq.first + row / tile.group, head * tile.group + row % tile.group, d, o, l);
+    put_chunk_row<E>(a, tile.first_row + row / tile.group, head * tile.group + row % tile.group, d, o, l);
 }
 
 }  // namespace ngemm

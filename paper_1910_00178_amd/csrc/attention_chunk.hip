@@ -10,8 +10,7 @@ using namespace ngemm;
 namespace {
 
 constexpr int64_t kUnits = 256;
-// Rows of a sequence that attention_chunk_few_kernel takes at most: heads of more than 128 leave no registers for two tiles of 16.
-constexpr int64_t few_rows_of(int64_t head_dim) { return head_dim <= 128 ? 32 : 16; }
+constexpr int64_t kFewRows = 32;                                 // of a sequence, that attention_chunk_few_kernel takes at most
 
 // f(ChunkCfg<...>{}) for the smallest DP that holds head_dim.  `wide`: 256 rows a workgroup where there are registers for it.
 template <class F>
@@ -34,8 +33,8 @@ int64_t most_tiles(int64_t queries, int64_t max_length, int64_t window, int64_t 
 }
 
 struct ChunkCut {
-    int64_t few_rows = 0;                                        // 0: no sequence can have so few
-    int64_t few_run = 1, few_parts = 1, slots = 0, run = 1, parts = 1;           // slots 0: no sequence can have more
+    int64_t few_rows = 0, few_slots = 0, slots = 0;              // 0: no sequence can have so few, or more
+    int64_t few_places = 0, places = 0;                          // 0: keys are not shared out
     bool wide = false;
     size_t few_bytes = 0, bytes = 0;
 };
@@ -44,25 +43,25 @@ ChunkCut chunk_cut(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t hea
 {
     ChunkCut cut;
     const int64_t group = q_heads / kv_heads, most_new = std::min(max_new, tokens);
-    const int64_t few = few_rows_of(head_dim);
-    if (group <= few && (batch > 1 || most_new * group <= few)) {
-        cut.few_rows = most_new * group <= 16 ? 16 : few;
-        const int64_t tiles = std::max<int64_t>(1, most_tiles(std::min(most_new, cut.few_rows / group), max_length, window, sinks)), grid = batch * kv_heads;
-        cut.few_run = std::max<int64_t>(std::min<int64_t>((tiles * grid / (2 * kUnits) + 3) / 4 * 4, 64), (tiles * grid / (32 * kUnits) + 4) / 4 * 4);
-        cut.few_parts = (tiles + cut.few_run - 1) / cut.few_run;
-        if (cut.few_parts > 1) cut.few_bytes = (size_t)(grid * cut.few_parts * cut.few_rows * (head_dim / 4 + 1) * 16);
+    if (group <= kFewRows && (batch > 1 || most_new * group <= kFewRows)) {
+        cut.few_rows = most_new * group <= 16 ? 16 : kFewRows;
+        cut.few_slots = batch;
+        if (batch <= kMostShared && most_tiles(std::min(most_new, cut.few_rows / group), max_length, window, sinks) >= 2 * kLeastTiles) {
+            cut.few_places = std::max(4 * kUnits, kv_heads);
+            cut.few_slots += cut.few_places / kv_heads + 1;
+            cut.few_bytes = (size_t)(cut.few_slots * kv_heads * cut.few_rows * (head_dim / 4 + 1) * 16);
+        }
     }
     if (most_new * group > cut.few_rows) {
         cut.wide = tokens * group / batch >= 256;
         const int64_t height = tile_rows(head_dim, cut.wide), places = cut.wide || head_dim > 128 ? kUnits : 2 * kUnits;
         cut.slots = tokens * group / height + batch;
-        const int64_t tiles = std::max<int64_t>(1, most_tiles(std::min(most_new, height / group + 2), max_length, window, sinks));
         const int64_t grid = std::max(batch, (tokens * group + height - 1) / height) * kv_heads;
-        cut.run = std::max<int64_t>((tiles * grid + places - 1) / places, 4);
-        cut.parts = grid >= places ? 1 : (tiles + cut.run - 1) / cut.run;
-        if (cut.parts == 1) cut.run = tiles;
-        else
-            with_chunk_form(head_dim, cut.wide, [&](auto form) { cut.bytes = (size_t)(cut.slots * kv_heads * cut.parts) * decltype(form)::kPart * 16; });
+        if (batch <= kMostShared && grid < places && most_tiles(std::min(most_new, height / group + 2), max_length, window, sinks) >= 2 * kLeastTiles) {
+            cut.places = places;
+            cut.slots += cut.places / kv_heads + 1;
+            with_chunk_form(head_dim, cut.wide, [&](auto form) { cut.bytes = (size_t)(cut.slots * kv_heads) * decltype(form)::kPart * 16; });
+        }
     }
     return cut;
 }
@@ -82,9 +81,16 @@ bool launch_few(const ChunkArgs &a, int device, hipStream_t st)
     const auto lds = [](int rows) constexpr { return kFewWaves * (2 * 16 * R + rows * D) * 4; };
     if (!allow_lds<FewForm<E, D, R>, lds(16 * R)>(device, attention_chunk_few_kernel<E, D, R>)) return false;
     const int most = (int)std::min<int64_t>(16 * R, (int64_t)std::min(a.max_new, a.tokens) * (a.q_heads / a.cache.kv_heads));
-    const unsigned units = (unsigned)(a.batch * a.cache.kv_heads);
-    hipLaunchKernelGGL((attention_chunk_few_kernel<E, D, R>), dim3(units * a.parts), dim3(kFewWaves * 64), (size_t)lds(most), st, a);
-    if (a.parts > 1) hipLaunchKernelGGL((attention_chunk_few_join_kernel<E, D, R>), dim3(units * 16 * R), dim3(kFewJoinThreads), 0, st, a);
+    hipLaunchKernelGGL((attention_chunk_few_kernel<E, D, R>), dim3((unsigned)(a.slots * a.cache.kv_heads)), dim3(kFewWaves * 64), (size_t)lds(most), st, a);
+    if (a.share > 0.0f) {
+        // as many rows a workgroup as leave a group of lanes no more than some 8 parts in turn, by the places that a sequence has on average
+        const int lanes = kFewJoinThreads / (D / 4);
+        int rows_each = 1;
+        while (rows_each * 2 <= std::min(lanes, 16 * R) && 4 * a.slots * rows_each <= a.batch * lanes * 8) rows_each *= 2;
+        const int blocks = (most + rows_each - 1) / rows_each;
+        hipLaunchKernelGGL((attention_chunk_few_join_kernel<E, D, R>), dim3((unsigned)(a.batch * a.cache.kv_heads * blocks)), dim3(kFewJoinThreads), 0, st, a,
+                           rows_each, blocks);
+    }
     return true;
 }
 
@@ -93,9 +99,11 @@ template <class E, class C, bool VEC>
 bool launch_many(const ChunkArgs &a, int device, hipStream_t st)
 {
     if (!allow_lds<ManyForm<E, C, VEC>, C::kLds>(device, attention_chunk_kernel<E, C, VEC>)) return false;
-    const unsigned units = (unsigned)(a.slots * a.cache.kv_heads);
-    hipLaunchKernelGGL((attention_chunk_kernel<E, C, VEC>), dim3(units * a.parts), dim3(C::NW * 64), C::kLds, st, a);
-    if (a.parts > 1) hipLaunchKernelGGL((attention_chunk_join_kernel<E, C>), dim3(units * (C::DP / 8)), dim3(C::NW * 64), 0, st, a);
+    hipLaunchKernelGGL((attention_chunk_kernel<E, C, VEC>), dim3((unsigned)(a.slots * a.cache.kv_heads)), dim3(C::NW * 64), C::kLds, st, a);
+    if (a.share > 0.0f) {
+        const int64_t tiles = (int64_t)a.tokens * (a.q_heads / a.cache.kv_heads) / C::BM + a.batch;
+        hipLaunchKernelGGL((attention_chunk_join_kernel<E, C>), dim3((unsigned)(tiles * a.cache.kv_heads * (C::DP / 8))), dim3(C::NW * 64), 0, st, a);
+    }
     return true;
 }
 
@@ -105,23 +113,17 @@ bool launch_chunk(ChunkArgs a, const ChunkCut &cut, bool vec, uint8_t *workspace
     bool ok = true;
     a.few_rows = (int32_t)cut.few_rows;
     if (cut.slots > 0) {
-        a.run = (int32_t)cut.run, a.parts = (int32_t)cut.parts, a.slots = (int32_t)cut.slots, a.part_data = (f4 *)workspace;
+        a.slots = (int32_t)cut.slots, a.share = (float)cut.places / (float)a.cache.kv_heads, a.part_data = (f4 *)workspace;
         with_chunk_form(a.cache.head_dim, cut.wide, [&](auto form) {
             typedef decltype(form) C;
             ok = vec ? launch_many<E, C, true>(a, device, st) : launch_many<E, C, false>(a, device, st);
         });
     }
     if (cut.few_rows > 0 && ok) {
-        a.run = (int32_t)cut.few_run, a.parts = (int32_t)cut.few_parts, a.part_data = (f4 *)(workspace + cut.bytes);
+        a.slots = (int32_t)cut.few_slots, a.share = (float)cut.few_places / (float)a.cache.kv_heads, a.part_data = (f4 *)(workspace + cut.bytes);
         with_head_dim(a.cache.head_dim, [&](auto dim) {
             constexpr int D = decltype(dim)::value;
-            if constexpr (few_rows_of(D) > 16) {
-                if (cut.few_rows > 16) {
-                    ok = launch_few<E, D, 2>(a, device, st);
-                    return;
-                }
-            }
-            ok = launch_few<E, D, 1>(a, device, st);
+            ok = cut.few_rows <= 16 ? launch_few<E, D, 1>(a, device, st) : launch_few<E, D, 2>(a, device, st);
         });
     }
     return ok;
@@ -158,7 +160,7 @@ ngemm_status ngemm_attention_chunk(ngemm_ctx *ctx, const ngemm_kv_cache *cache, 
     if (const ngemm_status s = check_rows(q, type, tokens, q_heads, head_dim, false); s != NGEMM_OK) return s;
     if (const ngemm_status s = check_rows(o, type, tokens, q_heads, head_dim, true); s != NGEMM_OK) return s;
     const ChunkCut cut = chunk_cut(batch, q_heads, kv_heads, head_dim, tokens, max_new, max_length, window, sinks);
-    if (std::max(cut.slots * kv_heads * std::max(cut.parts, head_dim / 8 + 4), batch * kv_heads * std::max(cut.few_parts, cut.few_rows)) > kMaxGroups)
+    if (std::max(cut.slots * kv_heads * (cut.places > 0 ? head_dim / 8 + 4 : 1), cut.few_slots * kv_heads * (cut.few_places > 0 ? cut.few_rows : 1)) > kMaxGroups)
         return NGEMM_ERR_BAD_SHAPE;
     const size_t need = cut.few_bytes + cut.bytes;
     if (need > 0 && !workspace_dev) return NGEMM_ERR_INVALID_ARG;
@@ -167,7 +169,7 @@ ngemm_status ngemm_attention_chunk(ngemm_ctx *ctx, const ngemm_kv_cache *cache, 
     DeviceGuard g(ctx->device);
     if (!g.ok) return NGEMM_ERR_DEVICE;
     const ChunkArgs a{view_of(cache, pages_dev, pages_stride), q, o, offsets_dev, starts_dev, (int32_t)batch, (int32_t)q_heads, (int32_t)tokens, (int32_t)max_new,
-                      pages_stride > 0 ? (int32_t)max_length : 0, (int32_t)window, (int32_t)sinks, scale * 1.44269504f, 0, 1, 1, 0, nullptr, in_pieces(o, type)};
+                      pages_stride > 0 ? (int32_t)max_length : 0, (int32_t)window, (int32_t)sinks, scale * 1.44269504f, 0, 0, 0.0f, nullptr, in_pieces(o, type)};
     const bool vec = in_pieces(q, type) && in_pieces(o, type);
     hipStream_t st = (hipStream_t)hip_stream;
     const bool ok = type == NGEMM_F16 ? launch_chunk<F16>(a, cut, vec, (uint8_t *)workspace_dev, ctx->device, st)

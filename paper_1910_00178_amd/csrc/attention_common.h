@@ -80,6 +80,21 @@ __device__ __forceinline__ float of_row(float x)
     return __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(x), 0x150 + K, 0xf, 0xf, true));
 }
 
+// Sums over a wavefront's lanes up to and with each.
+template <class T>
+__device__ __forceinline__ T sums_up_to(T x)
+{
+#define NGEMM_WITH(dpp, rows) x += __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), dpp, rows, 0xf, true))
+    NGEMM_WITH(0x111, 0xf);                              // in rows of 16 lanes: the lane's 1, 2, 4, 8 before
+    NGEMM_WITH(0x112, 0xf);
+    NGEMM_WITH(0x114, 0xf);
+    NGEMM_WITH(0x118, 0xf);
+    NGEMM_WITH(0x142, 0xa);                              // rows 0 and 2 to the next
+    NGEMM_WITH(0x143, 0xc);                              // row 1 to rows 2 and 3
+#undef NGEMM_WITH
+    return x;
+}
+
 // f(Index<0>) .. f(Index<N - 1>)
 template <int I> struct Index { static constexpr int value = I; };
 template <int N, int I = 0, class F>

@@ -82,21 +82,6 @@ __device__ __forceinline__ void copy_to_lds(Buffer from, uint32_t lds_at, uint32
 #pragma clang diagnostic pop
 __device__ __forceinline__ void copies_landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
 
-// Sums over a wavefront's lanes up to and with each.
-template <class T>
-__device__ __forceinline__ T sums_up_to(T x)
-{
-#define NGEMM_WITH(dpp, rows) x += __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), dpp, rows, 0xf, true))
-    NGEMM_WITH(0x111, 0xf);                              // in rows of 16 lanes: the lane's 1, 2, 4, 8 before
-    NGEMM_WITH(0x112, 0xf);
-    NGEMM_WITH(0x114, 0xf);
-    NGEMM_WITH(0x118, 0xf);
-    NGEMM_WITH(0x142, 0xa);                              // rows 0 and 2 to the next
-    NGEMM_WITH(0x143, 0xc);                              // row 1 to rows 2 and 3
-#undef NGEMM_WITH
-    return x;
-}
-
 // A tile of a sequence's rows, which are its queries times the heads that share a K/V head, heads fastest.
 template <class C>
 struct PromptTile {
