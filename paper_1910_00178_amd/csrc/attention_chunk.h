@@ -110,6 +110,7 @@ struct ChunkUnit {
             }
             take(a, of[0], of[1], of[2]);
             there = mine(a) && row0 >= 0 && row0 < rows;
+            same_in_all_lanes();
             return;
         }
         // Up to kMostShared sequences, a lane each.  If each tile took what its sequence's last one does, all places of the device would have the same; tiles that see less
@@ -161,7 +162,11 @@ struct ChunkUnit {
         row0 = tile * BM;
         parts = max(1, min(each, keys(a).count / kLeastTiles));
         there = part < parts && part0 >= 0 && part0 + parts <= a.slots;          // (places past the end: offsets that fall)
-        // (the same in all lanes, which the compiler does not see)
+        same_in_all_lanes();
+    }
+    // (as it is, which the compiler does not see)
+    __device__ __forceinline__ void same_in_all_lanes()
+    {
         for (int *const x : {&b, &first_row, &queries, &rows, &row0, &part, &parts, &part0}) *x = __builtin_amdgcn_readfirstlane(*x);
         start = (int64_t)__builtin_amdgcn_readfirstlane((int)start);
         there = __builtin_amdgcn_readfirstlane(there);
@@ -220,18 +225,18 @@ __device__ __forceinline__ void put_chunk_row(const ChunkArgs &a, int token, int
     else store<E, 4, false>(to, x);
 }
 
-constexpr int kFewWaves = 4;
-constexpr int few_waves_per_simd(int D, int R) { return D * R <= 128 ? 2 : 1; }
+constexpr int few_waves_per_simd(int D, int R, int NW) { return D * R <= 128 || NW == 8 ? 2 : 1; }
 
 // Sequences of few rows: those of up to R tiles of 16 (new tokens times the heads that share a K/V head, heads fastest).  A wavefront takes
 // tiles of 64 keys = 4 blocks: S^T = K Q^T and O^T = V^T P^T on 16 x 16 x 32 matrix instructions.  Row r of the first product's tile t is
 // token 4 t + r % 4 of block r / 4, so that lane 16 g + h holds row h's scores of block g's tokens, which is what the second product wants of it.
 // The weights times V's scales enter the second product as two bf16 numbers each.
-template <class E, int D, int R>
-__global__ __launch_bounds__(kFewWaves * 64, few_waves_per_simd(D, R)) void attention_chunk_few_kernel(const ChunkArgs a)
+template <class E, int D, int R, int NW>
+__global__ __launch_bounds__(NW * 64, few_waves_per_simd(D, R, NW)) void attention_chunk_few_kernel(const ChunkArgs a)
 {
     extern __shared__ __align__(16) float shared[];
-    constexpr int NW = kFewWaves, NJ = (D + 63) / 64, DT = D / 16, ROWS = 16 * R;
+    constexpr int NJ = (D + 63) / 64, DT = D / 16, ROWS = 16 * R;
+    constexpr bool SHORT = few_waves_per_simd(D, R, NW) == 1;    // of registers for the vector unit
     typedef typename E::T T;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int h = lane & 15, g = lane >> 4;
@@ -263,7 +268,7 @@ __global__ __launch_bounds__(kFewWaves * 64, few_waves_per_simd(D, R)) void atte
             const int d = 64 * (s / 2) + 16 * g + 8 * (s % 2);
             __builtin_memcpy(&q[r][s], from + (d < D ? d : 0), 16);
             if (d >= D) q[r][s] = (u4)(0u);
-            if constexpr (few_waves_per_simd(D, R) == 1) asm volatile("" : "+a"(q[r][s]));       // (out of the vector unit's registers, which are short)
+            if constexpr (SHORT) asm volatile("" : "+a"(q[r][s]));       // (out of the vector unit's registers, which are short)
         }
     }
 
@@ -350,9 +355,9 @@ __global__ __launch_bounds__(kFewWaves * 64, few_waves_per_simd(D, R)) void atte
                 m[r] = next;
 #pragma unroll
                 for (int t = 0; t < DT; ++t) {
-                    if constexpr (few_waves_per_simd(D, R) == 1) asm volatile("" : "+a"(o[r][t]));
+                    if constexpr (SHORT) asm volatile("" : "+a"(o[r][t]));
                     o[r][t] *= fall;
-                    if constexpr (few_waves_per_simd(D, R) == 1) asm volatile("" : "+a"(o[r][t]));
+                    if constexpr (SHORT) asm volatile("" : "+a"(o[r][t]));
                 }
             }
             unrolled<16>([&](auto at) {
@@ -761,6 +766,19 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_SIMD) void attention_chunk_kerne
             lost_next = (uint32_t)(__ballot(places < 0) >> (4 * n)) & 15u;
             ++i;
         };
+        if (row0 >= rows) {                                      // a wavefront without rows: codes alone
+            while (i < count) {
+                store_scales(i + 1);
+                unrolled<4 * PIECES>([&](auto x) { store_step(Index<0>{}, x, ~i & 1); });
+                n = next(i + 2);
+                load_k(places, n);
+                __syncthreads();
+                unrolled<4 * PIECES>([&](auto x) { store_step(Index<1>{}, x, ~i & 1); });
+                load_v(places, n);
+                ++i;
+            }
+            if (parts == 1) return;
+        }
         while (i < count) {                                      // (two loops, not a choice in one: that would keep the sums twice)
             while (i < count && whole()) step(Index<0>{});
             while (i < count && !whole()) step(Index<1>{});

@@ -10,6 +10,7 @@ using namespace ngemm;
 namespace {
 
 constexpr int64_t kUnits = 256;
+constexpr int kWideFew = 192;                                    // heads that leave registers for eight wavefronts
 constexpr int64_t kFewRows = 32;                                 // of a sequence, that attention_chunk_few_kernel takes at most
 
 // f(ChunkCfg<...>{}) for the smallest DP that holds head_dim.  `wide`: 256 rows a workgroup where there are registers for it.
@@ -34,7 +35,7 @@ int64_t most_tiles(int64_t queries, int64_t max_length, int64_t window, int64_t 
 
 struct ChunkCut {
     int64_t few_rows = 0, few_slots = 0, slots = 0;              // 0: no sequence can have so few, or more
-    int64_t few_places = 0, places = 0;                          // 0: keys are not shared out
+    int64_t few_places = 0, places = 0, few_waves = 4;           // places 0: keys are not shared out
     bool wide = false;
     size_t few_bytes = 0, bytes = 0;
 };
@@ -46,8 +47,10 @@ ChunkCut chunk_cut(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t hea
     if (group <= kFewRows && (batch > 1 || most_new * group <= kFewRows)) {
         cut.few_rows = most_new * group <= 16 ? 16 : kFewRows;
         cut.few_slots = batch;
-        if (batch <= kMostShared && most_tiles(std::min(most_new, cut.few_rows / group), max_length, window, sinks) >= 2 * kLeastTiles) {
-            cut.few_places = std::max(4 * kUnits, kv_heads);
+        const int64_t grid = batch * kv_heads;
+        if (grid >= kUnits / 2 && cut.few_rows <= 16 && head_dim <= kWideFew) cut.few_waves = 8;
+        else if (grid < 4 * kUnits && batch <= kMostShared && most_tiles(std::min(most_new, cut.few_rows / group), max_length, window, sinks) >= 2 * kLeastTiles) {
+            cut.few_places = std::max(cut.few_rows / 16 * head_dim <= 128 ? 2 * kUnits : kUnits, kv_heads);
             cut.few_slots += cut.few_places / kv_heads + 1;
             cut.few_bytes = (size_t)(cut.few_slots * kv_heads * cut.few_rows * (head_dim / 4 + 1) * 16);
         }
@@ -74,14 +77,14 @@ bool sizes_ok(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim
            max_length <= kMaxLength && window >= 0 && window <= kMaxLength && sinks >= 0 && sinks <= kMaxLength;
 }
 
-template <class E, int D, int R> struct FewForm {};
-template <class E, int D, int R>
+template <class E, int D, int R, int NW> struct FewForm {};
+template <class E, int D, int R, int NW>
 bool launch_few(const ChunkArgs &a, int device, hipStream_t st)
 {
-    const auto lds = [](int rows) constexpr { return kFewWaves * (2 * 16 * R + rows * D) * 4; };
-    if (!allow_lds<FewForm<E, D, R>, lds(16 * R)>(device, attention_chunk_few_kernel<E, D, R>)) return false;
+    const auto lds = [](int rows) constexpr { return NW * (2 * 16 * R + rows * D) * 4; };
+    if (!allow_lds<FewForm<E, D, R, NW>, lds(16 * R)>(device, attention_chunk_few_kernel<E, D, R, NW>)) return false;
     const int most = (int)std::min<int64_t>(16 * R, (int64_t)std::min(a.max_new, a.tokens) * (a.q_heads / a.cache.kv_heads));
-    hipLaunchKernelGGL((attention_chunk_few_kernel<E, D, R>), dim3((unsigned)(a.slots * a.cache.kv_heads)), dim3(kFewWaves * 64), (size_t)lds(most), st, a);
+    hipLaunchKernelGGL((attention_chunk_few_kernel<E, D, R, NW>), dim3((unsigned)(a.slots * a.cache.kv_heads)), dim3(NW * 64), (size_t)lds(most), st, a);
     if (a.share > 0.0f) {
         // as many rows a workgroup as leave a group of lanes no more than some 8 parts in turn, by the places that a sequence has on average
         const int lanes = kFewJoinThreads / (D / 4);
@@ -123,7 +126,13 @@ bool launch_chunk(ChunkArgs a, const ChunkCut &cut, bool vec, uint8_t *workspace
         a.slots = (int32_t)cut.few_slots, a.share = (float)cut.few_places / (float)a.cache.kv_heads, a.part_data = (f4 *)(workspace + cut.bytes);
         with_head_dim(a.cache.head_dim, [&](auto dim) {
             constexpr int D = decltype(dim)::value;
-            ok = cut.few_rows <= 16 ? launch_few<E, D, 1>(a, device, st) : launch_few<E, D, 2>(a, device, st);
+            if constexpr (D <= kWideFew) {
+                if (cut.few_waves == 8) {
+                    ok = launch_few<E, D, 1, 8>(a, device, st);
+                    return;
+                }
+            }
+            ok = cut.few_rows <= 16 ? launch_few<E, D, 1, 4>(a, device, st) : launch_few<E, D, 2, 4>(a, device, st);
         });
     }
     return ok;
