@@ -63,7 +63,7 @@ inline bool in_pieces(const Rows &r, int type)
 // What a call that moves rows of K and V to or from the cache launches: heads of a workgroup, workgroups (0: nothing to do).
 struct MovePlan {
     int32_t heads = 0;
-    int64_t groups = 0;
+    int64_t groups = 0, slots = 0;                       // slots: workgroups of a head
 };
 inline ngemm_status plan_move(MovePlan &plan, const ngemm_ctx *ctx, const ngemm_kv_cache *cache, int type, int64_t batch, int64_t tokens, const Rows &k,
                               const Rows &v, const int32_t *offsets, const int32_t *pages, int64_t pages_stride, bool written)
@@ -83,7 +83,7 @@ inline ngemm_status plan_move(MovePlan &plan, const ngemm_ctx *ctx, const ngemm_
     const int64_t heads = std::min<int64_t>(cache->kv_heads, std::max<int64_t>(slots * cache->kv_heads >= 4096 ? 2 : 1, slots * cache->kv_heads / kMaxGroups + 1));
     const int64_t groups = slots * ((cache->kv_heads + heads - 1) / heads);
     if (groups > kMaxGroups) return NGEMM_ERR_BAD_SHAPE;
-    plan = MovePlan{(int32_t)heads, groups};
+    plan = MovePlan{(int32_t)heads, groups, slots};
     return NGEMM_OK;
 }
 

@@ -74,7 +74,8 @@ struct TurnedRow {
 #pragma unroll
             for (int i = 0; i < 16; ++i) sum = __builtin_fmaf(y[i], y[i], sum);
             sum = sum_of_lanes<LANES>(sum);
-            float by = 1.0f / sqrtf(sum / (float)D + eps);
+            const float of_one = 1.0f / (float)D;
+            float by = __builtin_amdgcn_rsqf(__builtin_fmaf(sum, of_one, eps));
             if (!(sum < 0x1p120f && sum > 0x1p-100f)) {          // (the lanes of a row agree)
                 const uint32_t bits = max_of_lanes<LANES>(max(most_bits(x[0]), most_bits(x[1])));
                 if (bits == 0) {
@@ -87,11 +88,11 @@ struct TurnedRow {
                         const float z = __builtin_amdgcn_ldexpf(y[i], -ex);
                         sum = __builtin_fmaf(z, z, sum);
                     }
-                    sum = sum_of_lanes<LANES>(sum) / (float)D;
+                    sum = sum_of_lanes<LANES>(sum) * of_one;
                     // eps relative to 2^(2 ex): out of range, it counts alone
                     const float small = __builtin_amdgcn_ldexpf(__builtin_amdgcn_ldexpf(eps, -ex), -ex);
                     if (small < 0x1p120f) {
-                        by = 1.0f / sqrtf(sum + small);
+                        by = __builtin_amdgcn_rsqf(sum + small);
 #pragma unroll
                         for (int i = 0; i < 16; ++i) y[i] = __builtin_amdgcn_ldexpf(y[i], -ex);
                     } else {
@@ -220,7 +221,6 @@ __global__ __launch_bounds__(16 * LANES) void kv_write_rotated_kernel(const Turn
     block += head0 * head_bytes;
     const int end = min(head0 + a.heads, a.cache.kv_heads);
     for (int head = head0, turn = 0; head < end; ++head, turn ^= 1, block += head_bytes) {
-        if (head > head0) load(head);
         float y[16];
         row.turn(y, k, args.weight != nullptr, w, args.eps, D);
         Piece<F32> z[2];
@@ -243,6 +243,7 @@ __global__ __launch_bounds__(16 * LANES) void kv_write_rotated_kernel(const Turn
                 ((float *)(block + 32 * D))[16 + token] = v_finite ? v_most / 127.0f : __builtin_nanf("");
             }
         }
+        if (head + 1 < end) load(head + 1);              // on their way while this head's codes are turned and stored
         __syncthreads();                                 // (the next head writes the other half)
         for (int i = tid; i < D; i += 16 * LANES) {      // tokens 4 t .. 4 t + 3 of elements 4 q .. 4 q + 3
             const int t = i & 3, q = i >> 2;
