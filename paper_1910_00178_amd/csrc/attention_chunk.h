@@ -649,12 +649,13 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_SIMD) void attention_chunk_kerne
                 ks[G & 1] = *(const f4 *)from;
                 if constexpr (G == 4) vs_next = B == 0 ? vs_from[i % 3 * (C::kScales / 4) + 32] : vs_from[next * (C::kScales / 4)];
             }
-            float x = __builtin_fmaf(s[B][N], ks[N / 4 & 1][N % 4], -m);
-            if constexpr (MASKED) x = where_bit(seen, 16 * (N / 8) + N % 8, x, -__builtin_inff());
-            x = __builtin_amdgcn_exp2f(x);
+            float x = __builtin_amdgcn_exp2f(__builtin_fmaf(s[B][N], ks[N / 4 & 1][N % 4], -m));
+            // what is not seen is made 0 by its bits, whatever it is: as a weight, and times V's scale, which may be NaN
+            const uint32_t keep = MASKED ? (uint32_t)__builtin_amdgcn_sbfe((int)seen, 16 * (N / 8) + N % 8, 1) : 0;
+            if constexpr (MASKED) x = __uint_as_float(__float_as_uint(x) & keep);
             sum += x;
             x *= of_row<N>(vs);
-            if constexpr (MASKED) x = where_bit(seen, 16 * (N / 8) + N % 8, x, 0.0f);            // (a hidden key's scale may be NaN)
+            if constexpr (MASKED) x = __uint_as_float(__float_as_uint(x) & keep);
             w[N % 2] = x;
             if constexpr (N % 2 == 1) {
                 if constexpr (SPLIT) {
