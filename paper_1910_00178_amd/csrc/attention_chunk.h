@@ -113,8 +113,8 @@ struct ChunkUnit {
             same_in_all_lanes();
             return;
         }
-        // Up to kMostShared sequences, a lane each.  If each tile took what its sequence's last one does, all places of the device would have the same; tiles that see less
-        // are cut into as many parts.
+        // Up to kMostShared sequences, a lane each.  All places of the device would have the same if each tile saw what its sequence's first and last ones do on
+        // average; all of a sequence's are cut into as many parts as its last one's keys take places (at most twice the places in all).
         constexpr int TURNS = kMostShared / 64;
         const int lane = threadIdx.x & 63;
         int of[TURNS][3] = {}, tiles[TURNS] = {}, most[TURNS] = {};
@@ -126,9 +126,11 @@ struct ChunkUnit {
             of[i][0] = a.offsets[at], of[i][1] = a.offsets[at + 1], of[i][2] = a.starts ? a.starts[at] : 0;
             take(a, of[i][0], of[i][1], of[i][2]);
             tiles[i] = 64 * i + lane < a.batch && mine(a) ? (rows + BM - 1) / BM : 0;
+            row0 = 0;
+            const int least = tiles[i] > 0 ? keys(a).count : 0;
             row0 = max(tiles[i] - 1, 0) * BM;
             most[i] = tiles[i] > 0 ? keys(a).count : 0;
-            work += (float)tiles[i] * (float)most[i];
+            work += (float)tiles[i] * (0.5f * (float)(most[i] + max(least, 0)));
         }
         work = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sums_up_to(work)), 63));
         const float share = a.share / fmaxf(work, 1.0f);
@@ -587,7 +589,8 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_SIMD) void attention_chunk_kerne
             if constexpr (VEC) q[s] = *(const u4 *)at;
             else __builtin_memcpy(&q[s], at, 16);
             if (d >= D) q[s] = (u4)(0u);
-            asm volatile("" : "+a"(q[s]));               // (only the matrix unit reads it: beside the sums, out of the vector unit's registers)
+            // (only the matrix unit reads it: beside the sums, out of the vector unit's registers, where a wavefront has more than these)
+            if constexpr (C::PER_SIMD == 1) asm volatile("" : "+a"(q[s]));
         }
     }
     // the key whose scores are row `col` of the first product: so that a lane holds 8 consecutive keys' of each 16
@@ -703,9 +706,9 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_SIMD) void attention_chunk_kerne
             sum = 0.0f;
 #pragma unroll
             for (int t = 0; t < DT; ++t) {               // (one after the other, and not before the branch: or the registers would not do)
-                asm volatile("" : "+a"(o[t]));
+                if constexpr (C::PER_SIMD == 1) asm volatile("" : "+a"(o[t]));
                 o[t] *= fall;
-                asm volatile("" : "+a"(o[t]));
+                if constexpr (C::PER_SIMD == 1) asm volatile("" : "+a"(o[t]));
             }
 #pragma unroll
             for (int e = 0; e < 16; e += 2) {

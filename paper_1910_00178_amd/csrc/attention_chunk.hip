@@ -51,7 +51,7 @@ ChunkCut chunk_cut(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t hea
         if (grid >= kUnits / 2 && cut.few_rows <= 16 && head_dim <= kWideFew) cut.few_waves = 8;
         else if (grid < 4 * kUnits && batch <= kMostShared && most_tiles(std::min(most_new, cut.few_rows / group), max_length, window, sinks) >= 2 * kLeastTiles) {
             cut.few_places = std::max(cut.few_rows / 16 * head_dim <= 128 ? 2 * kUnits : kUnits, kv_heads);
-            cut.few_slots += cut.few_places / kv_heads + 1;
+            cut.few_slots += 2 * cut.few_places / kv_heads + 4;             // (and for rounding)
             cut.few_bytes = (size_t)(cut.few_slots * kv_heads * cut.few_rows * (head_dim / 4 + 1) * 16);
         }
     }
@@ -62,7 +62,7 @@ ChunkCut chunk_cut(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t hea
         const int64_t grid = std::max(batch, (tokens * group + height - 1) / height) * kv_heads;
         if (batch <= kMostShared && grid < places && most_tiles(std::min(most_new, height / group + 2), max_length, window, sinks) >= 2 * kLeastTiles) {
             cut.places = places;
-            cut.slots += cut.places / kv_heads + 1;
+            cut.slots += 2 * cut.places / kv_heads + 4;
             with_chunk_form(head_dim, cut.wide, [&](auto form) { cut.bytes = (size_t)(cut.slots * kv_heads) * decltype(form)::kPart * 16; });
         }
     }
