@@ -73,8 +73,8 @@ __device__ __forceinline__ int chunk_place(const ChunkArgs &a, int b, int head, 
     return there && id >= 0 && id < a.cache.num_pages ? (id * a.cache.kv_heads + head) * a.cache.page_blocks + (index - page * a.cache.page_blocks) : -1;
 }
 
-// A tile of a sequence's rows (new tokens times the heads that share a K/V head, heads fastest) and a workgroup's share of its keys.  FEW: the sequences of
-// up to few_rows rows, a tile each; else the others, in tiles of BM.
+// A tile of BM of a sequence's rows (new tokens times the heads that share a K/V head, heads fastest) and a workgroup's share of its keys.  FEW: of the sequences of
+// up to few_rows rows; else of the others.
 template <bool FEW, int BM>
 struct ChunkUnit {
     int b, first_row, queries, rows, row0, group;                // first_row: of the packed rows of tokens
@@ -92,7 +92,7 @@ struct ChunkUnit {
         return ChunkRow(a, (int)min(max(start + min(r, rows - 1) / group, (int64_t)-1), (int64_t)0x7ffffffe));
     }
     __device__ __forceinline__ ChunkTiles keys(const ChunkArgs &a) const { return ChunkTiles(a, row(a, row0), row(a, row0 + BM - 1)); }
-    __device__ __forceinline__ bool mine(const ChunkArgs &a) const { return FEW ? rows > 0 && rows <= min(a.few_rows, BM) : rows > a.few_rows; }
+    __device__ __forceinline__ bool mine(const ChunkArgs &a) const { return FEW ? rows > 0 && rows <= a.few_rows : rows > a.few_rows; }
 
     // Workgroup `number` of a head (JOIN: tile `number`).
     template <int JOIN>
@@ -101,7 +101,9 @@ struct ChunkUnit {
         if (a.share == 0.0f) {                                   // a workgroup takes all keys of its tile
             int of[3];
             if constexpr (FEW) {
-                b = number;
+                const int each = (a.few_rows + BM - 1) / BM;
+                b = number / each;
+                row0 = number % each * BM;
                 of[0] = a.offsets[b], of[1] = a.offsets[b + 1], of[2] = a.starts ? a.starts[b] : 0;
             } else {                                             // sequence b has the slots floor(rows before it / BM) + b .. : as many as its rows need or one more
                 const int group = this->group;
@@ -245,7 +247,7 @@ __global__ __launch_bounds__(NW * 64, few_waves_per_simd(D, R, NW)) void attenti
     const int kv_heads = a.cache.kv_heads, head = blockIdx.x % kv_heads;
     const ChunkUnit<true, ROWS> unit(a, blockIdx.x / kv_heads, Index<0>{});
     if (!unit.there) return;
-    const int group = unit.group, rows = unit.rows, parts = unit.parts, b = unit.b;
+    const int group = unit.group, rows = min(unit.rows - unit.row0, ROWS), parts = unit.parts, b = unit.b;         // rows: of this tile
     const ChunkTiles list = unit.keys(a);
     // parts of whole turns of the wavefronts (the last of them may be empty)
     const int each = ((list.count + parts - 1) / parts + NW - 1) / NW * NW;
@@ -262,7 +264,7 @@ __global__ __launch_bounds__(NW * 64, few_waves_per_simd(D, R, NW)) void attenti
     ChunkRow range[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {                        // (rows past the last repeat it and are not written)
-        const int row = min(16 * r + h, rows - 1), query = row / group;
+        const int row = unit.row0 + min(16 * r + h, rows - 1), query = row / group;
         range[r] = unit.row(a, row);
         const T *from = (const T *)a.q.data + (unit.first_row + query) * a.q.token_stride + (head * group + row % group) * a.q.head_stride;
 #pragma unroll
@@ -433,12 +435,13 @@ __global__ __launch_bounds__(NW * 64, few_waves_per_simd(D, R, NW)) void attenti
             to[1 + piece] = sum;
             if (piece == 0) to[0] = (f4){ref, weight, 0.0f, 0.0f};
         } else {
-            put_chunk_row<E>(a, unit.first_row + row / group, head * group + row % group, 4 * piece, sum, weight);
+            const int of = unit.row0 + row;
+            put_chunk_row<E>(a, unit.first_row + of / group, head * group + of % group, 4 * piece, sum, weight);
         }
     }
 }
 
-// The parts of a sequence's rows, joined in an order that depends on nothing but their number.  Lanes take D / 4 pieces of a row; with few parts a workgroup has as
+// The parts of a tile's rows, joined in an order that depends on nothing but their number.  Lanes take D / 4 pieces of a row; with few parts a workgroup has as
 // many rows as lanes allow, with many (rows_each 1) groups of lanes take the parts in turn, and the groups' sums are added in their order.
 constexpr int kFewJoinThreads = 256;
 
@@ -452,9 +455,9 @@ __global__ __launch_bounds__(kFewJoinThreads) void attention_chunk_few_join_kern
     const int head = id % kv_heads, number = id / kv_heads;
     const ChunkUnit<true, ROWS> unit(a, number, Index<1>{});
     const int groups = SLOTS / rows_each, slot = tid / PIECES, piece = tid % PIECES;
-    const int row = row0 + slot / groups, g = slot % groups;
-    if (!unit.there || unit.parts == 1 || row0 >= unit.rows) return;
-    const f4 *from = a.part_data + (((int64_t)unit.part0 * kv_heads + head) * ROWS + min(row, unit.rows - 1)) * (PIECES + 1);
+    const int row = row0 + slot / groups, g = slot % groups, rows = min(unit.rows - unit.row0, ROWS);
+    if (!unit.there || unit.parts == 1 || row0 >= rows) return;
+    const f4 *from = a.part_data + (((int64_t)unit.part0 * kv_heads + head) * ROWS + min(row, rows - 1)) * (PIECES + 1);
     const int64_t step = (int64_t)kv_heads * ROWS * (PIECES + 1);
     float top = -3.0e38f, weight = 0.0f;
     f4 sum = (f4)(0.0f);
@@ -480,14 +483,15 @@ __global__ __launch_bounds__(kFewJoinThreads) void attention_chunk_few_join_kern
         if (piece == 0) weights[slot] = weight, refs[slot] = top;
     }
     __syncthreads();
-    if (g > 0 || slot >= groups * rows_each || row >= unit.rows) return;
+    if (g > 0 || slot >= groups * rows_each || row >= rows) return;
     for (int x = 1; x < min(groups, unit.parts); ++x) {
         const float now = fmaxf(top, refs[slot + x]), fall = __builtin_amdgcn_exp2f(top - now), by = __builtin_amdgcn_exp2f(refs[slot + x] - now);
         weight = weight * fall + weights[slot + x] * by;
         sum = sum * fall + sums[tid + x * PIECES] * by;
         top = now;
     }
-    put_chunk_row<E>(a, unit.first_row + row / unit.group, head * unit.group + row % unit.group, 4 * piece, sum, weight);
+    const int of = unit.row0 + row;
+    put_chunk_row<E>(a, unit.first_row + of / unit.group, head * unit.group + of % unit.group, 4 * piece, sum, weight);
 }
 
 // ---- many rows ----
@@ -847,23 +851,23 @@ __global__ __launch_bounds__(C::NW * 64) void attention_chunk_join_kernel(const 
     const f4 *from = a.part_data + ((int64_t)tile.part0 * kv_heads + head) * C::kPart + tid;
     float top = -3.0e38f, l = 0.0f;
     f4 o = (f4)(0.0f);
-    for (int p0 = 0; p0 < parts; p0 += 4) {                      // four on their way together
-        f4 stats[4], x[4];
+    for (int p0 = 0; p0 < parts; p0 += 8) {                      // eight on their way together
+        f4 stats[8], x[8];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 8; ++i) {
             const f4 *part = from + (int64_t)min(p0 + i, parts - 1) * kv_heads * C::kPart;
             stats[i] = part[PIECES * THREADS];
             x[i] = part[piece * THREADS];
         }
         float now = top;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) now = fmaxf(now, stats[i][0]);
+        for (int i = 0; i < 8; ++i) now = fmaxf(now, stats[i][0]);
         const float fall = __builtin_amdgcn_exp2f(top - now);
         l *= fall;
         o *= fall;
         top = now;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+        for (int i = 0; i < 8; ++i) {
             if (p0 + i >= parts) break;
             const float by = __builtin_amdgcn_exp2f(stats[i][0] - top);
             l += stats[i][1] * by;

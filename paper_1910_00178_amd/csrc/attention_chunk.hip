@@ -11,7 +11,7 @@ namespace {
 
 constexpr int64_t kUnits = 256;
 constexpr int kWideFew = 192;                                    // heads that leave registers for eight wavefronts
-constexpr int64_t kFewRows = 32;                                 // of a sequence, that attention_chunk_few_kernel takes at most
+constexpr int64_t kFewRows = 64;                                 // of a sequence, that attention_chunk_few_kernel takes at most, in tiles of 16 or 32
 
 // f(ChunkCfg<...>{}) for the smallest DP that holds head_dim.  `wide`: 256 rows a workgroup where there are registers for it.
 template <class F>
@@ -46,13 +46,15 @@ ChunkCut chunk_cut(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t hea
     const int64_t group = q_heads / kv_heads, most_new = std::min(max_new, tokens);
     if (group <= kFewRows && (batch > 1 || most_new * group <= kFewRows)) {
         cut.few_rows = most_new * group <= 16 ? 16 : kFewRows;
-        cut.few_slots = batch;
-        const int64_t grid = batch * kv_heads;
+        const int64_t height = cut.few_rows <= 16 ? 16 : 32, each = (std::min(cut.few_rows, most_new * group) + height - 1) / height;
+        cut.few_rows = each * height;
+        cut.few_slots = batch * each;
+        const int64_t grid = cut.few_slots * kv_heads;
         if (grid >= kUnits / 2 && cut.few_rows <= 16 && head_dim <= kWideFew) cut.few_waves = 8;
-        else if (grid < 4 * kUnits && batch <= kMostShared && most_tiles(std::min(most_new, cut.few_rows / group), max_length, window, sinks) >= 2 * kLeastTiles) {
-            cut.few_places = std::max(cut.few_rows / 16 * head_dim <= 128 ? 2 * kUnits : kUnits, kv_heads);
+        else if (grid < 4 * kUnits && batch <= kMostShared && most_tiles(std::min(most_new, height / group + 2), max_length, window, sinks) >= 2 * kLeastTiles) {
+            cut.few_places = std::max(height / 16 * head_dim <= 128 ? 2 * kUnits : kUnits, kv_heads);
             cut.few_slots += 2 * cut.few_places / kv_heads + 4;             // (and for rounding)
-            cut.few_bytes = (size_t)(cut.few_slots * kv_heads * cut.few_rows * (head_dim / 4 + 1) * 16);
+            cut.few_bytes = (size_t)(cut.few_slots * kv_heads * height * (head_dim / 4 + 1) * 16);
         }
     }
     if (most_new * group > cut.few_rows) {
@@ -89,9 +91,10 @@ bool launch_few(const ChunkArgs &a, int device, hipStream_t st)
         // as many rows a workgroup as leave a group of lanes no more than some 8 parts in turn, by the places that a sequence has on average
         const int lanes = kFewJoinThreads / (D / 4);
         int rows_each = 1;
-        while (rows_each * 2 <= std::min(lanes, 16 * R) && 4 * a.slots * rows_each <= a.batch * lanes * 8) rows_each *= 2;
+        const int64_t tiles = (int64_t)a.batch * ((a.few_rows + 16 * R - 1) / (16 * R));
+        while (rows_each * 2 <= std::min(lanes, 16 * R) && a.slots * rows_each <= tiles * lanes * 2) rows_each *= 2;
         const int blocks = (most + rows_each - 1) / rows_each;
-        hipLaunchKernelGGL((attention_chunk_few_join_kernel<E, D, R>), dim3((unsigned)(a.batch * a.cache.kv_heads * blocks)), dim3(kFewJoinThreads), 0, st, a,
+        hipLaunchKernelGGL((attention_chunk_few_join_kernel<E, D, R>), dim3((unsigned)(tiles * a.cache.kv_heads * blocks)), dim3(kFewJoinThreads), 0, st, a,
                            rows_each, blocks);
     }
     return true;
