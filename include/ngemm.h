@@ -519,8 +519,10 @@ ngemm_status ngemm_attention_decode(ngemm_ctx *ctx, const ngemm_kv_cache *cache,
  * sequence, max_length: the most tokens of one with them (up to 2^30); larger numbers are right as well, and slower, since the launches and the workspace are
  * sized by them.  With smaller ones a sequence's rows past the first max_new are left alone, and tokens from max_length on are not read.  window and
  * sinks up to 2^30.  Softmax statistics and sums are float; scores are products of the 8-bit codes and the queries as they are; the weights w_t
- * times V's scales enter the second product as bf16 (bf16 rows of sequences with more than 32 rows, new tokens times q_heads / kv_heads) or as the sum of
- * two bf16 numbers, 16 bits, so that they have the floats' range.  Workspace, order of sums and streams as for ngemm_attention_decode.
+ * times V's scales enter the second product as bf16 (bf16 rows of sequences of many of them) or as the sum of two bf16 numbers, 16 bits (f16 rows, and
+ * sequences of few: at most 64 new tokens times q_heads / kv_heads), so that they have the floats' range.  The keys of a sequence are shared out over workgroups
+ * by the lengths that the device holds; the parts meet in the workspace and are joined in their order, so that equal calls give equal bits.  The workspace has to
+ * be 16-byte aligned and must not be in use by a call on another stream.  Rows of Q and O of the usual strides and 16-byte alignment move in 16-byte pieces.
  */
 size_t ngemm_attention_chunk_workspace_bytes(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t tokens, int64_t max_new,
                                              int64_t max_length, int64_t window, int64_t sinks);

@@ -172,7 +172,7 @@ ngemm_status ngemm_attention_chunk(ngemm_ctx *ctx, const ngemm_kv_cache *cache, 
     if (const ngemm_status s = check_rows(q, type, tokens, q_heads, head_dim, false); s != NGEMM_OK) return s;
     if (const ngemm_status s = check_rows(o, type, tokens, q_heads, head_dim, true); s != NGEMM_OK) return s;
     const ChunkCut cut = chunk_cut(batch, q_heads, kv_heads, head_dim, tokens, max_new, max_length, window, sinks);
-    if (std::max(cut.slots * kv_heads * (cut.places > 0 ? head_dim / 8 + 4 : 1), cut.few_slots * kv_heads * (cut.few_places > 0 ? cut.few_rows : 1)) > kMaxGroups)
+    if (std::max(cut.slots * kv_heads * (cut.places > 0 ? head_dim / 8 + 8 : 1), cut.few_slots * kv_heads * (cut.few_places > 0 ? cut.few_rows : 1)) > kMaxGroups)
         return NGEMM_ERR_BAD_SHAPE;
     const size_t need = cut.few_bytes + cut.bytes;
     if (need > 0 && !workspace_dev) return NGEMM_ERR_INVALID_ARG;

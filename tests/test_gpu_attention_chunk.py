@@ -215,6 +215,89 @@ def test_missing_pages_and_limits(ctx):  # noqa: F811
         assert not run(ctx, cache, table, q, new, starts, longest=0).any()
 
 
+@pytest.mark.parametrize("dtype", [F16, BF16])
+@pytest.mark.parametrize("window", [(0, 0), (40, 5)], ids=["all", "window"])
+def test_many_sequences(ctx, window, dtype):  # noqa: F811
+    """More sequences than share keys out: single tokens, some tokens, pieces of prompts, none."""
+    g = gen(17)
+    new = [int(n) for n in torch.randint(0, 90, (150,), generator=g)]
+    new[::3] = [1] * len(new[::3])
+    starts = [int(n) for n in torch.randint(0, 700, (150,), generator=g)]
+    for heads in ((2, 1, 64), (6, 2, 32)):
+        for most in (new, [min(n, 7) for n in new]):
+            cache, table, q = make(18, heads, most, starts, dtype, page=32)
+            got = run(ctx, cache, table, q, most, starts, *window)
+            check(got, *wanted(cache, table, q, most, starts, *window), dtype, weights=weights(heads, most, dtype))
+
+
+@pytest.mark.parametrize("heads", [(4, 1, 128), (3, 3, 64), (2, 1, 208)], ids=lambda h: "x".join(map(str, h)))
+def test_rows_between_the_forms(ctx, heads):  # noqa: F811
+    """As many rows as the kernel of few takes, and one more; a tile's rows and one more."""
+    group = heads[0] // heads[1]
+    for rows in (16, 32, 64, 128, 256):
+        for more in (0, 1):
+            n = rows // group + more
+            new, starts = [n, 1, n], [300, 900, 0]
+            cache, table, q = make(19, heads, new, starts, F16)
+            got = run(ctx, cache, table, q, new, starts)
+            check(got, *wanted(cache, table, q, new, starts), F16)
+
+
+def test_replay_with_other_lengths(ctx):  # noqa: F811
+    """Captured once, replayed with other lengths, pages and queries: what eager calls with the same bounds give."""
+    Hq, H, D, page, batch, most, longest = 8, 2, 64, 32, 4, 40, 3000
+    per = longest // page + 1
+    cases = [([1, 40, 3, 0], [2000, 100, 0, 50]), ([40, 40, 40, 40], [2960, 0, 1000, 30]), ([2, 1, 0, 1], [5, 2990, 7, 400])]
+    g = gen(20)
+    caches = [make(21 + i, (Hq, H, D), new, starts, BF16, page=page) for i, (new, starts) in enumerate(cases)]
+    pool = max(c.raw.shape[0] for c, _, _ in caches)
+    raw = torch.zeros(pool, H, page // 16, 32 * D + 128, dtype=torch.int8, device="cuda")
+    c = ng.ngemm_kv_cache_create(ctx, pool, page, H, D, raw, raw.numel())
+    n = most * batch
+    q, o = (torch.zeros(n, Hq, D, dtype=BF16, device="cuda") for _ in range(2))
+    off, start, pages = torch.zeros(batch + 1, dtype=torch.int32, device="cuda"), torch.zeros(batch, dtype=torch.int32, device="cuda"), torch.full((batch, per), -1).int().cuda()
+    size = ng.ngemm_attention_chunk_workspace_bytes(batch, Hq, H, D, n, most, longest, 900, 8)
+    ws = torch.empty(max(16, size), dtype=torch.uint8, device="cuda")
+
+    def call():
+        ng.ngemm_attention_chunk(ctx, c, ng.NGEMM_BF16, batch, Hq, n, q, Hq * D, D, off, start, most, longest, pages, per, 900, 8, 0.125, o, Hq * D, D, ws, size)
+
+    def fill(i):
+        (new, starts), (cache, table, rows) = cases[i], caches[i]
+        raw.zero_()
+        raw[:cache.raw.shape[0]].copy_(cache.raw)
+        q.zero_()
+        q[:sum(new)].copy_(rows)
+        off.copy_(ints(sums(new)))
+        start.copy_(ints(starts))
+        pages.fill_(-1)
+        pages[:, :table.shape[1]].copy_(table[:, :per])
+        o.zero_()
+        torch.cuda.synchronize()
+
+    fill(0)
+    call()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    for i in (0, 1, 2, 0, 2, 1):
+        fill(i)
+        graph.replay()
+        torch.cuda.synchronize()
+        got = o.clone()
+        fill(i)
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(o, got)
+        torch.randn(1000, device="cuda").sum().item()
+        new, starts = cases[i]
+        cache, table, rows = caches[i]
+        check(got.cpu()[:sum(new)], *wanted(cache, table, rows, new, starts, 900, 8), BF16)
+        assert not got[sum(new):].any()
+    ng.ngemm_kv_cache_free(c)
+
+
 def test_as_decode(ctx):  # noqa: F811
     """A token of each sequence: what ngemm_attention_decode gives, up to the roundings of both."""
     lengths, heads = [1, 40, 333, 64], (8, 2, 128)
