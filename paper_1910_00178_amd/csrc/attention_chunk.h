@@ -87,6 +87,13 @@ struct ChunkUnit {
         const ChunkSequence seq(a, begin, end, at);
         first_row = seq.first, queries = seq.queries, start = seq.start, rows = queries * group;
     }
+    // (of rows that are the same in all lanes: `start` takes 64 bits, which the compiler compares in the vector unit and leaves there)
+    __device__ __forceinline__ ChunkRow row_of_all(const ChunkArgs &a, int r) const
+    {
+        ChunkRow x = row(a, r);
+        x.lo = __builtin_amdgcn_readfirstlane(x.lo), x.hi = __builtin_amdgcn_readfirstlane(x.hi);
+        return x;
+    }
     __device__ __forceinline__ ChunkRow row(const ChunkArgs &a, int r) const
     {
         return ChunkRow(a, (int)min(max(start + min(r, rows - 1) / group, (int64_t)-1), (int64_t)0x7ffffffe));
@@ -98,7 +105,7 @@ struct ChunkUnit {
     template <int JOIN>
     __device__ __forceinline__ ChunkUnit(const ChunkArgs &a, int number, Index<JOIN>) : row0(0), group(a.q_heads / a.cache.kv_heads), part(0), parts(1), part0(0)
     {
-        if (a.share == 0.0f) {                                   // a workgroup takes all keys of its tile
+        if (FEW ? a.share == 0.0f : a.batch > kMostShared) {     // a workgroup takes all keys of its tile
             int of[3];
             if constexpr (FEW) {
                 const int each = (a.few_rows + BM - 1) / BM;
@@ -115,8 +122,10 @@ struct ChunkUnit {
             same_in_all_lanes();
             return;
         }
-        // Up to kMostShared sequences, a lane each.  All places of the device would have the same if each tile saw what its sequence's first and last ones do on
-        // average; all of a sequence's are cut into as many parts as its last one's keys take places (at most twice the places in all).
+        // Up to kMostShared sequences, a lane each: tiles are numbered without gaps.  (Workgroups without a tile between others leave the units unevenly loaded:
+        // 16 x 128 tokens behind 1000, a tile per unit, 88 us with them, 52 without.)  All places of the device would have the same if each tile saw what its sequence's
+        // first and last ones do on average; all of a sequence's are cut into as many parts as its last one's keys take places (at most twice the places in all;
+        // share 0: into one).
         constexpr int TURNS = kMostShared / 64;
         const int lane = threadIdx.x & 63;
         int of[TURNS][3] = {}, tiles[TURNS] = {}, most[TURNS] = {};
@@ -128,13 +137,14 @@ struct ChunkUnit {
             of[i][0] = a.offsets[at], of[i][1] = a.offsets[at + 1], of[i][2] = a.starts ? a.starts[at] : 0;
             take(a, of[i][0], of[i][1], of[i][2]);
             tiles[i] = 64 * i + lane < a.batch && mine(a) ? (rows + BM - 1) / BM : 0;
+            if (a.share == 0.0f) continue;
             row0 = 0;
             const int least = tiles[i] > 0 ? keys(a).count : 0;
             row0 = max(tiles[i] - 1, 0) * BM;
             most[i] = tiles[i] > 0 ? keys(a).count : 0;
             work += (float)tiles[i] * (0.5f * (float)(most[i] + max(least, 0)));
         }
-        work = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sums_up_to(work)), 63));
+        if (a.share > 0.0f) work = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, sums_up_to(work)), 63));
         const float share = a.share / fmaxf(work, 1.0f);
         int tile = 0, each = 1, tiles_before = 0, parts_before = 0;
         there = false;
@@ -144,7 +154,7 @@ struct ChunkUnit {
             if (64 * i >= a.batch) break;
             // (a whole number of parts may come out as a little less)
             const int cut = max(1, min((int)((float)most[i] * share + 0x1p-8f), most[i] / kLeastTiles)), all = tiles[i] * cut;
-            const int tiles_to = tiles_before + sums_up_to(tiles[i]), parts_to = parts_before + sums_up_to(all);
+            const int tiles_to = tiles_before + sums_up_to(tiles[i]), parts_to = a.share > 0.0f ? parts_before + sums_up_to(all) : tiles_to;
             const int begin = JOIN ? tiles_to - tiles[i] : parts_to - all, end = JOIN ? tiles_to : parts_to;
             const uint64_t here = __ballot(begin <= number && number < end);
             if (here) {
@@ -156,7 +166,11 @@ struct ChunkUnit {
                 tile = JOIN ? at : at / each;
                 part = JOIN ? 0 : at % each;
                 part0 = __builtin_amdgcn_readlane(parts_to - all, l) + tile * each;
-                tile = __builtin_amdgcn_readlane(tiles[i], l) - 1 - tile;          // the longest first
+                // The longest first; of whole tiles every other four turned round: workgroups go to a chiplet's four engines in turn, and one of these would always
+                // get the longest of four (64 x 512 tokens: 320 us so, 307 turned).
+                const int count = __builtin_amdgcn_readlane(tiles[i], l), four = tile & ~3;
+                if (each == 1 && (__builtin_amdgcn_readlane(tiles_to - tiles[i], l) + four) & 4) tile = four + min(4, count - four) - 1 - (tile & 3);
+                tile = count - 1 - tile;
                 there = true;
             }
             tiles_before = __builtin_amdgcn_readlane(tiles_to, 63);
@@ -164,7 +178,7 @@ struct ChunkUnit {
         }
         if (!there) return;
         row0 = tile * BM;
-        parts = max(1, min(each, keys(a).count / kLeastTiles));
+        if (each > 1) parts = max(1, min(each, keys(a).count / kLeastTiles));
         there = part < parts && part0 >= 0 && part0 + parts <= a.slots;          // (places past the end: offsets that fall)
         same_in_all_lanes();
     }
@@ -517,19 +531,20 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_SIMD) void attention_chunk_kerne
     constexpr bool SPLIT = __is_same(typename E::T, _Float16);   // two bf16 numbers per weight
     // codes are asked for two blocks ahead of their conversion: a prompt of 8192 554 -> 548 us, 512 tokens behind 16000 111 -> 110. Rows of f16 of
     // 128 keep one block ahead, whose registers are all taken
-    constexpr bool EARLY = !(SPLIT && DP == 128);
+    constexpr bool EARLY = DP != 128 || (!SPLIT && PIECES == 1);
     typedef typename E::T T;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, col = lane & 31;
     const int kv_heads = a.cache.kv_heads, D = a.cache.head_dim;
     const int head = blockIdx.x % kv_heads, number = blockIdx.x / kv_heads;
-    const ChunkUnit<false, C::BM> tile(a, a.share > 0.0f ? number : a.slots - 1 - number, Index<0>{});
+    const ChunkUnit<false, C::BM> tile(a, a.batch <= kMostShared ? number : a.slots - 1 - number, Index<0>{});
     if (!tile.there) return;
     const int group = tile.group, rows = tile.rows, parts = tile.parts;
-    const ChunkTiles list = tile.keys(a);
-    const int first = (int)((int64_t)list.count * tile.part / parts), count = (int)((int64_t)list.count * (tile.part + 1) / parts) - first;
+    const ChunkTiles list(a, tile.row_of_all(a, tile.row0), tile.row_of_all(a, tile.row0 + C::BM - 1));
+    const int first = __builtin_amdgcn_readfirstlane((int)((int64_t)list.count * tile.part / parts));
+    const int count = __builtin_amdgcn_readfirstlane((int)((int64_t)list.count * (tile.part + 1) / parts)) - first;
 
     const int row0 = tile.row0 + 32 * wave, row = min(row0 + col, rows - 1);             // the wavefront's first, the lane's
-    const ChunkRow range = tile.row(a, row), row_first = tile.row(a, row0), row_last = tile.row(a, row0 + 31);
+    const ChunkRow range = tile.row(a, row), row_first = tile.row_of_all(a, row0), row_last = tile.row_of_all(a, row0 + 31);
 
     // ---- the blocks of 16 tiles: lane l looks up block l % 4 of tile l / 4 ----
     const int block_bytes = 32 * D + 128;
@@ -828,7 +843,10 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_SIMD) void attention_chunk_kerne
         return;
     }
     // ---- O = O^T / l: 4 consecutive elements per lane and quarter, exchanged between lane halves to 8 ----
-    T *to = (T *)a.o.data + token * a.o.token_stride + qhead * a.o.head_stride;
+    int of = row0 + col;
+    asm volatile("" : "+v"(of));                                 // (found again here: what is kept through the loop takes its registers)
+    of = min(of, rows - 1);
+    T *to = (T *)a.o.data + (tile.first_row + of / group) * a.o.token_stride + (head * group + of % group) * a.o.head_stride;
     const float by = 1.0f / weight;
 #pragma unroll
     for (int t = 0; t < DT; ++t)
@@ -854,43 +872,46 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_SIMD) void attention_chunk_kerne
         }
 }
 
-// The parts of a tile, joined in their order: a workgroup per tile and piece of 4 elements of a lane.
+// The parts of a tile, joined in their order: `blocks` workgroups a tile, DP / 8 / blocks pieces of 4 elements of a lane each.
 template <class E, class C>
-__global__ __launch_bounds__(C::NW * 64) void attention_chunk_join_kernel(const ChunkArgs a)
+__global__ __launch_bounds__(C::NW * 64) void attention_chunk_join_kernel(const ChunkArgs a, int blocks)
 {
     constexpr int THREADS = C::NW * 64, PIECES = C::DP / 8;
-    const int piece = blockIdx.x % PIECES, kv_heads = a.cache.kv_heads, head = blockIdx.x / PIECES % kv_heads, number = blockIdx.x / PIECES / kv_heads;
+    const int kv_heads = a.cache.kv_heads, block = blockIdx.x % blocks, head = blockIdx.x / blocks % kv_heads, number = blockIdx.x / blocks / kv_heads;
     const ChunkUnit<false, C::BM> tile(a, number, Index<1>{});
     const int tid = threadIdx.x, lane = tid & 63, row = tile.row0 + 32 * (tid >> 6) + (lane & 31), parts = tile.parts;
-    const int d = 8 * piece + 4 * (lane >> 5);                   // 32 (piece / 4) + 8 (piece % 4) + ..
-    if (!tile.there || parts == 1 || row >= tile.rows || d >= a.cache.head_dim) return;
+    if (!tile.there || parts == 1 || row >= tile.rows) return;
     const f4 *from = a.part_data + ((int64_t)tile.part0 * kv_heads + head) * C::kPart + tid;
-    float top = -3.0e38f, l = 0.0f;
-    f4 o = (f4)(0.0f);
-    for (int p0 = 0; p0 < parts; p0 += 8) {                      // eight on their way together
-        f4 stats[8], x[8];
+    for (int piece = block; piece < PIECES; piece += blocks) {
+        const int d = 8 * piece + 4 * (lane >> 5);               // 32 (piece / 4) + 8 (piece % 4) + ..
+        if (d >= a.cache.head_dim) return;
+        float top = -3.0e38f, l = 0.0f;
+        f4 o = (f4)(0.0f);
+        for (int p0 = 0; p0 < parts; p0 += 8) {                  // eight on their way together
+            f4 stats[8], x[8];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const f4 *part = from + (int64_t)min(p0 + i, parts - 1) * kv_heads * C::kPart;
-            stats[i] = part[PIECES * THREADS];
-            x[i] = part[piece * THREADS];
+            for (int i = 0; i < 8; ++i) {
+                const f4 *part = from + (int64_t)min(p0 + i, parts - 1) * kv_heads * C::kPart;
+                stats[i] = part[PIECES * THREADS];
+                x[i] = part[piece * THREADS];
+            }
+            float now = top;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) now = fmaxf(now, stats[i][0]);
+            const float fall = __builtin_amdgcn_exp2f(top - now);
+            l *= fall;
+            o *= fall;
+            top = now;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                if (p0 + i >= parts) break;
+                const float by = __builtin_amdgcn_exp2f(stats[i][0] - top);
+                l += stats[i][1] * by;
+                o += x[i] * by;
+            }
         }
-        float now = top;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) now = fmaxf(now, stats[i][0]);
-        const float fall = __builtin_amdgcn_exp2f(top - now);
-        l *= fall;
-        o *= fall;
-        top = now;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            if (p0 + i >= parts) break;
-            const float by = __builtin_amdgcn_exp2f(stats[i][0] - top);
-            l += stats[i][1] * by;
-            o += x[i] * by;
-        }
+        put_chunk_row<E>(a, tile.first_row + row / tile.group, head * tile.group + row % tile.group, d, o, l);
     }
-    put_chunk_row<E>(a, tile.first_row + row / tile.group, head * tile.group + row % tile.group, d, o, l);
 }
 
 }  // namespace ngemm

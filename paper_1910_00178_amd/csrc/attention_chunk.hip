@@ -43,22 +43,33 @@ ChunkCut chunk_cut(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t hea
                    int64_t window, int64_t sinks)
 {
     ChunkCut cut;
-    const int64_t group = q_heads / kv_heads, most_new = std::min(max_new, tokens);
-    if (group <= kFewRows && (batch > 1 || most_new * group <= kFewRows)) {
-        cut.few_rows = most_new * group <= 16 ? 16 : kFewRows;
-        const int64_t height = cut.few_rows <= 16 ? 16 : 32, each = (std::min(cut.few_rows, most_new * group) + height - 1) / height;
-        cut.few_rows = each * height;
-        cut.few_slots = batch * each;
+    const int64_t group = q_heads / kv_heads, most_new = std::min(max_new, tokens), most_rows = most_new * group;
+    // Sequences of up to 64 rows on attention_chunk_few_kernel (heads of 128, 32 on 8; us).  Up to 16 rows always: it reads a key once where a tile of 128 rows
+    // would convert it into LDS for them (16 x 4 tokens behind 1000: 15 for 31).  Up to 64 where their tiles of 32 fit the device together: 16 x 16 tokens behind 1000
+    // 28 for 33, 32 x 8 31 for 43; but 64 x 16 behind 500, four rounds of tiles, 66 for 42.  Among longer ones those of up to 16 alone (16 x 20 behind 1000: 35, with tiles
+    // of 32 for those of up to 64 rows 39).
+    const int64_t tall = (most_rows + 31) / 32;                  // tiles of 32 of a sequence
+    if (most_rows > 16 && most_rows <= kFewRows && batch * tall * kv_heads <= (head_dim <= 64 ? 2 * kUnits : kUnits)) cut.few_rows = 32 * tall;
+    else if (most_rows <= 16 || (group <= 16 && batch > 1)) cut.few_rows = 16;
+    if (cut.few_rows > 0) {
+        const int64_t height = std::min<int64_t>(cut.few_rows, 32);
+        cut.few_slots = batch * (cut.few_rows / height);
         const int64_t grid = cut.few_slots * kv_heads;
-        if (grid >= kUnits / 2 && cut.few_rows <= 16 && head_dim <= kWideFew) cut.few_waves = 8;
-        else if (grid < 4 * kUnits && batch <= kMostShared && most_tiles(std::min(most_new, height / group + 2), max_length, window, sinks) >= 2 * kLeastTiles) {
+        // A tile's keys by eight wavefronts of one workgroup where that fills half of the units at least: 16 x 4 tokens behind 1000 14.5, shared out and joined 19.5;
+        // 32 x 4 behind 8000 97 and 107 (16 x 4 behind 8000 57 and 51).  By four of one workgroup from two workgroups a unit on: 64 x 4 behind 1000 26.5 (by eight 32),
+        // 256 x 4 behind 500 52 (82).  Else shared out over workgroups: 8 x 4 behind 8000 34 (whole 54).
+        if (grid >= kUnits / 2 && grid < 2 * kUnits && cut.few_rows <= 16 && head_dim <= kWideFew) cut.few_waves = 8;
+        else if (grid < 2 * kUnits && batch <= kMostShared && most_tiles(std::min(most_new, height / group + 2), max_length, window, sinks) >= 2 * kLeastTiles) {
             cut.few_places = std::max(height / 16 * head_dim <= 128 ? 2 * kUnits : kUnits, kv_heads);
             cut.few_slots += 2 * cut.few_places / kv_heads + 4;             // (and for rounding)
             cut.few_bytes = (size_t)(cut.few_slots * kv_heads * height * (head_dim / 4 + 1) * 16);
         }
     }
-    if (most_new * group > cut.few_rows) {
-        cut.wide = tokens * group / batch >= 256;
+    if (most_rows > cut.few_rows) {
+        // 256 rows a workgroup convert a key once where two of 128 do it twice, but leave coarser pieces of work: prompts of 4096 155 us (128 rows: 169), 16 x 256 behind
+        // 2000 166 (177), 512 behind 16000 111 (120); a prompt of 2048 65 (57), 64 x 256 135 (120), 64 x 512 309 (293).
+        const int64_t seen = window > 0 ? std::min(max_length, window + sinks) : max_length - std::min(max_length, most_new) / 2;       // by a row, about
+        cut.wide = tokens * group / batch >= 256 && seen > 1024;
         const int64_t height = tile_rows(head_dim, cut.wide), places = cut.wide || head_dim > 128 ? kUnits : 2 * kUnits;
         cut.slots = tokens * group / height + batch;
         const int64_t grid = std::max(batch, (tokens * group + height - 1) / height) * kv_heads;
@@ -107,8 +118,11 @@ bool launch_many(const ChunkArgs &a, int device, hipStream_t st)
     if (!allow_lds<ManyForm<E, C, VEC>, C::kLds>(device, attention_chunk_kernel<E, C, VEC>)) return false;
     hipLaunchKernelGGL((attention_chunk_kernel<E, C, VEC>), dim3((unsigned)(a.slots * a.cache.kv_heads)), dim3(C::NW * 64), C::kLds, st, a);
     if (a.share > 0.0f) {
-        const int64_t tiles = (int64_t)a.tokens * (a.q_heads / a.cache.kv_heads) / C::BM + a.batch;
-        hipLaunchKernelGGL((attention_chunk_join_kernel<E, C>), dim3((unsigned)(tiles * a.cache.kv_heads * (C::DP / 8))), dim3(C::NW * 64), 0, st, a);
+        // as many pieces a workgroup as leave some thousands of them: tiles that were not shared out cost little then
+        const int64_t tiles = ((int64_t)a.tokens * (a.q_heads / a.cache.kv_heads) / C::BM + a.batch) * a.cache.kv_heads;
+        int blocks = C::DP / 8;
+        while (blocks % 2 == 0 && tiles * blocks > 2048) blocks /= 2;
+        hipLaunchKernelGGL((attention_chunk_join_kernel<E, C>), dim3((unsigned)(tiles * blocks)), dim3(C::NW * 64), 0, st, a, blocks);
     }
     return true;
 }
