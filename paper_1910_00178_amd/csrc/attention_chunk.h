@@ -64,7 +64,8 @@ struct ChunkTiles {
 };
 
 // The number of the block that holds positions 16 * index .. of sequence b and a head, or -1 where there is none.  Without branches (a table without
-// entries has been taken as one without tokens), so that loops around it have uniform ones only: sums in registers stay where they are.
+// entries has been taken as one without tokens), so that loops around it have uniform ones only: sums in registers stay where they are.  (Blocks have 640 bytes or more:
+// the number of one in a device's memory fits 32 bits.)
 __device__ __forceinline__ int chunk_place(const ChunkArgs &a, int b, int head, int index)
 {
     const int page = index / a.cache.page_blocks;

@@ -105,7 +105,7 @@ ngemm_status ngemm_qk_norm_rotate(ngemm_ctx *ctx, ngemm_type type, int64_t head_
     if (!ctx_ok(ctx) || !type_ok(type)) return NGEMM_ERR_INVALID_ARG;
     if (!head_dim_ok(head_dim) || tokens < 0 || tokens > kMaxCount || q_heads < 0 || k_heads < 0 || q_heads > 65536 || k_heads > 65536)
         return NGEMM_ERR_BAD_SHAPE;
-    if (const ngemm_status s = check_turn(ctx, rotation, head_dim, eps, q_weight_dev, k_weight_dev); s != NGEMM_OK) return s;
+    if (const ngemm_status s = check_turn(ctx, rotation, head_dim, eps, q_heads ? q_weight_dev : nullptr, k_heads ? k_weight_dev : nullptr); s != NGEMM_OK) return s;
     if (tokens == 0 || q_heads + k_heads == 0) return NGEMM_OK;
     if (rotation && !positions_dev) return NGEMM_ERR_INVALID_ARG;
     const Rows from[2] = {{const_cast<void *>(Q_dev), q_token_stride, q_head_stride}, {const_cast<void *>(K_dev), k_token_stride, k_head_stride}};

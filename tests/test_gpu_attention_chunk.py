@@ -406,3 +406,60 @@ def test_cache_past_32_bits(ctx):  # noqa: F811
         # (K's codes may be the next ones near a tie, one in thousands: a step of a code in a score)
         check(o, want, sz * 1.2, F16)
     ng.ngemm_kv_cache_free(c)
+
+
+@pytest.mark.parametrize("window", [(0, 0), (90, 3)], ids=["all", "window"])
+@pytest.mark.parametrize("batch, most, past", [(128, 40, 300), (100, 9, 200), (16, 130, 1100), (70, 2, 900), (3, 400, 1500)])
+def test_batches(ctx, batch, most, past, window):  # noqa: F811
+    """Every form by itself over batches that fill the device: tiles are numbered over up to 128 sequences, some of which have no tokens."""
+    g = gen(batch)
+    heads = (16, 8, 32)
+    for ragged in (False, True):
+        new = [int(n) for n in torch.randint(0, most + 1, (batch,), generator=g)] if ragged else [most] * batch
+        starts = [int(n) for n in torch.randint(0, past + 1, (batch,), generator=g)] if ragged else [past] * batch
+        if sum(new) == 0:
+            continue
+        cache, table, q = make(batch + 1, heads, new, starts, BF16, page=64)
+        got = run(ctx, cache, table, q, new, starts, *window)
+        check(got, *wanted(cache, table, q, new, starts, *window), BF16, weights=weights(heads, new, BF16))
+
+
+@pytest.mark.parametrize("dtype", [F16, BF16])
+def test_in_the_queries_place(ctx, dtype):  # noqa: F811
+    """O at Q's address: the same bits as elsewhere, with keys shared out and not, for few rows and for many."""
+    for heads, new, starts in (((8, 2, 128), [1, 3], [30, 20]), ((8, 2, 128), [2], [9000]), ((8, 2, 128), [16, 9], [700, 40]), ((8, 2, 128), [90, 40, 0, 70], [0, 30, 5, 100]),
+                               ((4, 4, 64), [300], [6000]), ((2, 1, 240), [700, 3], [0, 800])):
+        cache, table, q = make(23, heads, new, starts, dtype, page=64)
+        elsewhere = run(ctx, cache, table, q, new, starts)
+        raw = cache.raw.cuda()
+        c = handle(ctx, cache, raw)
+        rows, (Hq, H, D), longest = q.cuda(), heads, max(a + b for a, b in zip(new, starts))
+        size = ng.ngemm_attention_chunk_workspace_bytes(len(new), Hq, H, D, sum(new), max(new), longest, 0, 0)
+        ws = torch.empty(size + 16, dtype=torch.uint8, device="cuda")
+        ng.ngemm_attention_chunk(ctx, c, number(dtype), len(new), Hq, sum(new), rows, Hq * D, D, ints(sums(new)), ints(starts), max(new), longest, table.cuda(),
+                                 table.shape[1], 0, 0, 0.125, rows, Hq * D, D, ws, size)
+        torch.cuda.synchronize()
+        assert torch.equal(rows.cpu(), elsewhere)
+        ng.ngemm_kv_cache_free(c)
+
+
+def test_two_streams(ctx):  # noqa: F811
+    """Calls on two streams at once, each with a workspace of its own, give what they give one after the other."""
+    heads, parts = (8, 2, 128), []
+    for new, starts in (([5, 40, 300], [4000, 100, 900]), ([2] * 9, [1500] * 9)):
+        cache, table, q = make(29, heads, new, starts, BF16, page=64)
+        want = run(ctx, cache, table, q, new, starts)
+        raw, longest = cache.raw.cuda(), max(a + b for a, b in zip(new, starts))
+        size = ng.ngemm_attention_chunk_workspace_bytes(len(new), 8, 2, 128, sum(new), max(new), longest, 0, 0)
+        q = q.cuda()
+        parts.append((new, want, raw, handle(ctx, cache, raw), longest, size, q, torch.empty_like(q), table.cuda(), ints(sums(new)), ints(starts),
+                      torch.empty(size + 16, dtype=torch.uint8, device="cuda"), torch.cuda.Stream()))
+    torch.cuda.synchronize()
+    for _ in range(10):
+        for new, _want, _raw, c, longest, size, q, o, table, offsets, starts, ws, stream in parts:
+            ng.ngemm_attention_chunk(ctx, c, ng.NGEMM_BF16, len(new), 8, sum(new), q, 1024, 128, offsets, starts, max(new), longest, table, table.shape[1], 0, 0, 0.125,
+                                     o, 1024, 128, ws, size, stream.cuda_stream)
+    torch.cuda.synchronize()
+    for _new, want, _raw, c, _l, _s, _q, o, *_ in parts:
+        assert torch.equal(o.cpu(), want)
+        ng.ngemm_kv_cache_free(c)

@@ -70,6 +70,9 @@ def test_norm_rotate(ctx):
     for nothing in ({"tokens": 0}, {"hq": 0, "hk": 0}, {"tokens": 0, "q": None, "k": None, "qo": None, "ko": None, "at": None}):
         fn, *args = call(**nothing)
         fn(*args)
+    # a side without heads: its weights are not looked at (what is refused is the other side's size)
+    for unused in ({"hk": 0, "wk": HERE + 1}, {"hq": 0, "hk": 65536, "wq": HERE + 1}):
+        refused(SHAPE, *call(**({"tokens": 1 << 30, "hq": 65536, "qt": 0, "qh": 0, "kt": 0, "kh": 0, "qot": 65536 * 64, "kot": 65536 * 64} | unused)))
     for x in (r, elsewhere):
         ng.ngemm_rotation_free(x)
 
