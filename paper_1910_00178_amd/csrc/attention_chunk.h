@@ -246,10 +246,15 @@ __device__ __forceinline__ void put_chunk_row(const ChunkArgs &a, int token, int
 
 constexpr int few_waves_per_simd(int D, int R, int NW) { return D * R <= 128 || NW == 8 ? 2 : 1; }
 
-// Sequences of few rows: those of up to R tiles of 16 (new tokens times the heads that share a K/V head, heads fastest).  A wavefront takes
+// Sequences of few rows: tiles of R times 16 of them (new tokens times the heads that share a K/V head, heads fastest).  A wavefront takes
 // tiles of 64 keys = 4 blocks: S^T = K Q^T and O^T = V^T P^T on 16 x 16 x 32 matrix instructions.  Row r of the first product's tile t is
-// token 4 t + r % 4 of block r / 4, so that lane 16 g + h holds row h's scores of block g's tokens, which is what the second product wants of it.
-// The weights times V's scales enter the second product as two bf16 numbers each.
+// token 4 t + r % 4 of block r / 4, so that lane 16 g + h holds row h's scores of block g's tokens, which is what the second product wants of it:
+// codes go from memory to registers, become floats there and meet the matrix unit, without LDS.
+// A softmax in one pass: weights are exp2(s - m), m 2^8 above the largest score when it was set, so that it is set again only where a score passes it.  The weights
+// times V's scales enter the second product as two bf16 numbers each, 16 bits: the products are few, and a row of a batch of single tokens keeps the bits that
+// attention_decode gives it.
+// Bound by memory where a key is read for one tile: 32 sequences of 4 tokens behind 8000 (8 heads of 128) 97 us, 5.6 TB/s; by the chain of trips (lengths, pages, codes) in
+// small calls: 32 single tokens behind 500 9 us.
 template <class E, int D, int R, int NW>
 __global__ __launch_bounds__(NW * 64, few_waves_per_simd(D, R, NW)) void attention_chunk_few_kernel(const ChunkArgs a)
 {
@@ -458,6 +463,7 @@ __global__ __launch_bounds__(NW * 64, few_waves_per_simd(D, R, NW)) void attenti
 
 // The parts of a tile's rows, joined in an order that depends on nothing but their number.  Lanes take D / 4 pieces of a row; with few parts a workgroup has as
 // many rows as lanes allow, with many (rows_each 1) groups of lanes take the parts in turn, and the groups' sums are added in their order.
+// Bound by its trips to memory (the lengths, then the parts, four on their way together): 4 - 7 us with the launch.
 constexpr int kFewJoinThreads = 256;
 
 template <class E, int D, int R>
@@ -524,14 +530,24 @@ struct ChunkCfg {
     static constexpr int kPart = BM * 2 * (DP / 8 + 1);          // 16-byte pieces of a part: sums, maximum and weight
 };
 
+// A tile of BM rows of a sequence: S^T = K Q^T and O^T = V^T P^T on 32 x 32 x 16 matrix instructions, a wavefront 32 rows, lane c of each half row c.  Codes of 64 keys become
+// 16-bit floats (exact) once for all wavefronts, on their way into LDS; K's scales meet the scores and V's the weights, in floats.  A lane holds the scores of 8 consecutive
+// keys of each 16, which is the second product's operand as they lie.
+// A softmax in one pass, with a reference that need not be the maximum: weights are exp2(s - m), m a score that was the largest once; a block whose weights sum up to more than 2^12 in a lane
+// sets it anew.  Most blocks then have no maximum, no exchange between lanes and no sums to rescale.
+// bf16 rows: weights times V's scales rounded to bf16 (2^-9 of each, as matrix instructions take them; the formula's error 2.4e-3 of the norm for 1.7e-3 with weights in 32 bits). f16 rows:
+// two bf16 numbers, 16 bits, since one alone is less than the rows' own 11.
+// Bound: per 32 x 32 scores of heads of 128 the matrix unit takes 16 instructions of 16 cycles and the vector unit some 190; one wavefront's instructions of either kind keep the other's of the
+// same SIMD waiting (12 multiply-adds beside one matrix instruction: 113 - 120 cycles of two wavefronts, 67 and 65 of either alone), so a prompt of 8192 (32 heads on 8) takes
+// 550 us, the matrix unit busy 45 %, the vector unit 60 %, at 1.7 - 2.0 GHz. Hence what is not here: a maximum per block, conversions per wavefront, masks in tiles that all rows see.
 template <class E, class C, bool VEC>
 __global__ __launch_bounds__(C::NW * 64, C::PER_SIMD) void attention_chunk_kernel(const ChunkArgs a)
 {
     extern __shared__ __align__(1024) uint8_t lds[];
     constexpr int DP = C::DP, BN = C::BN, NW = C::NW, PIECES = C::PIECES, STEPS = DP / 16, DT = DP / 32;
     constexpr bool SPLIT = __is_same(typename E::T, _Float16);   // two bf16 numbers per weight
-    // codes are asked for two blocks ahead of their conversion: a prompt of 8192 554 -> 548 us, 512 tokens behind 16000 111 -> 110. Rows of f16 of
-    // 128 keep one block ahead, whose registers are all taken
+    // Codes are asked for two blocks ahead of their conversion: a prompt of 8192 554 -> 548 us, 512 tokens behind 16000 111 -> 110.  One block ahead
+    // where that would take more registers than there are (tiles of 128 rows, heads of 128: prompts of 2048 61 us with it, 57 without).
     constexpr bool EARLY = DP != 128 || (!SPLIT && PIECES == 1);
     typedef typename E::T T;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), half = lane >> 5, col = lane & 31;
@@ -873,7 +889,8 @@ __global__ __launch_bounds__(C::NW * 64, C::PER_SIMD) void attention_chunk_kerne
         }
 }
 
-// The parts of a tile, joined in their order: `blocks` workgroups a tile, DP / 8 / blocks pieces of 4 elements of a lane each.
+// The parts of a tile, joined in their order: `blocks` workgroups a tile, DP / 8 / blocks pieces of 4 elements of a lane each.  A launch of its own after the parts: 8 - 13 us,
+// of which the trips to the lengths and to the first parts are 3; one part at a time instead of eight on their way together 20.
 template <class E, class C>
 __global__ __launch_bounds__(C::NW * 64) void attention_chunk_join_kernel(const ChunkArgs a, int blocks)
 {

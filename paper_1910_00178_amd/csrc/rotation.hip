@@ -119,7 +119,9 @@ ngemm_status ngemm_qk_norm_rotate(ngemm_ctx *ctx, ngemm_type type, int64_t head_
         vec = vec && in_pieces(from[i], type) && in_pieces(to[i], type);
     }
     const int64_t lanes = head_dim <= 64 ? 4 : head_dim <= 128 ? 8 : 16, rows = tokens * (q_heads + k_heads);
-    const int64_t U = rows * lanes >= (int64_t)4 * 64 * 2048 ? 4 : 1;
+    // Four heads an item where that leaves some wavefronts for each SIMD: tokens of 32 + 8 heads of 128, bf16, with four and with one: 64 tokens 5.8 and 4.0 us, 512 6.2 and 6.3,
+    // 800 6.8 and 7.8, 1600 10.2 and 13.9, 10000 45 and 62
+    const int64_t U = rows * lanes >= (int64_t)3 * 64 * 1024 ? 4 : 1;
     const int64_t chunks_q = (q_heads + U - 1) / U, chunks = chunks_q + (k_heads + U - 1) / U, items = tokens * chunks;
     const int64_t groups = (items + 256 / lanes - 1) / (256 / lanes);
     if (groups > kMaxGroups) return NGEMM_ERR_BAD_SHAPE;
@@ -154,7 +156,7 @@ ngemm_status ngemm_kv_write_rotated(ngemm_ctx *ctx, const ngemm_kv_cache *cache,
     if (const ngemm_status s = plan_move(plan, ctx, cache, type, batch, tokens, k, v, offsets_dev, pages_dev, pages_stride, false); s != NGEMM_OK) return s;
     if (const ngemm_status s = check_turn(ctx, rotation, cache->head_dim, eps, k_weight_dev, nullptr); s != NGEMM_OK) return s;
     if (plan.groups == 0) return NGEMM_OK;
-    // four heads of a workgroup share a token's angles and weights where that leaves some thousands of workgroups (15800 tokens of 8 heads, written and read
+    // four heads of a workgroup share a token's angles and weights where that leaves some thousands of workgroups (17200 tokens of 8 heads, written and read
     // back: 53.5 us with four, 55.5 with two, 59 with one; 64 sequences of a token 14.5 with four, 9.5 with one)
     if (plan.slots * cache->kv_heads >= 8192 && plan.heads < 4) {
         plan.heads = (int32_t)std::min<int64_t>(cache->kv_heads, 4);
