@@ -514,7 +514,7 @@ ngemm_status ngemm_attention_decode(ngemm_ctx *ctx, const ngemm_kv_cache *cache,
  * alone), at the positions starts[b], starts[b] + 1, ... (starts_dev: int32 [batch], or NULL for 0).  The row at position p sees the tokens t <= p, with
  * a window (not 0) only t > p - window and the first `sinks` ones:
  *     O = sum_t w_t V_t / sum_t w_t,  w_t = exp(scale <Q, K_t> - max)
- * with the K and V of head h / (q_heads / kv_heads) (q_heads a multiple of the cache's kv_heads).  A row that sees nothing gives 0; what a row does not
+ * with the K and V of head h / (q_heads / kv_heads) (q_heads a multiple of the cache's kv_heads).  A row that sees nothing, or whose scores are all minus infinity, gives 0; what a row does not
  * see is without effect on it, NaN included; tokens in a page that is not one of the cache's are left out.  max_new: the most new tokens of a
  * sequence, max_length: the most tokens of one with them (up to 2^30); larger numbers are right as well, and slower, since the launches and the workspace are
  * sized by them.  With smaller ones a sequence's rows past the first max_new are left alone, and tokens from max_length on are not read.  window and
