@@ -535,7 +535,7 @@ struct ChunkCfg {
 // keys of each 16, which is the second product's operand as they lie.
 // A softmax in one pass, with a reference that need not be the maximum: weights are exp2(s - m), m a score that was the largest once; a block whose weights sum up to more than 2^12 in a lane
 // sets it anew.  Most blocks then have no maximum, no exchange between lanes and no sums to rescale.
-// bf16 rows: weights times V's scales rounded to bf16 (2^-9 of each, as matrix instructions take them; the formula's error 2.4e-3 of the norm for 1.7e-3 with weights in 32 bits). f16 rows:
+// bf16 rows: weights times V's scales rounded to bf16 (2^-8 of each at most, as matrix instructions take them; the formula's error 2.4e-3 of the norm for 1.7e-3 with weights in 32 bits). f16 rows:
 // two bf16 numbers, 16 bits, since one alone is less than the rows' own 11.
 // Bound: per 32 x 32 scores of heads of 128 the matrix unit takes 16 instructions of 16 cycles and the vector unit some 190; one wavefront's instructions of either kind keep the other's of the
 // same SIMD waiting (12 multiply-adds beside one matrix instruction: 113 - 120 cycles of two wavefronts, 67 and 65 of either alone), so a prompt of 8192 (32 heads on 8) takes

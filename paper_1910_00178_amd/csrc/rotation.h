@@ -193,7 +193,7 @@ struct TurnedMoveArgs {
 };
 
 // kv_write_kernel with K's rows normalised and turned in floats before their maximum is found: LANES lanes a token, two pieces each.  Codes are of the 32-bit
-// results: a rounding to the type in between would be of 2^-9 in bf16, half as much as the codes' own of a 254th of the largest.
+// results: a rounding to the type in between would be of 2^-8 in bf16, as much again as the codes' own, a 254th of the largest.
 // Bound by memory where tokens are many: 17 200 tokens of 8 heads of 128, bf16, 31 us (3.4 TB/s); vector instructions are next (some 12 an element).
 template <class E, int LANES, int PAIRS, bool VEC>
 __global__ __launch_bounds__(16 * LANES) void kv_write_rotated_kernel(const TurnedMoveArgs args)
