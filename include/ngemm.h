@@ -521,7 +521,7 @@ ngemm_status ngemm_attention_decode(ngemm_ctx *ctx, const ngemm_kv_cache *cache,
  * sinks up to 2^30.  Softmax statistics and sums are float; scores are products of the 8-bit codes and the queries as they are; the weights w_t
  * times V's scales enter the second product as bf16 (bf16 rows) or as the sum of two bf16 numbers, 16 bits (f16 rows, and bf16 ones of sequences of at most 16, in small
  * batches 64, new tokens times q_heads / kv_heads), so that they have the floats' range; in units where the largest of a row's is 2^12 at most, so that values of up to 2^90 in
- * magnitude do not overflow sums.  O may stand in Q's place (same address and strides); else it overlaps no input.  The keys of a sequence are shared out over workgroups
+ * magnitude do not overflow sums, and those from 2^-100 on keep these bits.  O may stand in Q's place (same address and strides); else it overlaps no input.  The keys of a sequence are shared out over workgroups
  * by the lengths that the device holds; the parts meet in the workspace and are joined in their order, so that equal calls give equal bits.  The workspace has to
  * be 16-byte aligned and must not be in use by a call on another stream.  Rows of Q and O of the usual strides and 16-byte alignment move in 16-byte pieces.
  */

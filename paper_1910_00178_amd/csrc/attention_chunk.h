@@ -250,9 +250,9 @@ constexpr int few_waves_per_simd(int D, int R, int NW) { return D * R <= 128 || 
 // tiles of 64 keys = 4 blocks: S^T = K Q^T and O^T = V^T P^T on 16 x 16 x 32 matrix instructions.  Row r of the first product's tile t is
 // token 4 t + r % 4 of block r / 4, so that lane 16 g + h holds row h's scores of block g's tokens, which is what the second product wants of it:
 // codes go from memory to registers, become floats there and meet the matrix unit, without LDS.
-// A softmax in one pass: weights are exp2(s - m), m 2^8 above the largest score when it was set, so that it is set again only where a score passes it.  The weights
-// times V's scales enter the second product as two bf16 numbers each, 16 bits: the products are few, and a row of a batch of single tokens keeps the bits that
-// attention_decode gives it.
+// A softmax in one pass: weights are exp2(s - m), the largest of them 2^4 when m was set, which it is again only where one passes 2^12.  The weights times V's scales
+// enter the second product as two bf16 numbers each, 16 bits (the products are few): no fewer than attention_decode's weights have.  A bf16 number's last
+// bits are lost below 2^-126, and the second's are 2^-16 of the weight: values of 2^-100 in magnitude keep all of them (weights of 1 at most lost 2^-9 of values of 2^-110).
 // Bound by memory where a key is read for one tile: 32 sequences of 4 tokens behind 8000 (8 heads of 128) 97 us, 5.6 TB/s; by the chain of trips (lengths, pages, codes) in
 // small calls: 32 single tokens behind 500 9 us.
 template <class E, int D, int R, int NW>
@@ -372,9 +372,9 @@ __global__ __launch_bounds__(NW * 64, few_waves_per_simd(D, R, NW)) void attenti
             float most = x[0][0];
 #pragma unroll
             for (int e = 1; e < 16; ++e) most = fmaxf(most, x[e / 4][e % 4]);
-            if (__any(most > m[r])) {                    // weights are 1 at most, and 2^-8 or more for the largest
+            if (__any(most > m[r] + 12.0f)) {            // weights are 2^12 at most, and 2^4 or more for the largest
                 most = max_of_rows(most);
-                const float next = most > m[r] ? most + 8.0f : m[r], fall = __builtin_amdgcn_exp2f(m[r] - next);
+                const float next = most > m[r] + 12.0f ? most - 4.0f : m[r], fall = __builtin_amdgcn_exp2f(m[r] - next);
                 l[r] *= fall;
                 m[r] = next;
 #pragma unroll
