@@ -193,13 +193,7 @@ struct ChunkUnit {
 };
 
 // Four codes as 16-bit floats, in order.
-__device__ __forceinline__ u2 codes4_to(F16, uint32_t x)
-{
-    const uint32_t y = x ^ kCodeSigns;
-    const h2 base = {(_Float16)-1152.0f, (_Float16)-1152.0f};
-    return (u2){__builtin_bit_cast(uint32_t, __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, y, 0x04010400u)) + base),
-                __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, y, 0x04030402u)) + base)};
-}
+__device__ __forceinline__ u2 codes4_to(F16, uint32_t x) { return codes4_to_f16(x); }
 __device__ __forceinline__ u2 codes4_to(BF16, uint32_t x)
 {
     float f[4];

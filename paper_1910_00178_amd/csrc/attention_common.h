@@ -58,18 +58,22 @@ __device__ __forceinline__ float sum_of_rows(float x)
     return sum_of_halves(__uint_as_float(s[0]) + __uint_as_float(s[1]));
 }
 
-// 16 codes as 16-bit floats, in order.  A code with its sign bit turned, as the low byte under 0x64, is the float 1024 + 128 + code.
+// Codes as 16-bit floats, in order: four, and 16.  A code with its sign bit turned, as the low byte under 0x64, is the float 1024 + 128 + code.
 constexpr uint32_t kCodeSigns = 0x80808080u;
+__device__ __forceinline__ u2 codes4_to_f16(uint32_t x, uint32_t signs = kCodeSigns)
+{
+    const uint32_t y = x ^ signs;
+    const h2 base = {(_Float16)-1152.0f, (_Float16)-1152.0f};
+    return (u2){__builtin_bit_cast(uint32_t, __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, y, 0x04010400u)) + base),
+                __builtin_bit_cast(uint32_t, __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, y, 0x04030402u)) + base)};
+}
 __device__ __forceinline__ void codes_to_f16(u4 x, u4 (&out)[2], uint32_t signs = kCodeSigns)
 {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-        const uint32_t y = x[e] ^ signs;
-        const h2 base = {(_Float16)-1152.0f, (_Float16)-1152.0f};
-        const h2 lo = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, y, 0x04010400u)) + base;
-        const h2 hi = __builtin_bit_cast(h2, __builtin_amdgcn_perm(0x64646464u, y, 0x04030402u)) + base;
-        out[e / 2][2 * (e % 2)] = __builtin_bit_cast(uint32_t, lo);
-        out[e / 2][2 * (e % 2) + 1] = __builtin_bit_cast(uint32_t, hi);
+        const u2 y = codes4_to_f16(x[e], signs);
+        out[e / 2][2 * (e % 2)] = y[0];
+        out[e / 2][2 * (e % 2) + 1] = y[1];
     }
 }
 

@@ -207,6 +207,30 @@ __device__ __forceinline__ void transpose_bytes(uint32_t (&x)[4])
     x[3] = __builtin_amdgcn_perm(d, b, 0x07060302u);
 }
 
+// V's codes of a block, whose tokens m.begin .. m.end - 1 lie in LDS as `rows`, four elements a dword, into the block as it holds them: a thread takes tokens
+// 4 t .. 4 t + 3 of elements 4 q .. 4 q + 3.
+template <int THREADS, int N>
+__device__ __forceinline__ void store_turned(uint8_t *block, const uint32_t (&rows)[16][N], const MoveBlock &m, int D)
+{
+    for (int i = threadIdx.x; i < D; i += THREADS) {
+        const int t = i & 3, q = i >> 2;
+        uint32_t x[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[j] = rows[4 * t + j][q];
+        transpose_bytes(x);
+        uint8_t *to = block + 16 * D + 64 * q + 4 * t;
+        if (4 * t >= m.begin && 4 * t + 4 <= m.end) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) *(uint32_t *)(to + 16 * j) = x[j];
+        } else {
+            for (int u = 0; u < 4; ++u)
+                if (4 * t + u >= m.begin && 4 * t + u < m.end)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) to[16 * j + u] = (uint8_t)(x[j] >> (8 * u));
+        }
+    }
+}
+
 // Codes of eight elements.  127 x / amax as one product is off by less than 2^-14 (its and the factor's roundings); where that could
 // matter for a tie, and for rows of very small numbers, the quotient is formed as the definition says: 127 x relative to a power
 // of two (exact for 16-bit types), one correctly rounded division.
@@ -301,23 +325,7 @@ __global__ __launch_bounds__(16 * LANES) void kv_write_kernel(const MoveArgs a)
             if (there && piece == 0) ((float *)(block + 32 * D))[16 * which + token] = finite ? most / 127.0f : __builtin_nanf("");
         }
         __syncthreads();                                 // (the next head writes the other half)
-        for (int i = tid; i < D; i += 16 * LANES) {             // tokens 4 t .. 4 t + 3 of elements 4 q .. 4 q + 3
-            const int t = i & 3, q = i >> 2;
-            uint32_t y[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) y[j] = turned[turn][4 * t + j][q];
-            transpose_bytes(y);
-            uint8_t *to = block + 16 * D + 64 * q + 4 * t;
-            if (4 * t >= m.begin && 4 * t + 4 <= m.end) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) *(uint32_t *)(to + 16 * j) = y[j];
-            } else {
-                for (int u = 0; u < 4; ++u)
-                    if (4 * t + u >= m.begin && 4 * t + u < m.end)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) to[16 * j + u] = (uint8_t)(y[j] >> (8 * u));
-            }
-        }
+        store_turned<16 * LANES>(block, turned[turn], m, D);
     }
 }
 

@@ -248,23 +248,7 @@ __global__ __launch_bounds__(16 * LANES) void kv_write_rotated_kernel(const Turn
         }
         if (head + 1 < end) load(head + 1);              // on their way while this head's codes are turned and stored
         __syncthreads();                                 // (the next head writes the other half)
-        for (int i = tid; i < D; i += 16 * LANES) {      // tokens 4 t .. 4 t + 3 of elements 4 q .. 4 q + 3
-            const int t = i & 3, q = i >> 2;
-            uint32_t x[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) x[j] = turned[turn][4 * t + j][q];
-            transpose_bytes(x);
-            uint8_t *to = block + 16 * D + 64 * q + 4 * t;
-            if (4 * t >= m.begin && 4 * t + 4 <= m.end) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) *(uint32_t *)(to + 16 * j) = x[j];
-            } else {
-                for (int u = 0; u < 4; ++u)
-                    if (4 * t + u >= m.begin && 4 * t + u < m.end)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) to[16 * j + u] = (uint8_t)(x[j] >> (8 * u));
-            }
-        }
+        store_turned<16 * LANES>(block, turned[turn], m, D);
     }
 }
 
