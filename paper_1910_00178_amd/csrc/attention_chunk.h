@@ -31,7 +31,6 @@ struct ChunkSequence {
         first = min(max(begin, 0), a.tokens);
         queries = min(min(max(end, first), a.tokens) - first, a.max_new);
     }
-    __device__ __forceinline__ int position(int query) const { return (int)min(max(start + query, (int64_t)-1), (int64_t)0x7ffffffe); }
 };
 
 __device__ __forceinline__ uint64_t low_bits(int n) { return n <= 0 ? 0 : n >= 64 ? ~(uint64_t)0 : ((uint64_t)1 << n) - 1; }
