@@ -518,7 +518,7 @@ ngemm_status ngemm_attention_decode(ngemm_ctx *ctx, const ngemm_kv_cache *cache,
  * see is without effect on it, NaN included; tokens in a page that is not one of the cache's are left out.  max_new: the most new tokens of a
  * sequence, max_length: the most tokens of one with them (up to 2^30); larger numbers are right as well, and slower, since the launches and the workspace are
  * sized by them.  With smaller ones a sequence's rows past the first max_new are left alone, and tokens from max_length on are not read.  window and
- * sinks up to 2^30.  Softmax statistics and sums are float; scores are products of the 8-bit codes and the queries as they are; the weights w_t
+ * sinks up to 2^30; scale up to 2^127 in magnitude.  Softmax statistics and sums are float; scores are products of the 8-bit codes and the queries as they are; the weights w_t
  * times V's scales enter the second product as bf16 (bf16 rows) or as the sum of two bf16 numbers, 16 bits (f16 rows, and bf16 ones of sequences of at most 16, in small
  * batches 64, new tokens times q_heads / kv_heads), so that they have the floats' range; in units where the largest of a row's is 2^12 at most, so that values of up to 2^90 in
  * magnitude do not overflow sums, and those from 2^-100 on keep these bits.  O may stand in Q's place (same address and strides); else it overlaps no input.  The keys of a sequence are shared out over workgroups

@@ -10,6 +10,7 @@ using namespace ngemm;
 namespace {
 
 constexpr int64_t kUnits = 256;
+constexpr float kLog2E = 1.44269504f;
 constexpr int kWideFew = 192;                                    // heads that leave registers for eight wavefronts
 constexpr int64_t kFewRows = 64;                                 // of a sequence, that attention_chunk_few_kernel takes at most, in tiles of 16 or 32
 
@@ -175,7 +176,7 @@ ngemm_status ngemm_attention_chunk(ngemm_ctx *ctx, const ngemm_kv_cache *cache, 
                                    void *workspace_dev, size_t workspace_bytes, void *hip_stream)
 {
     if (!ctx_ok(ctx) || !cache_ok(cache) || cache->device != ctx->device) return NGEMM_ERR_INVALID_ARG;
-    if ((type != NGEMM_F16 && type != NGEMM_BF16) || !std::isfinite(scale)) return NGEMM_ERR_INVALID_ARG;
+    if ((type != NGEMM_F16 && type != NGEMM_BF16) || !std::isfinite(scale * kLog2E)) return NGEMM_ERR_INVALID_ARG;
     const int64_t kv_heads = cache->kv_heads, head_dim = cache->head_dim;
     if (!sizes_ok(batch, q_heads, kv_heads, head_dim, tokens, max_new, max_length, window, sinks) || pages_stride < 0 || pages_stride > kMaxCount)
         return NGEMM_ERR_BAD_SHAPE;
@@ -195,7 +196,7 @@ ngemm_status ngemm_attention_chunk(ngemm_ctx *ctx, const ngemm_kv_cache *cache, 
     DeviceGuard g(ctx->device);
     if (!g.ok) return NGEMM_ERR_DEVICE;
     const ChunkArgs a{view_of(cache, pages_dev, pages_stride), q, o, offsets_dev, starts_dev, (int32_t)batch, (int32_t)q_heads, (int32_t)tokens, (int32_t)max_new,
-                      pages_stride > 0 ? (int32_t)max_length : 0, (int32_t)window, (int32_t)sinks, scale * 1.44269504f, 0, 0, 0.0f, nullptr, in_pieces(o, type)};
+                      pages_stride > 0 ? (int32_t)max_length : 0, (int32_t)window, (int32_t)sinks, scale * kLog2E, 0, 0, 0.0f, nullptr, in_pieces(o, type)};
     const bool vec = in_pieces(q, type) && in_pieces(o, type);
     hipStream_t st = (hipStream_t)hip_stream;
     const bool ok = type == NGEMM_F16 ? launch_chunk<F16>(a, cut, vec, (uint8_t *)workspace_dev, ctx->device, st)
