@@ -522,7 +522,10 @@ ngemm_status ngemm_attention_decode(ngemm_ctx *ctx, const ngemm_kv_cache *cache,
  * times V's scales enter the second product as bf16 (bf16 rows) or as the sum of two bf16 numbers, 16 bits (f16 rows, and bf16 ones of sequences of at most 16, in small
  * batches 64, new tokens times q_heads / kv_heads), so that they have the floats' range; in units where the largest of a row's is 2^12 at most, so that values of up to 2^90 in
  * magnitude do not overflow sums, and those from 2^-100 on keep these bits.  O may stand in Q's place (same address and strides); else it overlaps no input.  The keys of a sequence are shared out over workgroups
- * by the lengths that the device holds; the parts meet in the workspace and are joined in their order, so that equal calls give equal bits.  The workspace has to
+ * by the lengths that the device holds where the call's sizes leave too few workgroups otherwise: up to 128 sequences, and of up to 16 rows (new tokens times q_heads / kv_heads) less
+ * than 128 sequences times kv_heads (512 with heads of more than 192), of more rows less than 512 tiles of them times kv_heads, 256 in some forms.  In other calls (those that need no workspace) a
+ * workgroup takes all keys of its rows, so that a sequence much longer than the others bounds them: 64 single tokens on 8 K/V heads, one behind 32768 and the others behind 300,
+ * take 4 times as long as in ngemm_attention_decode.  The parts meet in the workspace and are joined in their order, so that equal calls give equal bits.  The workspace has to
  * be 16-byte aligned and must not be in use by a call on another stream.  Rows of Q and O of the usual strides and 16-byte alignment move in 16-byte pieces.
  */
 size_t ngemm_attention_chunk_workspace_bytes(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t head_dim, int64_t tokens, int64_t max_new,

@@ -530,9 +530,9 @@ struct ChunkCfg {
 // sets it anew.  Most blocks then have no maximum, no exchange between lanes and no sums to rescale.
 // bf16 rows: weights times V's scales rounded to bf16 (2^-8 of each at most, as matrix instructions take them; the formula's error 2.4e-3 of the norm for 1.7e-3 with weights in 32 bits). f16 rows:
 // two bf16 numbers, 16 bits, since one alone is less than the rows' own 11.
-// Bound: per 32 x 32 scores of heads of 128 the matrix unit takes 16 instructions of 16 cycles and the vector unit some 190; one wavefront's instructions of either kind keep the other's of the
+// Bound: per 32 x 32 scores of heads of 128 the matrix unit takes 16 instructions of 32 cycles and the vector unit some 150; one wavefront's instructions of either kind keep the other's of the
 // same SIMD waiting (12 multiply-adds beside one matrix instruction: 113 - 120 cycles of two wavefronts, 67 and 65 of either alone), so a prompt of 8192 (32 heads on 8) takes
-// 550 us, the matrix unit busy 45 %, the vector unit 60 %, at 1.7 - 2.0 GHz. Hence what is not here: a maximum per block, conversions per wavefront, masks in tiles that all rows see.
+// 560 us, the matrix unit busy 45 % of the cycles, at 1.7 - 2.0 GHz. Hence what is not here: a maximum per block, conversions per wavefront, masks in tiles that all rows see.
 template <class E, class C, bool VEC>
 __global__ __launch_bounds__(C::NW * 64, C::PER_SIMD) void attention_chunk_kernel(const ChunkArgs a)
 {

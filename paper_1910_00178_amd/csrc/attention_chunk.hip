@@ -59,6 +59,8 @@ ChunkCut chunk_cut(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t hea
         // A tile's keys by eight wavefronts of one workgroup where that fills half of the units at least: 16 x 4 tokens behind 1000 14.5, shared out and joined 19.5;
         // 32 x 4 behind 8000 97 and 107 (16 x 4 behind 8000 57 and 51).  By four of one workgroup from two workgroups a unit on: 64 x 4 behind 1000 26.5 (by eight 32),
         // 256 x 4 behind 500 52 (82).  Else shared out over workgroups: 8 x 4 behind 8000 34 (whole 54).
+        // (By the sizes alone, as lengths of one kind want it: where one sequence is much longer than the others it bounds a call whose keys are whole.  Single tokens behind 300 and
+        // one behind 32768: 15 sequences, shared out, 32; 16, by eight wavefronts, 190; 64, by four, 229.)
         if (grid >= kUnits / 2 && grid < 2 * kUnits && cut.few_rows <= 16 && head_dim <= kWideFew) cut.few_waves = 8;
         else if (grid < 2 * kUnits && batch <= kMostShared && most_tiles(std::min(most_new, height / group + 2), max_length, window, sinks) >= 2 * kLeastTiles) {
             cut.few_places = std::max(height / 16 * head_dim <= 128 ? 2 * kUnits : kUnits, kv_heads);
@@ -69,6 +71,9 @@ ChunkCut chunk_cut(int64_t batch, int64_t q_heads, int64_t kv_heads, int64_t hea
     if (most_rows > cut.few_rows) {
         // 256 rows a workgroup convert a key once where two of 128 do it twice, but leave coarser pieces of work: prompts of 4096 155 us (128 rows: 169), 16 x 256 behind
         // 2000 166 (177), 512 behind 16000 111 (120); a prompt of 2048 65 (57), 64 x 256 135 (120), 64 x 512 309 (293).
+        // Windows are alike, by what a row sees: of 10000 tokens, window 4096 572 (600), 1000 230 (228), 256 122 (117); 4 x 2500, window 1000 208 (199), 256 117 (110); f16 the same to 2 %.
+        // Not so where keys are shared out: 2000 tokens, window 1000 49 (56), 512 35 (44).
+        // (Heads of 128; those of 64 are faster with 128 rows beyond 1024 too: 4 x 2500 of 12 heads 118 (94), 10000 255 (247).)
         const int64_t seen = window > 0 ? std::min(max_length, window + sinks) : max_length - std::min(max_length, most_new) / 2;       // by a row, about
         cut.wide = tokens * group / batch >= 256 && seen > 1024;
         const int64_t height = tile_rows(head_dim, cut.wide), places = cut.wide || head_dim > 128 ? kUnits : 2 * kUnits;

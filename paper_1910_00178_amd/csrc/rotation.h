@@ -145,7 +145,7 @@ struct TurnArgs {
 
 // LANES lanes take U heads of a token, one item: its angles and weights are read once, and the rows are on their way together.  All of an
 // item's rows are read before any is written, so outputs may stand in their inputs' places.  The sums of squares are floats, and the result is rounded to the type once.
-// Bound by memory, a read and a write of every row: 9900 tokens of 32 + 8 heads of 128, bf16, 46 us = 4.4 TB/s (a large copy: 4.9).
+// Bound by memory, a read and a write of every row: 9900 tokens of 32 + 8 heads of 128, bf16, 46 us = 4.4 TB/s, f32 84 us = 4.9 (a large copy: 4.9).
 template <class E, int LANES, int PAIRS, int U, bool VEC>
 __global__ __launch_bounds__(256) void qk_norm_rotate_kernel(const TurnArgs a)
 {
@@ -194,7 +194,8 @@ struct TurnedMoveArgs {
 
 // kv_write_kernel with K's rows normalised and turned in floats before their maximum is found: LANES lanes a token, two pieces each.  Codes are of the 32-bit
 // results: a rounding to the type in between would be of 2^-8 in bf16, as much again as the codes' own, a 254th of the largest.
-// Bound by memory where tokens are many: 17 200 tokens of 8 heads of 128, bf16, 31 us (3.4 TB/s); vector instructions are next (some 12 an element).
+// Bound by memory where tokens are many: 17 200 tokens of 8 heads of 128, bf16, 31 us (3.4 TB/s), f32 34 (5.3 TB/s); vector instructions are next (some 21 an element of K
+// and V, bf16).
 template <class E, int LANES, int PAIRS, bool VEC>
 __global__ __launch_bounds__(16 * LANES) void kv_write_rotated_kernel(const TurnedMoveArgs args)
 {
